@@ -394,6 +394,113 @@ int moe_probe_h2d_copy(const void *host_src, void *dev_dst, size_t bytes, int wo
  * MOE_ERR_ARG for bad arguments, MOE_ERR_HIP for runtime failures. */
 int moe_probe_mfma_bf16(int shape, int iters, void *stream, double *tflops);
 
+/* ---------------------------------------------------------------------------
+ * The attention half of a layer, kept small beside the experts: products with
+ * 4-bit weights (the measured model's attention weights, Sec. 5.1: 4-bit codes,
+ * groups of 64, compressed zero points), a paged cache of keys and values in 4
+ * bits, attention over it, and the norms around a block.
+ *
+ * These calls take no handle.  They enqueue work on `stream` (a hipStream_t,
+ * NULL: the default stream) of the current device and return; all pointers are
+ * device memory of that device and must stay valid until the work is done.
+ * `dtype` is MOE_DTYPE_F32 or MOE_DTYPE_BF16, the type of all inputs and
+ * outputs not said to be something else; sums and softmax statistics are fp32,
+ * fp32 operands take part whole (no rounding to bf16).  Strides are in
+ * elements between rows (tokens); a row itself is contiguous.  Pointers and
+ * strides must be multiples of 16 bytes unless said otherwise.  With no rows
+ * (tokens) a call checks its arguments and does nothing.  MOE_ERR_ARG: a bad
+ * argument (moe_last_error says which); MOE_ERR_HIP: a launch failed. */
+
+/* Bytes of one 4-bit matrix [n x k]; 0 unless n >= 1 and k is a positive
+ * multiple of 64.  Three planes back to back: codes [n][k/2] bytes (column c in
+ * nibble c % 2 of byte c / 2, low nibble first), fp16 scales [n][k/64], uint8
+ * zero codes [n][k/64] (zero point = code/16); weight = (q - zero) * scale.
+ * 4.375 bits a weight. */
+size_t moe_q4_matrix_bytes(size_t n, size_t k);
+
+/* y[t][i] = sum_c x[t][c] W[i][c] for rows 0 <= t < rows (at most 2^20), W a
+ * 4-bit matrix [n x k] at w.  y's pointer and stride need only be aligned to
+ * their type.  A row of x with an infinity or a NaN gives a row of NaN. */
+int moe_q4_matmul(const void *x, int64_t x_stride, const void *w, void *y, int64_t y_stride, int rows, int n, int k,
+                  int dtype, void *stream);
+
+/* A paged cache of keys and values in 4 bits and a batch of sequences over it.
+ * A page holds page_size tokens of every kv head, [pages][kv_heads][record];
+ * a record is page_size * head_dim * 9 / 8 bytes:
+ *   key codes    [P][D/2] bytes          dimension c in nibble c % 2 of byte c / 2
+ *   value codes  [P/4][D/8][4] uint32    eight dimensions (nibble c % 8) of each of 4 tokens
+ *   key metas    [P][D/32] uint16        scale code k << 8 | zero z of 32 dimensions
+ *   value metas  [P/4][D/32][4] uint16
+ * A stored value is (q - z) * s, s = (8 + k % 8) * 2^(k/8 - 24), k <= 254; for
+ * 32 values x, lo = min(0, min x), hi = max(0, max x): k is the smallest with
+ * 15 s >= hi - lo (254 if there is none), z = rint(-lo / s), q = rint(x / s) + z,
+ * both clipped to 0..15.  A group with an infinity or a NaN gets k = 255 and
+ * reads as NaN.  Values have 8 significant bits at most: exact in bf16.
+ * Sequence b has kv_len[b] tokens, of which the last q_start[b+1] - q_start[b]
+ * are new in this call, rows q_start[b] .. of the call's tensors; new token i
+ * of n has position kv_len[b] - n + i.  The caller sees to q_start[0] == 0,
+ * q_start[seqs] == tokens and ascending entries.  Position p lies in page
+ * page_table[b][p / page_size]; an entry outside 0..pages-1, a column past
+ * table_cols or a negative position (kv_len[b] < n) means that there is no
+ * such token: it is not stored, not attended to and reads as zeros. */
+typedef struct {
+  void *pool;                /* device, 16-byte aligned                            */
+  const int32_t *page_table; /* device [seqs][table_cols]                          */
+  const int32_t *q_start;    /* device [seqs + 1]                                  */
+  const int32_t *kv_len;     /* device [seqs], this call's tokens included         */
+  int64_t table_stride;      /* entries between rows of page_table, >= table_cols  */
+  int pages, page_size;      /* page_size: a power of two in [16, 1024]            */
+  int kv_heads, head_dim;    /* head_dim: 64 or 128                                */
+  int table_cols;            /* table_cols * page_size <= 2^30                     */
+  int seqs, tokens;          /* tokens: new tokens of all sequences                */
+} moe_kv4_batch;
+
+/* Rotate and append: every new token's query heads and key heads are rotated
+ * by its position p, pairs (a, b) = (x[i], x[i + rot_dim/2]), i < rot_dim/2,
+ * becoming (a cos[p][i] - b sin[p][i], b cos[p][i] + a sin[p][i]); dimensions
+ * from rot_dim on stay.  Queries [tokens][heads][head_dim] go to q_out, keys
+ * and values [tokens][kv_heads][head_dim] into the cache.  cos and sin are fp32
+ * [max_pos][rot_dim/2], contiguous; rot_dim a multiple of 16, 0 for no
+ * rotation (cos and sin may then be NULL; max_pos still counts).  A token at a
+ * position past max_pos - 1 is not stored and its query is zeros.  q_out may be
+ * q itself only without rotation.  Other bytes of the cache stay as they are. */
+int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                   const void *v, int64_t v_stride, const float *cos, const float *sin, int max_pos, int rot_dim,
+                   void *q_out, int64_t q_out_stride, int heads, int dtype, void *stream);
+
+/* The stored keys and values of the batch's new tokens, to k and v
+ * [tokens][kv_heads][head_dim], contiguous (with q_start the sums of kv_len:
+ * of all tokens).  Exact in both types. */
+int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stream);
+
+/* Attention of every new token over its sequence's cache, itself and what is
+ * before it: o[t][h] = sum_j softmax_j(scale q[t][h] . K[j][h']) V[j][h'], h'
+ * = h / (heads / kv_heads); heads a multiple of kv_heads.  A row that sees no
+ * token gets zeros.  What a row does not see does not reach it, NaN included.
+ * max_new (new tokens of a sequence) and max_len (tokens of a sequence) say how
+ * the work is best cut; results are right whatever they are.  The workspace
+ * (16-byte aligned; NULL if it is 0 bytes) must hold
+ * moe_kv4_attention_workspace_bytes for the same batch, heads, max_new and
+ * max_len (0 for invalid arguments as well). */
+size_t moe_kv4_attention_workspace_bytes(const moe_kv4_batch *b, int heads, int max_new, int max_len);
+int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, void *o, int64_t o_stride, int heads,
+                      float scale, int dtype, int max_new, int max_len, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
+/* Norms before and after a block with its gate and residual scale, for rows of
+ * d (a multiple of 8 in [8, 16384]) channels:
+ *   h_out = residual_scale * h + gate * y',   y' = y * post / rms(y)
+ *   x_out = h_out * pre / rms(h_out),         rms(v) = sqrt(mean(v^2) + eps)
+ * y is what the block gave (dtype), h the residual stream (fp32), x_out the
+ * next block's input (dtype), h_out fp32.  post and pre are fp32 [d], gate fp32
+ * [d] (gate_stride 0) or [rows][d].  May be NULL: y (h_out = residual_scale *
+ * h), post (y' = y), gate (1), pre (1), h_out or x_out (not wanted; not both).
+ * h_out may be h, and x_out y, at the same stride. */
+int moe_norm_residual(const float *h, int64_t h_stride, const void *y, int64_t y_stride, const float *gate,
+                      int64_t gate_stride, const float *post, const float *pre, float residual_scale, float eps,
+                      float *h_out, int64_t h_out_stride, void *x_out, int64_t x_stride, int rows, int d, int dtype,
+                      void *stream);
+
 /* Thread-local message of the last failure on this thread ("" if none). */
 const char *moe_last_error(void);
 

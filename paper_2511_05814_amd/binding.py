@@ -83,6 +83,18 @@ class moe_timing(ctypes.Structure):
                    ("pf_fetch_ms", ctypes.c_double), ("pf_fetch_n", ctypes.c_uint64)])
 
 
+class moe_kv4_batch(ctypes.Structure):
+    _fields_ = [
+        ("pool", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("q_start", ctypes.c_void_p),
+        ("kv_len", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+        ("pages", ctypes.c_int), ("page_size", ctypes.c_int), ("kv_heads", ctypes.c_int),
+        ("head_dim", ctypes.c_int), ("table_cols", ctypes.c_int), ("seqs", ctypes.c_int),
+        ("tokens", ctypes.c_int),
+    ]
+
+
+_P, _I, _I64, _F = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float
+
 # (name, restype, argtypes) of every exported function, in header order
 _SIGNATURES = [
     ("moe_cache_create", ctypes.c_int,
@@ -120,6 +132,16 @@ _SIGNATURES = [
      [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
       ctypes.POINTER(ctypes.c_double)]),
     ("moe_probe_mfma_bf16", ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.POINTER(ctypes.c_double)]),
+    ("moe_q4_matrix_bytes", ctypes.c_size_t, [ctypes.c_size_t, ctypes.c_size_t]),
+    ("moe_q4_matmul", _I, [_P, _I64, _P, _P, _I64, _I, _I, _I, _I, _P]),
+    ("moe_kv4_append", _I,
+     [ctypes.POINTER(moe_kv4_batch), _P, _I64, _P, _I64, _P, _I64, _P, _P, _I, _I, _P, _I64, _I, _I, _P]),
+    ("moe_kv4_read", _I, [ctypes.POINTER(moe_kv4_batch), _P, _P, _I, _P]),
+    ("moe_kv4_attention_workspace_bytes", ctypes.c_size_t, [ctypes.POINTER(moe_kv4_batch), _I, _I, _I]),
+    ("moe_kv4_attention", _I,
+     [ctypes.POINTER(moe_kv4_batch), _P, _I64, _P, _I64, _I, _F, _I, _I, _I, _P, ctypes.c_size_t, _P]),
+    ("moe_norm_residual", _I,
+     [_P, _I64, _P, _I64, _P, _I64, _P, _P, _F, _F, _P, _I64, _P, _I64, _I, _I, _I, _P]),
     ("moe_last_error", ctypes.c_char_p, []),
 ]
 EXPORTED = [s[0] for s in _SIGNATURES]
@@ -288,3 +310,41 @@ def moe_entropy_pack(w_ptr: int, n: int, cap_words: int, out_ptr: int) -> int:
     used = ctypes.c_size_t()
     _check(lib().moe_entropy_pack(w_ptr, n, cap_words, out_ptr, ctypes.byref(used)), "moe_entropy_pack")
     return used.value
+
+
+def moe_q4_matrix_bytes(n: int, k: int) -> int:
+    return lib().moe_q4_matrix_bytes(n, k)
+
+
+def moe_q4_matmul(x: int, x_stride: int, w: int, y: int, y_stride: int, rows: int, n: int, k: int, dtype: int,
+                  stream: int) -> None:
+    _check(lib().moe_q4_matmul(x, x_stride, w, y, y_stride, rows, n, k, dtype, stream), "moe_q4_matmul")
+
+
+def moe_kv4_append(batch: moe_kv4_batch, q: int, q_stride: int, k: int, k_stride: int, v: int, v_stride: int,
+                   cos: int, sin: int, max_pos: int, rot_dim: int, q_out: int, q_out_stride: int, heads: int,
+                   dtype: int, stream: int) -> None:
+    _check(lib().moe_kv4_append(batch, q, q_stride, k, k_stride, v, v_stride, cos, sin, max_pos, rot_dim, q_out,
+                                q_out_stride, heads, dtype, stream), "moe_kv4_append")
+
+
+def moe_kv4_read(batch: moe_kv4_batch, k: int, v: int, dtype: int, stream: int) -> None:
+    _check(lib().moe_kv4_read(batch, k, v, dtype, stream), "moe_kv4_read")
+
+
+def moe_kv4_attention_workspace_bytes(batch: moe_kv4_batch, heads: int, max_new: int, max_len: int) -> int:
+    return lib().moe_kv4_attention_workspace_bytes(batch, heads, max_new, max_len)
+
+
+def moe_kv4_attention(batch: moe_kv4_batch, q: int, q_stride: int, o: int, o_stride: int, heads: int, scale: float,
+                      dtype: int, max_new: int, max_len: int, workspace: int, workspace_bytes: int,
+                      stream: int) -> None:
+    _check(lib().moe_kv4_attention(batch, q, q_stride, o, o_stride, heads, scale, dtype, max_new, max_len, workspace,
+                                   workspace_bytes, stream), "moe_kv4_attention")
+
+
+def moe_norm_residual(h: int, h_stride: int, y: int, y_stride: int, gate: int, gate_stride: int, post: int, pre: int,
+                      residual_scale: float, eps: float, h_out: int, h_out_stride: int, x_out: int, x_stride: int,
+                      rows: int, d: int, dtype: int, stream: int) -> None:
+    _check(lib().moe_norm_residual(h, h_stride, y, y_stride, gate, gate_stride, post, pre, residual_scale, eps, h_out,
+                                   h_out_stride, x_out, x_stride, rows, d, dtype, stream), "moe_norm_residual")

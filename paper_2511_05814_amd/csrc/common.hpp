@@ -269,6 +269,69 @@ hipError_t launch_prefill_skinny_down(const GemmTile *tiles, int ntiles, int max
 hipError_t launch_prefill_unpermute(float *H, const float *Y, const float *g, const int32_t *pos_of, int T,
                                     int d, int K, const Launch &l);
 
+// Sets the calling thread's error message; returns `code`.
+int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+
+// ---- the attention half of a layer ---------------------------------------
+// Cache entries in 4 bits (moe_kv4_batch in moe_offload.h): positions of a
+// page's record.  P tokens a page, D dimensions a head.
+constexpr int kKvGroup = 32;  // dimensions that share a scale and a zero
+struct Kv4 {
+  uint8_t *pool;               // [pages][kv heads][record]
+  const int32_t *page_table;   // [seqs][table_cols]
+  const int32_t *q_start;      // [seqs + 1]
+  const int32_t *kv_len;       // [seqs]
+  int64_t table_stride;        // entries between rows of the table
+  int pages, page_log2, kv_heads, table_cols, seqs, tokens;
+};
+struct KvAppendArgs {
+  Kv4 kv;
+  const void *q, *k, *v;
+  void *q_out;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;  // elements between tokens
+  const float *cos, *sin;      // [max_pos][rot / 2]
+  int max_pos, rot, heads;
+};
+struct KvReadArgs {
+  Kv4 kv;
+  void *k, *v;                 // [tokens][kv heads][D]
+};
+struct KvAttnArgs {
+  Kv4 kv;
+  const void *q;
+  void *o;
+  int64_t q_stride, o_stride;
+  float *part;                 // [splits][tokens * heads][D]
+  float *ml;                   // [splits][tokens * heads][2]
+  float scale;
+  int heads, splits, row_blocks;
+};
+hipError_t launch_kv4_append(const KvAppendArgs &a, int head_dim, bool f32, hipStream_t s);
+hipError_t launch_kv4_read(const KvReadArgs &a, int head_dim, bool f32, hipStream_t s);
+// Splits of the keys that a launch of kv4_attention takes, and workgroups along its rows.
+void kv4_attention_shape(int seqs, int kv_heads, int heads, int max_new, int max_len, int *splits, int *row_blocks);
+hipError_t launch_kv4_attention(const KvAttnArgs &a, int head_dim, bool f32, hipStream_t s);
+
+struct Q4Args {
+  const void *x;
+  void *y;
+  const uint8_t *codes, *scales, *zeros;
+  int64_t x_stride, y_stride;
+  int rows, n, k;
+};
+hipError_t launch_q4_matmul(const Q4Args &a, bool f32, hipStream_t s);
+
+struct NormArgs {
+  const float *h, *gate, *post, *pre;
+  const void *y;
+  float *h_out;
+  void *x_out;
+  int64_t h_stride, y_stride, gate_stride, h_out_stride, x_stride;
+  float residual_scale, eps;
+  int rows, d;
+};
+hipError_t launch_norm_residual(const NormArgs &a, bool f32, hipStream_t s);
+
 // ---------------------------------------------------------------------------
 // device helpers
 
@@ -384,6 +447,29 @@ __device__ inline void wave_topk_lds(const double *const (&z)[N], int E, int K, 
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
   for (int q = 0; q < N; ++q) id[q] = lane < K ? out[q][lane] : -1;
+}
+
+// Eight consecutive elements of an fp32 or bf16 array as fp32, and back.
+__device__ __forceinline__ void load8(const float *p, float *f) {
+  const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+}
+__device__ __forceinline__ void load8(const uint16_t *p, float *f) {
+  bf16x8_to_f32(*reinterpret_cast<const uint4 *>(p), f);
+}
+// Two fp32 rounded to bf16 (nearest, ties to even, NaN kept), the first in the low half.
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 v = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ void store8(float *p, const float *f) {
+  *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+  *reinterpret_cast<float4 *>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+}
+__device__ __forceinline__ void store8(uint16_t *p, const float *f) {
+  *reinterpret_cast<uint4 *>(p) =
+      make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
 }
 
 }  // namespace moe

@@ -32,10 +32,10 @@
 using namespace moe;
 
 namespace {
-
 thread_local std::string g_err;
+}
 
-int fail(int code, const char *fmt, ...) {
+int moe::fail(int code, const char *fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -44,6 +44,8 @@ int fail(int code, const char *fmt, ...) {
   g_err = buf;
   return code;
 }
+
+namespace {
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

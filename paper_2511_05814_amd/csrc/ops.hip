@@ -1,0 +1,241 @@
+// C entries of the attention half of a layer: argument checks and launches.
+#include "common.hpp"
+#include "moe_offload.h"
+
+using namespace moe;
+
+namespace {
+
+bool misaligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) != 0; }
+
+// a * b * c for non-negative factors, or -1 past 2^62
+int64_t product(int64_t a, int64_t b, int64_t c = 1) {
+  int64_t v;
+  if (__builtin_mul_overflow(a, b, &v) || __builtin_mul_overflow(v, c, &v) || v >= (int64_t)1 << 62) return -1;
+  return v;
+}
+
+int check_dtype(int dtype) {
+  if (dtype != MOE_DTYPE_F32 && dtype != MOE_DTYPE_BF16) return fail(MOE_ERR_ARG, "dtype must be MOE_DTYPE_F32 or MOE_DTYPE_BF16");
+  return MOE_OK;
+}
+
+// A row-strided operand: non-NULL, rows of `width` elements of `bytes` bytes, aligned to `align`.
+int check_rows(const char *name, const void *p, int64_t stride, int64_t width, int bytes, int align) {
+  if (!p || misaligned(p, align)) return fail(MOE_ERR_ARG, "%s must be a non-NULL device pointer aligned to %d bytes", name, align);
+  if (stride < width || stride > (int64_t)1 << 40) return fail(MOE_ERR_ARG, "%s: a stride of %lld for rows of %lld", name, (long long)stride, (long long)width);
+  if (stride * bytes % align) return fail(MOE_ERR_ARG, "%s: its stride must be a multiple of %d bytes", name, align);
+  return MOE_OK;
+}
+
+int element(int dtype) { return dtype == MOE_DTYPE_F32 ? 4 : 2; }
+
+int launched(hipError_t e, const char *what) {
+  return e == hipSuccess ? MOE_OK : fail(MOE_ERR_HIP, "%s failed: %s", what, hipGetErrorString(e));
+}
+
+int check_batch(const moe_kv4_batch *b) {
+  if (!b) return fail(MOE_ERR_ARG, "NULL batch");
+  if (b->head_dim != 64 && b->head_dim != 128) return fail(MOE_ERR_ARG, "head_dim must be 64 or 128, not %d", b->head_dim);
+  if (b->page_size < 16 || b->page_size > 1024 || (b->page_size & (b->page_size - 1)))
+    return fail(MOE_ERR_ARG, "page_size must be a power of two in [16, 1024], not %d", b->page_size);
+  if (b->kv_heads < 1 || b->kv_heads > 1024) return fail(MOE_ERR_ARG, "kv_heads must be in [1, 1024]");
+  if (b->pages < 1) return fail(MOE_ERR_ARG, "pages must be >= 1");
+  if (b->table_cols < 1 || product(b->table_cols, b->page_size) > (int64_t)1 << 30)
+    return fail(MOE_ERR_ARG, "table_cols must be in [1, 2^30 / page_size]");
+  if (b->table_stride < b->table_cols) return fail(MOE_ERR_ARG, "table_stride < table_cols");
+  if (b->seqs < 1 || b->seqs > 1 << 20) return fail(MOE_ERR_ARG, "seqs must be in [1, 2^20]");
+  if (b->tokens < 0 || b->tokens > 1 << 24) return fail(MOE_ERR_ARG, "tokens must be in [0, 2^24]");
+  if (!b->pool || misaligned(b->pool, 16)) return fail(MOE_ERR_ARG, "pool must be a non-NULL 16-byte aligned device pointer");
+  if (!b->page_table || !b->q_start || !b->kv_len || misaligned(b->page_table, 4) || misaligned(b->q_start, 4) || misaligned(b->kv_len, 4))
+    return fail(MOE_ERR_ARG, "page_table, q_start and kv_len must be non-NULL device arrays of int32");
+  return MOE_OK;
+}
+
+int check_heads(const moe_kv4_batch *b, int heads) {
+  if (heads < 1 || heads > 4096 || heads % b->kv_heads)
+    return fail(MOE_ERR_ARG, "heads (%d) must be a multiple of kv_heads (%d), at most 4096", heads, b->kv_heads);
+  return MOE_OK;
+}
+
+Kv4 kv_of(const moe_kv4_batch *b) {
+  Kv4 k;
+  k.pool = static_cast<uint8_t *>(b->pool);
+  k.page_table = b->page_table;
+  k.q_start = b->q_start;
+  k.kv_len = b->kv_len;
+  k.table_stride = b->table_stride;
+  k.pages = b->pages;
+  k.page_log2 = __builtin_ctz((unsigned)b->page_size);
+  k.kv_heads = b->kv_heads;
+  k.table_cols = b->table_cols;
+  k.seqs = b->seqs;
+  k.tokens = b->tokens;
+  return k;
+}
+
+#define CHECK(expr)                    \
+  do {                                 \
+    const int rc_ = (expr);            \
+    if (rc_ != MOE_OK) return rc_;     \
+  } while (0)
+
+}  // namespace
+
+extern "C" {
+
+size_t moe_q4_matrix_bytes(size_t n, size_t k) {
+  if (n < 1 || k < 64 || k % 64 || n > ((size_t)1 << 40) / k) return 0;
+  return n * (k / 2) + n * (k / 64) * 3;
+}
+
+int moe_q4_matmul(const void *x, int64_t x_stride, const void *w, void *y, int64_t y_stride, int rows, int n, int k,
+                  int dtype, void *stream) {
+  CHECK(check_dtype(dtype));
+  if (rows < 0 || rows > 1 << 20) return fail(MOE_ERR_ARG, "rows must be in [0, 2^20]");
+  if (n < 1 || n > 1 << 24) return fail(MOE_ERR_ARG, "n must be in [1, 2^24]");
+  if (k < 64 || k % 64 || k > 1 << 20) return fail(MOE_ERR_ARG, "k must be a multiple of 64 in [64, 2^20]");
+  if (!w || misaligned(w, 16)) return fail(MOE_ERR_ARG, "w must be a non-NULL 16-byte aligned device pointer");
+  CHECK(check_rows("x", x, x_stride, k, element(dtype), 16));
+  CHECK(check_rows("y", y, y_stride, n, element(dtype), element(dtype)));
+  if (rows == 0) return MOE_OK;
+  Q4Args a;
+  a.x = x;
+  a.y = y;
+  a.codes = static_cast<const uint8_t *>(w);
+  a.scales = a.codes + (size_t)n * (k / 2);
+  a.zeros = a.scales + (size_t)n * (k / 64) * 2;
+  a.x_stride = x_stride;
+  a.y_stride = y_stride;
+  a.rows = rows;
+  a.n = n;
+  a.k = k;
+  return launched(launch_q4_matmul(a, dtype == MOE_DTYPE_F32, static_cast<hipStream_t>(stream)), "4-bit product");
+}
+
+int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                   const void *v, int64_t v_stride, const float *cos, const float *sin, int max_pos, int rot_dim,
+                   void *q_out, int64_t q_out_stride, int heads, int dtype, void *stream) {
+  CHECK(check_batch(b));
+  CHECK(check_dtype(dtype));
+  CHECK(check_heads(b, heads));
+  const int bytes = element(dtype), d = b->head_dim;
+  CHECK(check_rows("q", q, q_stride, (int64_t)heads * d, bytes, 16));
+  CHECK(check_rows("k", k, k_stride, (int64_t)b->kv_heads * d, bytes, 16));
+  CHECK(check_rows("v", v, v_stride, (int64_t)b->kv_heads * d, bytes, 16));
+  CHECK(check_rows("q_out", q_out, q_out_stride, (int64_t)heads * d, bytes, 16));
+  if (rot_dim < 0 || rot_dim > d || rot_dim % 16) return fail(MOE_ERR_ARG, "rot_dim must be a multiple of 16 in [0, head_dim], not %d", rot_dim);
+  if (max_pos < 1) return fail(MOE_ERR_ARG, "max_pos must be >= 1");
+  if (rot_dim && (!cos || !sin || misaligned(cos, 16) || misaligned(sin, 16)))
+    return fail(MOE_ERR_ARG, "cos and sin must be non-NULL 16-byte aligned device pointers");
+  if (rot_dim && q_out == q) return fail(MOE_ERR_ARG, "q_out may be q only without rotation");
+  if (product(b->tokens, heads + 2 * b->kv_heads, d / 8) >= (int64_t)256 << 31) return fail(MOE_ERR_ARG, "too many tokens times heads");
+  if (b->tokens == 0) return MOE_OK;
+  KvAppendArgs a;
+  a.kv = kv_of(b);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out_stride = q_out_stride;
+  a.cos = cos;
+  a.sin = sin;
+  a.max_pos = max_pos;
+  a.rot = rot_dim;
+  a.heads = heads;
+  return launched(launch_kv4_append(a, d, dtype == MOE_DTYPE_F32, static_cast<hipStream_t>(stream)), "cache append");
+}
+
+int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stream) {
+  CHECK(check_batch(b));
+  CHECK(check_dtype(dtype));
+  if (!k || !v || misaligned(k, 16) || misaligned(v, 16)) return fail(MOE_ERR_ARG, "k and v must be non-NULL 16-byte aligned device pointers");
+  if (product(b->tokens, 2 * b->kv_heads, b->head_dim / 8) >= (int64_t)256 << 31) return fail(MOE_ERR_ARG, "too many tokens times heads");
+  if (b->tokens == 0) return MOE_OK;
+  KvReadArgs a;
+  a.kv = kv_of(b);
+  a.k = k;
+  a.v = v;
+  return launched(launch_kv4_read(a, b->head_dim, dtype == MOE_DTYPE_F32, static_cast<hipStream_t>(stream)), "cache read");
+}
+
+size_t moe_kv4_attention_workspace_bytes(const moe_kv4_batch *b, int heads, int max_new, int max_len) {
+  if (check_batch(b) != MOE_OK || check_heads(b, heads) != MOE_OK || max_new < 1 || max_len < 1) return 0;
+  int splits = 1, row_blocks = 1;
+  kv4_attention_shape(b->seqs, b->kv_heads, heads, max_new, max_len, &splits, &row_blocks);
+  return splits == 1 ? 0 : (size_t)splits * b->tokens * heads * (b->head_dim + 2) * sizeof(float);
+}
+
+int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, void *o, int64_t o_stride, int heads,
+                      float scale, int dtype, int max_new, int max_len, void *workspace, size_t workspace_bytes,
+                      void *stream) {
+  CHECK(check_batch(b));
+  CHECK(check_dtype(dtype));
+  CHECK(check_heads(b, heads));
+  const int bytes = element(dtype), d = b->head_dim;
+  CHECK(check_rows("q", q, q_stride, (int64_t)heads * d, bytes, 16));
+  CHECK(check_rows("o", o, o_stride, (int64_t)heads * d, bytes, 16));
+  if (max_new < 1 || max_len < 1) return fail(MOE_ERR_ARG, "max_new and max_len must be >= 1");
+  if (product(b->seqs, b->kv_heads) >= (int64_t)1 << 31 || product(b->tokens, heads, d / 4) >= (int64_t)256 << 31)
+    return fail(MOE_ERR_ARG, "too many sequences or tokens times heads");
+  KvAttnArgs a;
+  a.kv = kv_of(b);
+  a.q = q;
+  a.o = o;
+  a.q_stride = q_stride;
+  a.o_stride = o_stride;
+  a.scale = scale;
+  a.heads = heads;
+  kv4_attention_shape(b->seqs, b->kv_heads, heads, max_new, max_len, &a.splits, &a.row_blocks);
+  const size_t rows = (size_t)b->tokens * heads, need = a.splits == 1 ? 0 : (size_t)a.splits * rows * (d + 2) * sizeof(float);
+  if (workspace_bytes < need || (need && (!workspace || misaligned(workspace, 16))))
+    return fail(MOE_ERR_ARG, "workspace must be 16-byte aligned and hold %zu bytes (got %zu)", need, workspace_bytes);
+  if (b->tokens == 0) return MOE_OK;
+  a.part = static_cast<float *>(workspace);
+  a.ml = a.part ? a.part + (size_t)a.splits * rows * d : nullptr;
+  return launched(launch_kv4_attention(a, d, dtype == MOE_DTYPE_F32, static_cast<hipStream_t>(stream)), "cache attention");
+}
+
+int moe_norm_residual(const float *h, int64_t h_stride, const void *y, int64_t y_stride, const float *gate,
+                      int64_t gate_stride, const float *post, const float *pre, float residual_scale, float eps,
+                      float *h_out, int64_t h_out_stride, void *x_out, int64_t x_stride, int rows, int d, int dtype,
+                      void *stream) {
+  CHECK(check_dtype(dtype));
+  if (rows < 0 || rows > 1 << 24) return fail(MOE_ERR_ARG, "rows must be in [0, 2^24]");
+  if (d < 8 || d % 8 || d > 16384) return fail(MOE_ERR_ARG, "d must be a multiple of 8 in [8, 16384]");
+  const int bytes = element(dtype);
+  CHECK(check_rows("h", h, h_stride, d, 4, 16));
+  if (y) CHECK(check_rows("y", y, y_stride, d, bytes, 16));
+  if (!y && (gate || post)) return fail(MOE_ERR_ARG, "gate and post need y");
+  if (gate && gate_stride) CHECK(check_rows("gate", gate, gate_stride, d, 4, 16));
+  if (misaligned(gate, 16) || misaligned(post, 16) || misaligned(pre, 16)) return fail(MOE_ERR_ARG, "gate, post and pre must be 16-byte aligned");
+  if (!h_out && !x_out) return fail(MOE_ERR_ARG, "neither h_out nor x_out is wanted");
+  if (h_out) CHECK(check_rows("h_out", h_out, h_out_stride, d, 4, 16));
+  if (x_out) CHECK(check_rows("x_out", x_out, x_stride, d, bytes, 16));
+  if (h_out == h && h_out_stride != h_stride) return fail(MOE_ERR_ARG, "h_out on h needs the same stride");
+  if (x_out && x_out == y && x_stride != y_stride) return fail(MOE_ERR_ARG, "x_out on y needs the same stride");
+  if (rows == 0) return MOE_OK;
+  NormArgs a;
+  a.h = h;
+  a.gate = gate;
+  a.post = post;
+  a.pre = pre;
+  a.y = y;
+  a.h_out = h_out;
+  a.x_out = x_out;
+  a.h_stride = h_stride;
+  a.y_stride = y_stride;
+  a.gate_stride = gate_stride;
+  a.h_out_stride = h_out_stride;
+  a.x_stride = x_stride;
+  a.residual_scale = residual_scale;
+  a.eps = eps;
+  a.rows = rows;
+  a.d = d;
+  return launched(launch_norm_residual(a, dtype == MOE_DTYPE_F32, static_cast<hipStream_t>(stream)), "norm");
+}
+
+}  // extern "C"
