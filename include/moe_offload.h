@@ -420,7 +420,8 @@ size_t moe_q4_matrix_bytes(size_t n, size_t k);
 
 /* y[t][i] = sum_c x[t][c] W[i][c] for rows 0 <= t < rows (at most 2^20), W a
  * 4-bit matrix [n x k] at w.  y's pointer and stride need only be aligned to
- * their type.  A row of x with an infinity or a NaN gives a row of NaN. */
+ * their type.  A row of x with an infinity or a NaN gives a row of NaN, and
+ * a sum past fp32's range is a NaN. */
 int moe_q4_matmul(const void *x, int64_t x_stride, const void *w, void *y, int64_t y_stride, int rows, int n, int k,
                   int dtype, void *stream);
 

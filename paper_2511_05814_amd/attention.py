@@ -21,6 +21,7 @@ from __future__ import annotations
 from typing import Optional
 
 import torch
+from torch._C import _cuda_getCurrentRawStream
 
 from . import binding as b
 
@@ -29,56 +30,66 @@ KV_GROUP = 32       # dimensions of a cache entry that share one
 _DTYPES = {torch.float32: b.MOE_DTYPE_F32, torch.bfloat16: b.MOE_DTYPE_BF16}
 
 
-def _dtype(t) -> int:
-    try:
-        return _DTYPES[t]
-    except KeyError:
-        raise ValueError(f"tensors must be float32 or bfloat16, not {t}") from None
+# The checks below are written out for speed: a call's launch takes some 3 us,
+# and decode calls are this short.
+
+def _place(t: torch.Tensor, dtype):
+    """(device, stream, MOE_DTYPE_* of dtype) of a call on t: its device, which
+    must be the current one, and torch's current stream there."""
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
+        raise ValueError(f"tensors must be on the current GPU, not on {t.device}")
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise ValueError(f"tensors must be float32 or bfloat16, not {dtype}")
+    return device, _cuda_getCurrentRawStream(device), code
 
 
-def _stream(t: torch.Tensor) -> int:
-    """The current stream of t's device, which must be the current device."""
-    if not t.is_cuda:
-        raise ValueError("tensors must be on the GPU")
-    s = torch.cuda.current_stream()
-    if t.get_device() != s.device_index:
-        raise ValueError(f"tensors are on device {t.get_device()}, the current device is {s.device_index}")
-    return s.cuda_stream
-
-
-def _same(device: int, name: str, t: torch.Tensor, dtype, shape) -> torch.Tensor:
+def _rows(name: str, t: torch.Tensor, device: int, dtype, shape) -> int:
+    """Elements between the rows of t, which must be of this device, type and
+    shape (2 or 3 dimensions), each row contiguous."""
     if t.dtype != dtype or t.get_device() != device or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {tuple(shape)} on device {device}, "
                          f"not {t.dtype} {tuple(t.shape)} on device {t.get_device()}")
-    return t
-
-
-def _rows(name: str, t: torch.Tensor) -> int:
-    """Elements between the rows of t [rows][...], each row contiguous."""
-    inner = 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if size != 1 and stride != inner:
+    stride, inner = t.stride(), 1
+    if len(shape) == 3:
+        inner = shape[2]
+        if stride[2] != 1 and inner > 1 or stride[1] != inner and shape[1] > 1:
             raise ValueError(f"{name}: rows must be contiguous")
-        inner *= size
-    return t.stride(0) if t.shape[0] > 1 else inner
+        inner *= shape[1]
+    else:
+        inner = shape[1]
+        if stride[1] != 1 and inner > 1:
+            raise ValueError(f"{name}: rows must be contiguous")
+    return stride[0] if shape[0] > 1 else inner
+
+
+def _vector(name: str, t: Optional[torch.Tensor], device: int, dtype, n: int) -> Optional[int]:
+    """Address of a contiguous vector of n elements, None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.get_device() != device or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} [{n}] on device {device}, "
+                         f"not {t.dtype} {tuple(t.shape)} on device {t.get_device()}")
+    return t.data_ptr()
 
 
 def q4_matmul(x: torch.Tensor, w: torch.Tensor, n: int, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x [rows, k] times the 4-bit matrix [n x k] in the bytes w, transposed: [rows, n]."""
     if x.dim() != 2:
         raise ValueError("x must be [rows, k]")
-    rows, k = x.shape
-    dtype, stream, device = _dtype(x.dtype), _stream(x), x.get_device()
+    shape = x.shape
+    rows, k = shape
+    device, stream, code = _place(x, x.dtype)
     if k % GROUP or k == 0 or n < 1:
         raise ValueError(f"a 4-bit matrix [{n} x {k}]: columns must be a multiple of {GROUP}")
-    _same(device, "w", w, torch.uint8, (n * k // 2 + n * (k // GROUP) * 3,))
-    if not w.is_contiguous():
-        raise ValueError("w must be contiguous")
+    weights = _vector("w", w, device, torch.uint8, n * k // 2 + n * (k // GROUP) * 3)
     if out is None:
-        out = torch.empty((rows, n), dtype=x.dtype, device=x.device)
+        out, out_stride = x.new_empty((rows, n)), n
     else:
-        _same(device, "out", out, x.dtype, (rows, n))
-    b.moe_q4_matmul(x.data_ptr(), _rows("x", x), w.data_ptr(), out.data_ptr(), _rows("out", out), rows, n, k, dtype, stream)
+        out_stride = _rows("out", out, device, x.dtype, (rows, n))
+    b.moe_q4_matmul(x.data_ptr(), _rows("x", x, device, x.dtype, shape), weights, out.data_ptr(), out_stride, rows, n, k,
+                    code, stream)
     return out
 
 
@@ -99,15 +110,13 @@ def _batch(device, pool, page_table, q_start, kv_len, tokens, head_dim) -> b.moe
     page_size = record * 8 // (9 * head_dim)
     if page_size * head_dim * 9 != record * 8:
         raise ValueError(f"records of {record} bytes are not whole tokens of {head_dim} dimensions")
-    seqs = kv_len.shape[0]
-    for name, t, dims in (("page_table", page_table, 2), ("q_start", q_start, 1), ("kv_len", kv_len, 1)):
-        if t.dtype != torch.int32 or t.dim() != dims or t.get_device() != device or t.stride(-1) != 1:
-            raise ValueError(f"{name} must be int32 of {dims} dimension(s), contiguous in the last, on the call's device")
-    if page_table.shape[0] != seqs or q_start.shape[0] != seqs + 1:
-        raise ValueError(f"{seqs} sequences: page_table {tuple(page_table.shape)}, q_start {tuple(q_start.shape)}")
-    cols = page_table.shape[1]
-    return b.moe_kv4_batch(pool.data_ptr(), page_table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(),
-                           page_table.stride(0) if seqs > 1 else cols, pages, page_size, kv_heads, head_dim, cols, seqs, tokens)
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [sequences, columns]")
+    seqs, cols = page_table.shape
+    stride = _rows("page_table", page_table, device, torch.int32, (seqs, cols))
+    return b.moe_kv4_batch(pool.data_ptr(), page_table.data_ptr(), _vector("q_start", q_start, device, torch.int32, seqs + 1),
+                           _vector("kv_len", kv_len, device, torch.int32, seqs), stride, pages, page_size, kv_heads, head_dim,
+                           cols, seqs, tokens)
 
 
 def kv4_append(q, k, v, cos, sin, pool, page_table, q_start, kv_len, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -115,25 +124,24 @@ def kv4_append(q, k, v, cos, sin, pool, page_table, q_start, kv_len, out: Option
     positions, store k and v [tokens, kv_heads, head_dim] in the cache and
     return the rotated q.  cos and sin: fp32 [positions, rot_dim / 2]; with
     rot_dim 0 nothing is rotated.  Rows may be slices of a joined projection."""
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("q, k and v must be [tokens, heads, head_dim]")
-    tokens, heads, head_dim = q.shape
-    dtype, stream, device = _dtype(q.dtype), _stream(q), q.get_device()
+    if q.dim() != 3 or cos.dim() != 2:
+        raise ValueError("q must be [tokens, heads, head_dim], cos and sin [positions, rot_dim / 2]")
+    dtype, shape = q.dtype, q.shape
+    tokens, heads, head_dim = shape
+    device, stream, code = _place(q, dtype)
     batch = _batch(device, pool, page_table, q_start, kv_len, tokens, head_dim)
-    shape = (tokens, batch.kv_heads, head_dim)
-    _same(device, "k", k, q.dtype, shape)
-    _same(device, "v", v, q.dtype, shape)
-    if cos.dim() != 2 or not cos.is_contiguous() or not sin.is_contiguous():
-        raise ValueError("cos and sin must be contiguous [positions, rot_dim / 2]")
-    _same(device, "cos", cos, torch.float32, cos.shape)
-    _same(device, "sin", sin, torch.float32, cos.shape)
+    kv_shape = (tokens, batch.kv_heads, head_dim)
+    positions, half = cos.shape
+    if _rows("cos", cos, device, torch.float32, (positions, half)) != half or \
+            _rows("sin", sin, device, torch.float32, (positions, half)) != half:
+        raise ValueError("cos and sin must be contiguous")
     if out is None:
-        out = torch.empty((tokens, heads, head_dim), dtype=q.dtype, device=q.device)
+        out, out_stride = q.new_empty(shape), heads * head_dim
     else:
-        _same(device, "out", out, q.dtype, q.shape)
-    b.moe_kv4_append(batch, q.data_ptr(), _rows("q", q), k.data_ptr(), _rows("k", k), v.data_ptr(), _rows("v", v),
-                     cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], out.data_ptr(), _rows("out", out),
-                     heads, dtype, stream)
+        out_stride = _rows("out", out, device, dtype, shape)
+    b.moe_kv4_append(batch, q.data_ptr(), _rows("q", q, device, dtype, shape), k.data_ptr(),
+                     _rows("k", k, device, dtype, kv_shape), v.data_ptr(), _rows("v", v, device, dtype, kv_shape),
+                     cos.data_ptr(), sin.data_ptr(), positions, 2 * half, out.data_ptr(), out_stride, heads, code, stream)
     return out
 
 
@@ -141,10 +149,9 @@ def kv4_read(pool, page_table, q_start, kv_len, tokens: int, head_dim: int, dtyp
     """The stored keys and values of the batch's new tokens, [tokens, kv_heads,
     head_dim] each (exact in both types).  With q_start the running sums of
     kv_len that is everything the sequences have."""
-    code, stream, device = _dtype(dtype), _stream(pool), pool.get_device()
+    device, stream, code = _place(pool, dtype)
     batch = _batch(device, pool, page_table, q_start, kv_len, tokens, head_dim)
-    k = torch.empty((tokens, batch.kv_heads, head_dim), dtype=dtype, device=pool.device)
-    v = torch.empty_like(k)
+    k, v = (pool.new_empty((tokens, batch.kv_heads, head_dim), dtype=dtype) for _ in range(2))
     b.moe_kv4_read(batch, k.data_ptr(), v.data_ptr(), code, stream)
     return k, v
 
@@ -159,25 +166,27 @@ def kv4_attention(q, pool, page_table, q_start, kv_len, scale: float, max_new: O
     is allocated unless one is given."""
     if q.dim() != 3:
         raise ValueError("q must be [tokens, heads, head_dim]")
-    tokens, heads, head_dim = q.shape
-    dtype, stream, device = _dtype(q.dtype), _stream(q), q.get_device()
+    dtype, shape = q.dtype, q.shape
+    tokens, heads, head_dim = shape
+    device, stream, code = _place(q, dtype)
     batch = _batch(device, pool, page_table, q_start, kv_len, tokens, head_dim)
     if max_new is None:
         max_new = max(1, -(-tokens // max(1, batch.seqs)))
     if max_len is None:
         max_len = max(1, batch.table_cols * batch.page_size)
     if out is None:
-        out = torch.empty((tokens, heads, head_dim), dtype=q.dtype, device=q.device)
+        out, out_stride = q.new_empty(shape), heads * head_dim
     else:
-        _same(device, "out", out, q.dtype, q.shape)
+        out_stride = _rows("out", out, device, dtype, shape)
     if workspace is None:
         need = b.moe_kv4_attention_workspace_bytes(batch, heads, max_new, max_len)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    elif workspace.get_device() != device or not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous on the call's device")
-    b.moe_kv4_attention(batch, q.data_ptr(), _rows("q", q), out.data_ptr(), _rows("out", out), heads, scale, dtype,
-                        max_new, max_len, workspace.data_ptr() if workspace is not None else None,
-                        workspace.numel() * workspace.element_size() if workspace is not None else 0, stream)
+        if need:
+            workspace = q.new_empty((need,), dtype=torch.uint8)
+    else:
+        need = workspace.numel()
+        _vector("workspace", workspace, device, torch.uint8, need)
+    b.moe_kv4_attention(batch, q.data_ptr(), _rows("q", q, device, dtype, shape), out.data_ptr(), out_stride, heads, scale,
+                        code, max_new, max_len, workspace.data_ptr() if need else None, need, stream)
     return out
 
 
@@ -187,37 +196,35 @@ def norm_residual(h, y=None, gate=None, post=None, pre=None, residual_scale: flo
     block's input x = h' pre / rms(h') in y's type (`dtype` without y).  h fp32
     [rows, d], y [rows, d], gate [d] or [rows, d], post and pre [d], fp32; without
     y there is no block's result to add, without post y is taken as it is.
-    h_out=h updates the residual stream in place."""
+    h_out=h updates the residual stream in place; want_h or want_x False: None
+    in the place of h' or x."""
     if h.dim() != 2:
         raise ValueError("h must be [rows, d]")
-    rows, d = h.shape
-    stream, device = _stream(h), h.get_device()
-    _same(device, "h", h, torch.float32, h.shape)
+    shape = h.shape
+    rows, d = shape
     if y is not None:
-        if dtype not in (None, y.dtype):
+        if dtype is not None and dtype != y.dtype:
             raise ValueError(f"y is {y.dtype}, not {dtype}")
         dtype = y.dtype
-        _same(device, "y", y, dtype, h.shape)
-    dtype = dtype or torch.float32
-    code = _dtype(dtype)
-    for name, t in (("post", post), ("pre", pre)):
-        if t is not None and not _same(device, name, t, torch.float32, (d,)).is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-    gate_stride = 0
+    elif dtype is None:
+        dtype = torch.float32
+    device, stream, code = _place(h, dtype)
+    h_stride = _rows("h", h, device, torch.float32, shape)
+    y_ptr, y_stride = (y.data_ptr(), _rows("y", y, device, dtype, shape)) if y is not None else (None, d)
+    gate_ptr, gate_stride = None, 0
     if gate is not None:
-        _same(device, "gate", gate, torch.float32, (d,) if gate.dim() == 1 else (rows, d))
-        if gate.stride(-1) != 1:
-            raise ValueError("gate: rows must be contiguous")
-        gate_stride = 0 if gate.dim() == 1 else _rows("gate", gate)
+        if gate.dim() == 1:
+            gate_ptr = _vector("gate", gate, device, torch.float32, d)
+        else:
+            gate_ptr, gate_stride = gate.data_ptr(), _rows("gate", gate, device, torch.float32, shape)
+    h_out_stride = d
     if h_out is not None:
-        _same(device, "h_out", h_out, torch.float32, h.shape)
+        h_out_stride = _rows("h_out", h_out, device, torch.float32, shape)
     elif want_h:
-        h_out = torch.empty((rows, d), dtype=torch.float32, device=h.device)
-    x = torch.empty((rows, d), dtype=dtype, device=h.device) if want_x else None
-    b.moe_norm_residual(h.data_ptr(), _rows("h", h), y.data_ptr() if y is not None else None,
-                        _rows("y", y) if y is not None else d, gate.data_ptr() if gate is not None else None, gate_stride,
-                        post.data_ptr() if post is not None else None, pre.data_ptr() if pre is not None else None,
-                        residual_scale, eps, h_out.data_ptr() if h_out is not None else None,
-                        _rows("h_out", h_out) if h_out is not None else d, x.data_ptr() if x is not None else None, d,
-                        rows, d, code, stream)
+        h_out = h.new_empty(shape)
+    x = h.new_empty(shape, dtype=dtype) if want_x else None
+    b.moe_norm_residual(h.data_ptr(), h_stride, y_ptr, y_stride, gate_ptr, gate_stride,
+                        _vector("post", post, device, torch.float32, d), _vector("pre", pre, device, torch.float32, d),
+                        residual_scale, eps, h_out.data_ptr() if h_out is not None else None, h_out_stride,
+                        x.data_ptr() if want_x else None, d, rows, d, code, stream)
     return h_out, x

@@ -10,6 +10,17 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+// Stores a result; one that is not finite, from an infinity in x or past
+// fp32's range, is NaN whichever kernel computed it.
+template <typename T>
+__device__ __forceinline__ void store_result(T *out, float v) {
+  v = fmaf(v, 0.0f, v);
+  if constexpr (sizeof(T) == 4) *out = v;
+  else *out = (uint16_t)bf16_pair(v, 0.0f);
+}
 
 // Few rows of x.  A workgroup owns 16 weight rows and 16 * MT rows of x; its
 // eight waves share out the groups of 64 columns and add their results through
@@ -99,11 +110,176 @@ __global__ __launch_bounds__(kSmallWaves * kWave) void q4_small_kernel(Q4Args a)
 #pragma unroll
     for (int w = 0; w < kSmallWaves; ++w) v += sums[w][m][r][o % 16];
     if (n < a.n && t < a.rows) {
-      T *out = static_cast<T *>(a.y) + t * a.y_stride + n;
-      if constexpr (sizeof(T) == 4) *out = v;
-      else *out = (uint16_t)bf16_pair(v, 0.0f);
+      store_result(static_cast<T *>(a.y) + t * a.y_stride + n, v);
     }
   }
+}
+
+// Many rows of x: tiles of BM rows by 128 weight rows, a group of 64 columns a
+// step.  Four waves, two by two, own BM / 2 rows by 64 each.  The step's
+// weights are expanded once a workgroup, to the integers 16 q - zero (at most
+// 8 bits and a sign: exact in bf16), and wait with the rows of x in LDS, 128
+// bytes a row, 16-byte chunk c of row r at c ^ (r / 2 % 8) so that a fragment
+// read touches every bank once.  The products of one group are summed by
+// themselves and added to the result with the group's scale / 16, one fp32
+// fused multiply-add an element and group.  The next step's bytes are on their
+// way to registers while a step is multiplied; two LDS buffers, one barrier a
+// step.
+constexpr int kTileN = 128;
+
+// Sixteen codes as bf16 16 q - zero, in column order.
+__device__ __forceinline__ void expand16(uint2 w, float zero, uint4 *out) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t v = h ? w.y : w.x, even = v << 4 & 0xF0F0F0F0u, odd = v & 0xF0F0F0F0u;
+    uint32_t r[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const float a = (float)(even >> (8 * b) & 255u) - zero, c = (float)(odd >> (8 * b) & 255u) - zero;
+      r[b] = __builtin_amdgcn_perm(__float_as_uint(c), __float_as_uint(a), 0x07060302u);  // both exact: the upper halves
+    }
+    out[h] = make_uint4(r[0], r[1], r[2], r[3]);
+  }
+}
+
+template <int BM, typename T>
+__global__ __launch_bounds__(256, 1) void q4_tile_kernel(Q4Args a, int m_blocks, int n_blocks) {
+  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+  constexpr int XB = BM * 128, BUF = PARTS * XB + kTileN * 128;  // bytes of a part of x, of a step
+  constexpr int MI = BM / 64;          // 32-row blocks of a wave
+  constexpr int NX = BM * 8 / 256;     // 16-byte chunks of bf16 that a thread stages
+  __shared__ __align__(16) uint8_t lds[2 * BUF];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  // Runs of tiles to each XCD (workgroup i is on XCD i % 8), row blocks
+  // fastest, so that an XCD's L2 sees few weights.
+  const int tiles = m_blocks * n_blocks, per = tiles / 8, extra = tiles % 8;
+  const int xcd = blockIdx.x % 8, tile = xcd * per + min(xcd, extra) + blockIdx.x / 8;
+  const int t0 = tile % m_blocks * BM, n0 = tile / m_blocks * kTileN;
+  const int groups = a.k / 64;
+
+  // what this thread stages: chunk tid % 8 of rows tid / 8 + 32 i of x, half a group of weight row tid / 2
+  const T *xp[NX];
+#pragma unroll
+  for (int i = 0; i < NX; ++i) xp[i] = static_cast<const T *>(a.x) + min(t0 + tid / 8 + 32 * i, a.rows - 1) * a.x_stride + tid % 8 * 8;
+  const int wrow = min(n0 + tid / 2, a.n - 1);
+  const uint8_t *wp = a.codes + (size_t)wrow * (a.k / 2) + tid % 2 * 16;
+  const uint8_t *zp = a.zeros + (size_t)wrow * groups;
+  const uint32_t x_at = tid / 8 * 128 + ((tid % 8 ^ (tid / 16 & 7)) << 4);  // rows 32 i further: + 4096 i
+  const int wm = wave / 2, wn = wave % 2, r32 = lane & 31, hi = lane >> 5;
+  const _Float16 *sp[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+    sp[j] = reinterpret_cast<const _Float16 *>(a.scales) + (size_t)min(n0 + wn * 64 + j * 32 + r32, a.n - 1) * groups;
+
+  u32x4 xr[NX][sizeof(T) / 2], wr;
+  float zr, sr[2];
+  auto fetch = [&](int g) {
+#pragma unroll
+    for (int i = 0; i < NX; ++i)
+#pragma unroll
+      for (int h = 0; h < (int)sizeof(T) / 2; ++h) xr[i][h] = reinterpret_cast<const u32x4 *>(xp[i] + g * 64)[h];
+    wr = *reinterpret_cast<const u32x4 *>(wp + (size_t)g * 32);
+    zr = (float)zp[g];
+  };
+  auto stage = [&](uint8_t *to) {
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+      if constexpr (PARTS == 1) {
+        *reinterpret_cast<u32x4 *>(to + x_at + i * 4096) = xr[i][0];
+      } else {
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(xr[i][e / 4][e % 4]);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+          uint4 v;
+          v.x = bf16_pair(f[0], f[1]), v.y = bf16_pair(f[2], f[3]), v.z = bf16_pair(f[4], f[5]), v.w = bf16_pair(f[6], f[7]);
+          *reinterpret_cast<uint4 *>(to + p * XB + x_at + i * 4096) = v;
+          if (p + 1 < PARTS) {
+            float b[8];
+            bf16x8_to_f32(v, b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] -= b[e];
+          }
+        }
+      }
+    }
+    uint4 v[4];
+    expand16(make_uint2(wr.x, wr.y), zr, v);
+    expand16(make_uint2(wr.z, wr.w), zr, v + 2);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<uint4 *>(to + PARTS * XB + tid / 2 * 128 + (((tid % 2 * 4 + c) ^ (tid / 4 & 7)) << 4)) = v[c];
+  };
+
+  floatx16 y[MI][2];
+#pragma unroll
+  for (int m = 0; m < MI; ++m)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[m][j][i] = 0.0f;
+
+  fetch(0);
+  sr[0] = (float)sp[0][0], sr[1] = (float)sp[1][0];
+  stage(lds);
+  __syncthreads();
+  const uint32_t sw = (r32 >> 1) & 7;
+  for (int g = 0; g < groups; ++g) {
+    const uint8_t *from = lds + (g & 1) * BUF;
+    const float s0 = sr[0] * 0.0625f, s1 = sr[1] * 0.0625f;
+    if (g + 1 < groups) {
+      fetch(g + 1);
+      sr[0] = (float)sp[0][g + 1], sr[1] = (float)sp[1][g + 1];
+    }
+    bf16x8 w[2][4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        w[j][c] = *reinterpret_cast<const bf16x8 *>(from + PARTS * XB + (wn * 64 + j * 32 + r32) * 128 + (((2 * c + hi) ^ sw) << 4));
+#pragma unroll
+    for (int m = 0; m < MI; ++m) {
+      floatx16 d[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) d[j][i] = 0.0f;
+#pragma unroll
+      for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const bf16x8 x = *reinterpret_cast<const bf16x8 *>(from + p * XB + (wm * (BM / 2) + m * 32 + r32) * 128 + (((2 * c + hi) ^ sw) << 4));
+#pragma unroll
+          for (int j = 0; j < 2; ++j) d[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, w[j][c], d[j], 0, 0, 0);
+        }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        y[m][0][i] = fmaf(s0, d[0][i], y[m][0][i]);
+        y[m][1][i] = fmaf(s1, d[1][i], y[m][1][i]);
+      }
+    }
+    if (g + 1 < groups) stage(lds + (~g & 1) * BUF);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int m = 0; m < MI; ++m)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int n = n0 + wn * 64 + j * 32 + r32;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int t = t0 + wm * (BM / 2) + m * 32 + 8 * (i / 4) + 4 * hi + i % 4;
+        if (n < a.n && t < a.rows) store_result(static_cast<T *>(a.y) + t * a.y_stride + n, y[m][j][i]);
+      }
+    }
+}
+
+template <int BM, typename T>
+hipError_t launch_tile(const Q4Args &a, hipStream_t s) {
+  const int mb = (a.rows + BM - 1) / BM, nb = (a.n + kTileN - 1) / kTileN;
+  hipLaunchKernelGGL((q4_tile_kernel<BM, T>), dim3((unsigned)mb * nb), dim3(256), 0, s, a, mb, nb);
+  return hipGetLastError();
 }
 
 template <int MT>
@@ -117,7 +293,9 @@ void launch_small(const Q4Args &a, bool f32, hipStream_t s) {
 
 hipError_t launch_q4_matmul(const Q4Args &a, bool f32, hipStream_t s) {
   if (a.rows <= 16) launch_small<1>(a, f32, s);
-  else launch_small<2>(a, f32, s);
+  else if (a.rows <= 32) launch_small<2>(a, f32, s);
+  else if (f32) return a.rows <= 64 ? launch_tile<64, float>(a, s) : launch_tile<128, float>(a, s);
+  else return a.rows <= 64 ? launch_tile<64, uint16_t>(a, s) : a.rows <= 128 ? launch_tile<128, uint16_t>(a, s) : launch_tile<256, uint16_t>(a, s);
   return hipGetLastError();
 }
 
