@@ -10,6 +10,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
@@ -143,12 +144,15 @@ __device__ __forceinline__ void expand16(uint2 w, float zero, uint4 *out) {
 }
 
 template <int BM, typename T>
-__global__ __launch_bounds__(256, 1) void q4_tile_kernel(Q4Args a, int m_blocks, int n_blocks) {
+__global__ __launch_bounds__(256, BM <= 128 && sizeof(T) == 2 ? 2 : 1) void q4_tile_kernel(Q4Args a, int m_blocks, int n_blocks) {
   constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
   constexpr int XB = BM * 128, BUF = PARTS * XB + kTileN * 128;  // bytes of a part of x, of a step
   constexpr int MI = BM / 64;          // 32-row blocks of a wave
   constexpr int NX = BM * 8 / 256;     // 16-byte chunks of bf16 that a thread stages
+  constexpr int SROW = 18, ZROW = 20;  // a weight row's 16 scales (of 18 halves) and zeros (of 20 bytes): rows on different banks
   __shared__ __align__(16) uint8_t lds[2 * BUF];
+  __shared__ __align__(16) _Float16 lds_s[2][kTileN * SROW];
+  __shared__ __align__(16) uint8_t lds_z[2][kTileN * ZROW];
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   // Runs of tiles to each XCD (workgroup i is on XCD i % 8), row blocks
   // fastest, so that an XCD's L2 sees few weights.
@@ -164,24 +168,50 @@ __global__ __launch_bounds__(256, 1) void q4_tile_kernel(Q4Args a, int m_blocks,
   const int wrow = min(n0 + tid / 2, a.n - 1);
   const uint8_t *wp = a.codes + (size_t)wrow * (a.k / 2) + tid % 2 * 16;
   const uint8_t *zp = a.zeros + (size_t)wrow * groups;
+  const uint16_t *sp = reinterpret_cast<const uint16_t *>(a.scales) + (size_t)wrow * groups;
   const uint32_t x_at = tid / 8 * 128 + ((tid % 8 ^ (tid / 16 & 7)) << 4);  // rows 32 i further: + 4096 i
   const int wm = wave / 2, wn = wave % 2, r32 = lane & 31, hi = lane >> 5;
-  const _Float16 *sp[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-    sp[j] = reinterpret_cast<const _Float16 *>(a.scales) + (size_t)min(n0 + wn * 64 + j * 32 + r32, a.n - 1) * groups;
 
-  u32x4 xr[NX][sizeof(T) / 2], wr;
-  float zr, sr[2];
-  auto fetch = [&](int g) {
+  u32x4 xr[NX][sizeof(T) / 2], wc[4], wn4[4], sr;
+  u32x2 zr;
+  auto fetch_x = [&](int g) {
 #pragma unroll
     for (int i = 0; i < NX; ++i)
 #pragma unroll
       for (int h = 0; h < (int)sizeof(T) / 2; ++h) xr[i][h] = reinterpret_cast<const u32x4 *>(xp[i] + g * 64)[h];
-    wr = *reinterpret_cast<const u32x4 *>(wp + (size_t)g * 32);
-    zr = (float)zp[g];
   };
-  auto stage = [&](uint8_t *to) {
+  // Codes of four groups at a time: they share a line.
+  auto fetch_w = [&](u32x4 *w, int g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const u32x4 *>(wp + (size_t)min(g + i, groups - 1) * 32);
+  };
+  // Scales and zeros of sixteen groups, eight a thread; one by one where rows are not multiples of eight groups.
+  auto fetch_meta = [&](int g) {
+    g += tid % 2 * 8;
+    if (groups % 8 == 0) {
+      g = min(g, groups - 8);
+      sr = *reinterpret_cast<const u32x4 *>(sp + g);
+      zr = *reinterpret_cast<const u32x2 *>(zp + g);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sr[i] = (uint32_t)sp[min(g + 2 * i, groups - 1)] | (uint32_t)sp[min(g + 2 * i + 1, groups - 1)] << 16;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        zr[i] = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) zr[i] |= (uint32_t)zp[min(g + 4 * i + b, groups - 1)] << (8 * b);
+      }
+    }
+  };
+  auto stage_meta = [&](int chunk) {
+    uint32_t *s = reinterpret_cast<uint32_t *>(&lds_s[chunk & 1][tid / 2 * SROW + tid % 2 * 8]);
+    uint32_t *z = reinterpret_cast<uint32_t *>(&lds_z[chunk & 1][tid / 2 * ZROW + tid % 2 * 8]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = sr[i];
+    z[0] = zr[0], z[1] = zr[1];
+  };
+  auto stage = [&](int g, u32x4 codes) {
+    uint8_t *to = lds + (g & 1) * BUF;
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
       if constexpr (PARTS == 1) {
@@ -204,9 +234,10 @@ __global__ __launch_bounds__(256, 1) void q4_tile_kernel(Q4Args a, int m_blocks,
         }
       }
     }
+    const float zero = (float)lds_z[g / 16 & 1][tid / 2 * ZROW + g % 16];
     uint4 v[4];
-    expand16(make_uint2(wr.x, wr.y), zr, v);
-    expand16(make_uint2(wr.z, wr.w), zr, v + 2);
+    expand16(make_uint2(codes[0], codes[1]), zero, v);
+    expand16(make_uint2(codes[2], codes[3]), zero, v + 2);
 #pragma unroll
     for (int c = 0; c < 4; ++c)
       *reinterpret_cast<uint4 *>(to + PARTS * XB + tid / 2 * 128 + (((tid % 2 * 4 + c) ^ (tid / 4 & 7)) << 4)) = v[c];
@@ -220,47 +251,58 @@ __global__ __launch_bounds__(256, 1) void q4_tile_kernel(Q4Args a, int m_blocks,
 #pragma unroll
       for (int i = 0; i < 16; ++i) y[m][j][i] = 0.0f;
 
-  fetch(0);
-  sr[0] = (float)sp[0][0], sr[1] = (float)sp[1][0];
-  stage(lds);
+  fetch_meta(0);
+  fetch_x(0);
+  fetch_w(wc, 0);
+  stage_meta(0);
+  __syncthreads();
+  stage(0, wc[0]);
   __syncthreads();
   const uint32_t sw = (r32 >> 1) & 7;
-  for (int g = 0; g < groups; ++g) {
-    const uint8_t *from = lds + (g & 1) * BUF;
-    const float s0 = sr[0] * 0.0625f, s1 = sr[1] * 0.0625f;
-    if (g + 1 < groups) {
-      fetch(g + 1);
-      sr[0] = (float)sp[0][g + 1], sr[1] = (float)sp[1][g + 1];
-    }
-    bf16x8 w[2][4];
+  for (int g0 = 0; g0 < groups; g0 += 4) {
+    if (g0 % 16 == 0) fetch_meta(g0 + 16);
+    if (g0 % 16 == 8) stage_meta(g0 / 16 + 1);
+    fetch_w(wn4, g0 + 4);
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int step = 0; step < 4; ++step) {
+      const int g = g0 + step;
+      if (g >= groups) break;
+      const uint8_t *from = lds + (g & 1) * BUF;
+      float scale[2];
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        w[j][c] = *reinterpret_cast<const bf16x8 *>(from + PARTS * XB + (wn * 64 + j * 32 + r32) * 128 + (((2 * c + hi) ^ sw) << 4));
-#pragma unroll
-    for (int m = 0; m < MI; ++m) {
-      floatx16 d[2];
+      for (int j = 0; j < 2; ++j) scale[j] = (float)lds_s[g / 16 & 1][(wn * 64 + j * 32 + r32) * SROW + g % 16] * 0.0625f;
+      if (g + 1 < groups) fetch_x(g + 1);
+      bf16x8 w[2][4];
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) d[j][i] = 0.0f;
+        for (int c = 0; c < 4; ++c)
+          w[j][c] = *reinterpret_cast<const bf16x8 *>(from + PARTS * XB + (wn * 64 + j * 32 + r32) * 128 + (((2 * c + hi) ^ sw) << 4));
 #pragma unroll
-      for (int p = PARTS - 1; p >= 0; --p)
+      for (int m = 0; m < MI; ++m) {
+        floatx16 d[2];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const bf16x8 x = *reinterpret_cast<const bf16x8 *>(from + p * XB + (wm * (BM / 2) + m * 32 + r32) * 128 + (((2 * c + hi) ^ sw) << 4));
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) d[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, w[j][c], d[j], 0, 0, 0);
-        }
+          for (int i = 0; i < 16; ++i) d[j][i] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        y[m][0][i] = fmaf(s0, d[0][i], y[m][0][i]);
-        y[m][1][i] = fmaf(s1, d[1][i], y[m][1][i]);
+        for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const bf16x8 x = *reinterpret_cast<const bf16x8 *>(from + p * XB + (wm * (BM / 2) + m * 32 + r32) * 128 + (((2 * c + hi) ^ sw) << 4));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) d[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, w[j][c], d[j], 0, 0, 0);
+          }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) y[m][j][i] = fmaf(scale[j], d[j][i], y[m][j][i]);
       }
+      if (g + 1 < groups) stage(g + 1, step < 3 ? wc[(step + 1) % 4] : wn4[0]);
+      __syncthreads();
     }
-    if (g + 1 < groups) stage(lds + (~g & 1) * BUF);
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) wc[i] = wn4[i];
   }
 #pragma unroll
   for (int m = 0; m < MI; ++m)
@@ -295,7 +337,7 @@ hipError_t launch_q4_matmul(const Q4Args &a, bool f32, hipStream_t s) {
   if (a.rows <= 16) launch_small<1>(a, f32, s);
   else if (a.rows <= 32) launch_small<2>(a, f32, s);
   else if (f32) return a.rows <= 64 ? launch_tile<64, float>(a, s) : launch_tile<128, float>(a, s);
-  else return a.rows <= 64 ? launch_tile<64, uint16_t>(a, s) : a.rows <= 128 ? launch_tile<128, uint16_t>(a, s) : launch_tile<256, uint16_t>(a, s);
+  else return a.rows <= 64 ? launch_tile<64, uint16_t>(a, s) : a.rows <= 128000 ? launch_tile<128, uint16_t>(a, s) : launch_tile<256, uint16_t>(a, s);
   return hipGetLastError();
 }
 
