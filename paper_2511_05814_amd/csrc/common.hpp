@@ -449,6 +449,18 @@ __device__ inline void wave_topk_lds(const double *const (&z)[N], int E, int K, 
   for (int q = 0; q < N; ++q) id[q] = lane < K ? out[q][lane] : -1;
 }
 
+// Byte j of a word as a float (v_cvt_f32_ubyte<j>).  Written out because the
+// compiler otherwise extracts each field on its own before converting.
+template <int J>
+__device__ __forceinline__ float byte_to_f32(uint32_t m) {
+  float r;
+  if constexpr (J == 0) asm("v_cvt_f32_ubyte0 %0, %1" : "=v"(r) : "v"(m));
+  else if constexpr (J == 1) asm("v_cvt_f32_ubyte1 %0, %1" : "=v"(r) : "v"(m));
+  else if constexpr (J == 2) asm("v_cvt_f32_ubyte2 %0, %1" : "=v"(r) : "v"(m));
+  else asm("v_cvt_f32_ubyte3 %0, %1" : "=v"(r) : "v"(m));
+  return r;
+}
+
 // Eight consecutive elements of an fp32 or bf16 array as fp32, and back.
 __device__ __forceinline__ void load8(const float *p, float *f) {
   const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);

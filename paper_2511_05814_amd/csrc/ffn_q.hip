@@ -89,18 +89,6 @@ __device__ __forceinline__ void load_x(const float *p, int c, int n, float scale
   }
 }
 
-// Byte j of a word as a float (v_cvt_f32_ubyte<j>).  Written out because the
-// compiler otherwise extracts each 2-bit field on its own before converting.
-template <int J>
-__device__ __forceinline__ float byte_to_f32(uint32_t m) {
-  float r;
-  if constexpr (J == 0) asm("v_cvt_f32_ubyte0 %0, %1" : "=v"(r) : "v"(m));
-  else if constexpr (J == 1) asm("v_cvt_f32_ubyte1 %0, %1" : "=v"(r) : "v"(m));
-  else if constexpr (J == 2) asm("v_cvt_f32_ubyte2 %0, %1" : "=v"(r) : "v"(m));
-  else asm("v_cvt_f32_ubyte3 %0, %1" : "=v"(r) : "v"(m));
-  return r;
-}
-
 // sum over the unit's 64 columns of w_c x_c
 __device__ __forceinline__ float unit_dot(const QUnit &u, const float *x, const float *xs) {
   float out = 0.0f;

@@ -133,13 +133,12 @@ __device__ __forceinline__ void expand16(uint2 w, float zero, uint4 *out) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const uint32_t v = h ? w.y : w.x, even = v << 4 & 0xF0F0F0F0u, odd = v & 0xF0F0F0F0u;
-    uint32_t r[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const float a = (float)(even >> (8 * b) & 255u) - zero, c = (float)(odd >> (8 * b) & 255u) - zero;
-      r[b] = __builtin_amdgcn_perm(__float_as_uint(c), __float_as_uint(a), 0x07060302u);  // both exact: the upper halves
-    }
-    out[h] = make_uint4(r[0], r[1], r[2], r[3]);
+    // two exact differences make a pair of bf16 from their upper halves
+    auto pair = [&](float a, float c) {
+      return __builtin_amdgcn_perm(__float_as_uint(c - zero), __float_as_uint(a - zero), 0x07060302u);
+    };
+    out[h] = make_uint4(pair(byte_to_f32<0>(even), byte_to_f32<0>(odd)), pair(byte_to_f32<1>(even), byte_to_f32<1>(odd)),
+                        pair(byte_to_f32<2>(even), byte_to_f32<2>(odd)), pair(byte_to_f32<3>(even), byte_to_f32<3>(odd)));
   }
 }
 
@@ -257,6 +256,7 @@ __global__ __launch_bounds__(256, BM <= 128 && sizeof(T) == 2 ? 2 : 1) void q4_t
   stage_meta(0);
   __syncthreads();
   stage(0, wc[0]);
+  fetch_x(min(1, groups - 1));
   __syncthreads();
   const uint32_t sw = (r32 >> 1) & 7;
   for (int g0 = 0; g0 < groups; g0 += 4) {
@@ -271,13 +271,14 @@ __global__ __launch_bounds__(256, BM <= 128 && sizeof(T) == 2 ? 2 : 1) void q4_t
       float scale[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) scale[j] = (float)lds_s[g / 16 & 1][(wn * 64 + j * 32 + r32) * SROW + g % 16] * 0.0625f;
-      if (g + 1 < groups) fetch_x(g + 1);
       bf16x8 w[2][4];
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
           w[j][c] = *reinterpret_cast<const bf16x8 *>(from + PARTS * XB + (wn * 64 + j * 32 + r32) * 128 + (((2 * c + hi) ^ sw) << 4));
+      stage(g + 1, step < 3 ? wc[(step + 1) % 4] : wn4[0]);
+      fetch_x(min(g + 2, groups - 1));
 #pragma unroll
       for (int m = 0; m < MI; ++m) {
         floatx16 d[2];
@@ -298,7 +299,6 @@ __global__ __launch_bounds__(256, BM <= 128 && sizeof(T) == 2 ? 2 : 1) void q4_t
 #pragma unroll
           for (int i = 0; i < 16; ++i) y[m][j][i] = fmaf(scale[j], d[j][i], y[m][j][i]);
       }
-      if (g + 1 < groups) stage(g + 1, step < 3 ? wc[(step + 1) % 4] : wn4[0]);
       __syncthreads();
     }
 #pragma unroll
