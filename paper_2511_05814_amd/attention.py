@@ -132,8 +132,9 @@ def kv4_append(q, k, v, cos, sin, pool, page_table, q_start, kv_len, out: Option
     batch = _batch(device, pool, page_table, q_start, kv_len, tokens, head_dim)
     kv_shape = (tokens, batch.kv_heads, head_dim)
     positions, half = cos.shape
-    if _rows("cos", cos, device, torch.float32, (positions, half)) != half or \
-            _rows("sin", sin, device, torch.float32, (positions, half)) != half:
+    _rows("cos", cos, device, torch.float32, (positions, half))
+    _rows("sin", sin, device, torch.float32, (positions, half))
+    if not cos.is_contiguous() or not sin.is_contiguous():
         raise ValueError("cos and sin must be contiguous")
     if out is None:
         out, out_stride = q.new_empty(shape), heads * head_dim

@@ -304,12 +304,16 @@ struct KvAttnArgs {
   float *part;                 // [splits][tokens * heads][D]
   float *ml;                   // [splits][tokens * heads][2]
   float scale;
-  int heads, splits, row_blocks;
+  int heads, splits, row_blocks, prompt;
 };
 hipError_t launch_kv4_append(const KvAppendArgs &a, int head_dim, bool f32, hipStream_t s);
 hipError_t launch_kv4_read(const KvReadArgs &a, int head_dim, bool f32, hipStream_t s);
-// Splits of the keys that a launch of kv4_attention takes, and workgroups along its rows.
-void kv4_attention_shape(int seqs, int kv_heads, int heads, int max_new, int max_len, int *splits, int *row_blocks);
+// How a launch of kv4_attention is cut: splits of the keys, workgroups along the
+// rows, and whether rows go in the large blocks of the prompt kernel.
+struct KvAttnShape {
+  int splits, row_blocks, prompt;
+};
+KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int max_new, int max_len);
 hipError_t launch_kv4_attention(const KvAttnArgs &a, int head_dim, bool f32, hipStream_t s);
 
 struct Q4Args {

@@ -17,15 +17,11 @@ constexpr int kTile = 32;           // tokens of a wave's step
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kPShift = 14.0f;    // probabilities are held times 2^14: fp16 keeps 2^-38 of the largest
 
-// 2^(s - top) in that scale.  s - top is exact near the top, so that 2^14 is
-// not passed even where a score's last place is worth more than 1.
-__device__ __forceinline__ float power(float s, float top) {
-#pragma clang fp contract(off)
-  return __builtin_amdgcn_exp2f((s - top) + kPShift);
-}
-__device__ __forceinline__ float scaled(float dot, float down) {
-#pragma clang fp contract(off)
-  return dot * down;
+// 2^((dot - top) down) in that scale.  The difference of dot products is exact
+// near the top, so that 2^14 is not passed even where the last place of a score
+// is worth more than 1.
+__device__ __forceinline__ float power(float dot, float top, float down) {
+  return __builtin_amdgcn_exp2f(fmaf(dot - top, down, kPShift));
 }
 
 // Codes of a word that lie 16 bits apart, as pairs of fp16 1024 + q (low
@@ -33,6 +29,23 @@ __device__ __forceinline__ float scaled(float dot, float down) {
 __device__ __forceinline__ half2v low_nibbles(uint32_t w) { return __builtin_bit_cast(half2v, (w & 0x000F000Fu) | 0x64006400u); }
 __device__ __forceinline__ half2v high_nibbles(uint32_t w) { return __builtin_bit_cast(half2v, (w & 0x00F000F0u) | 0x64006400u); }
 __device__ __forceinline__ half2v both(float v) { return half2v{(_Float16)v, (_Float16)v}; }
+
+// A row of q goes to fp16 times a power of two that brings its largest element
+// to 2^9 .. 2^10 (and the sign of the scale).  Its dot products times `unit`,
+// exactly, are those of q and k, and times `down` the exponents of 2.
+struct RowScale {
+  float up, unit, down;
+};
+// |scale| log2(e), kept off zero so that a masked score is minus infinity in any scale
+__device__ __forceinline__ float exponent_factor(float scale) { return fmaxf(fabsf(scale) * kLog2e, 0x1p-50f); }
+__device__ __forceinline__ RowScale row_scale(float amax, float scale) {
+  const int exponent = min(max((int)(__float_as_uint(amax) >> 23) - 127, -60), 127);
+  RowScale r;
+  r.up = copysignf(ldexpf(1.0f, 9 - exponent), scale);
+  r.unit = ldexpf(1.0f, exponent - 9);
+  r.down = exponent_factor(scale) * r.unit;
+  return r;
+}
 
 // scale(k), which fp16 holds exactly; NaN for the mark of a group that could not be stored
 __device__ __forceinline__ float meta_scale(uint32_t meta) {
@@ -103,6 +116,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
   const size_t page_bytes = (size_t)(D * 9 / 8) << a.kv.page_log2;
   const int32_t *table = a.kv.page_table + b * a.kv.table_stride;
   const int page_mask = (1 << a.kv.page_log2) - 1;
+  const float factor = exponent_factor(a.scale);
 
   for (int row0 = blockIdx.y * 16; row0 < seq.rows; row0 += gridDim.y * 16) {
     const int row = min(row0 + r, seq.rows - 1);
@@ -122,14 +136,14 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
       for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(f[t][e]));
     }
     amax = max_over_j(amax);
-    const int exponent = min(max((int)(__float_as_uint(amax) >> 23) - 127, -110), 127);
-    const float up = ldexpf(1.0f, 9 - exponent), down = a.scale * kLog2e * ldexpf(1.0f, exponent - 9);
+    const RowScale rs = row_scale(amax, a.scale);
+    const float down = rs.down;
 #pragma unroll
     for (int t = 0; t < KW; ++t)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int from = e / 2 + 4 * (e & 1);
-        float v = f[t][from] * up;
+        float v = f[t][from] * rs.up;
         q[0][t][e] = (_Float16)v;
         if constexpr (PARTS == 2) q[1][t][e] = (_Float16)(v - (float)q[0][t][e]);
       }
@@ -171,7 +185,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
           for (int p = PARTS - 1; p >= 0; --p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[p][t], acc, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[h][i] = held && at + 4 * j + i <= last ? scaled(acc[i], down) : -__builtin_inff();
+        for (int i = 0; i < 4; ++i) s[h][i] = held && at + 4 * j + i <= last ? acc[i] : -__builtin_inff();
         // tokens that no row of the tile sees must not reach the products, whatever their bytes are
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -183,13 +197,13 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
       for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i / 4][i % 4]);
       top = fmaxf(m, max_over_j(top));
       const float ref = top == -__builtin_inff() ? 0.0f : top;
-      const float keep = __builtin_amdgcn_exp2f(m - ref);
+      const float keep = __builtin_amdgcn_exp2f((m - ref) * down);
       m = top;
       half8 p[PARTS];
       float add = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float v = power(s[i / 4][i % 4], ref);
+        const float v = power(s[i / 4][i % 4], ref, down);
         p[0][i] = (_Float16)v;
         float used = (float)p[0][i];
         if constexpr (PARTS == 2) {
@@ -266,7 +280,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
         *reinterpret_cast<float4 *>(&s_o[wave][r][dim + u]) = make_float4(o[u][i], o[u + 1][i], o[u + 2][i], o[u + 3][i]);
     }
     if (j == 0) {
-      s_ml[wave][r][0] = m;
+      s_ml[wave][r][0] = m * rs.unit;
       s_ml[wave][r][1] = l;
     }
     __syncthreads();
@@ -278,7 +292,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const float f = s_ml[w][orow][0] == -__builtin_inff() ? (s_ml[w][orow][1] == 0.0f ? 0.0f : 1.0f)
-                                                             : __builtin_amdgcn_exp2f(s_ml[w][orow][0] - top);
+                                                             : __builtin_amdgcn_exp2f((s_ml[w][orow][0] - top) * factor);
       if (f == 0.0f) continue;
       total += s_ml[w][orow][1] * f;
 #pragma unroll
@@ -309,6 +323,310 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
   }
 }
 
+// Rows of prompts: 128 rows a workgroup, 32 a wave, over tiles of 64 tokens.
+//
+// The workgroup expands a tile's keys and values once, into LDS and in the
+// order of the operands, 16 bytes a lane, so that reads and writes go through
+// the banks in lane order.  Scores are again transposed: a lane has a row's
+// (lane % 32) scores of tokens 8 b + 4 (lane / 32) + 0 .. 3 of each block of 32,
+// which is the operand of O^T = V^T P^T when its sum takes the tokens in that
+// order.  Two tiles of LDS, one barrier a tile; the bytes of the tile after
+// next are on their way to registers.
+constexpr int kPromptTile = 64, kPromptRows = 128;
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Maximum and sum of the two lanes that share a row.
+__device__ __forceinline__ float max_of_halves(float v) { return fmaxf(v, __shfl_xor(v, 32, kWave)); }
+
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_kernel(KvAttnArgs a) {
+  constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
+  constexpr int KS = D / 16;           // steps of a score's dot product
+  constexpr int NB = D / 32;           // output blocks of 32 dimensions
+  constexpr int KW = D / 32;           // words of a key that a thread expands
+  constexpr int KB = 32 * D * 2;       // LDS bytes of 32 keys, or of 32 values
+  __shared__ __align__(16) uint8_t s_kv[2][4 * KB];          // keys of both blocks, values of both
+  __shared__ __align__(16) uint8_t s_mark[2][D / 32][kPromptTile];  // value groups that are marked as not stored
+  __shared__ uint32_t s_any[2][kWaves];
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = lane & 31, hi = lane >> 5;
+  const int b = blockIdx.x / a.kv.kv_heads, g = blockIdx.x % a.kv.kv_heads;
+  const int group = a.heads / a.kv.kv_heads;
+  const Seq seq = sequence(a, b, group);
+  const size_t page_bytes = (size_t)(D * 9 / 8) << a.kv.page_log2;
+  const size_t values = (size_t)(D / 2) << a.kv.page_log2, kmetas = (size_t)D << a.kv.page_log2, vmetas = kmetas + ((size_t)(D / 16) << a.kv.page_log2);
+  const int32_t *table = a.kv.page_table + b * a.kv.table_stride;
+  const int page_mask = (1 << a.kv.page_log2) - 1;
+  const int stride = a.splits * kPromptTile;
+
+  // the page of token `at`, and whether there is one
+  auto page_of = [&](int at, bool &held) {
+    const int col = at >> a.kv.page_log2;
+    const int page = __builtin_amdgcn_readfirstlane(col < a.kv.table_cols ? table[col] : -1);
+    held = page >= 0 && page < a.kv.pages;
+    return a.kv.pool + ((size_t)(held ? page : 0) * a.kv.kv_heads + g) * page_bytes;
+  };
+
+  for (int block = gridDim.y - 1 - blockIdx.y; block * kPromptRows < seq.rows; block += gridDim.y) {
+    const int wrow = block * kPromptRows + wave * 32;   // the wave's first row
+    const int row = min(wrow + r, seq.rows - 1);
+    const int token = seq.start + row / group, head = g * group + row % group;
+    const int last = min(seq.first + row / group, seq.held - 1);
+    const int wfirst = min(seq.first + min(wrow, seq.rows - 1) / group, seq.held - 1);
+    const int wend = wrow < seq.rows ? min(seq.first + min(wrow + 31, seq.rows - 1) / group, seq.held - 1) + 1 : 0;
+    const int end = min(seq.first + min(block * kPromptRows + kPromptRows - 1, seq.rows - 1) / group, seq.held - 1) + 1;
+
+    half8 q[PARTS][KS];
+    const T *qp = static_cast<const T *>(a.q) + token * a.q_stride + head * D + 8 * hi;
+    float amax = 0.0f;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) {
+      float f[8];
+      load8(qp + 16 * t, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(f[e]));
+    }
+    const RowScale rs = row_scale(max_of_halves(amax), a.scale);
+#pragma unroll
+    for (int t = 0; t < KS; ++t) {
+      float f[8];
+      load8(qp + 16 * t, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = f[e / 2 + 4 * (e & 1)] * rs.up;
+        q[0][t][e] = (_Float16)v;
+        if constexpr (PARTS == 2) q[1][t][e] = (_Float16)(v - (float)q[0][t][e]);
+      }
+    }
+
+    float m = -__builtin_inff(), l = 0.0f;
+    floatx16 o[NB];
+#pragma unroll
+    for (int u = 0; u < NB; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[u][i] = 0.0f;
+
+    // A thread's share of a tile: words KW * (2 (wave / 2) + hi) .. of key
+    // 32 (wave % 2) + r, and, of the 8 dimensions of octet r / (8 / NB), NB of
+    // values 32 (wave % 2) + 16 (wave / 2) + 4 hi + 0 .. 3 and + 8.
+    uint32_t kw[KW], km;
+    u32x4 vw[2];
+    u32x2 vm[2];
+    bool k_held, v_held;
+    auto fetch = [&](int t0) {
+      const int sub = t0 + 32 * (wave & 1);
+      bool h0, h1;
+      const uint8_t *p0 = page_of(sub, h0), *p1 = page_of(sub + 16, h1);
+      const uint8_t *rec = r < 16 ? p0 : p1;
+      k_held = r < 16 ? h0 : h1;
+      const int in = (sub + r) & page_mask, part = 2 * (wave >> 1) + hi;
+      const uint8_t *kp = rec + (size_t)in * (D / 2) + KW * 4 * part;
+      if constexpr (KW == 4) *reinterpret_cast<u32x4 *>(kw) = *reinterpret_cast<const u32x4 *>(kp);
+      else *reinterpret_cast<u32x2 *>(kw) = *reinterpret_cast<const u32x2 *>(kp);
+      km = *reinterpret_cast<const uint16_t *>(rec + kmetas + in * (D / 16) + (D == 128 ? part : part / 2) * 2);
+      const uint8_t *vrec = wave >> 1 ? p1 : p0;
+      v_held = wave >> 1 ? h1 : h0;
+      const int quad = (((sub + 16 * (wave >> 1)) & page_mask) >> 2) + hi, oct = r / (8 / NB);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        vw[x] = *reinterpret_cast<const u32x4 *>(vrec + values + (size_t)(quad + 2 * x) * (2 * D) + oct * 16);
+        vm[x] = *reinterpret_cast<const u32x2 *>(vrec + vmetas + (quad + 2 * x) * (D / 4) + oct / 4 * 8);
+      }
+    };
+    auto stage = [&](int t0, int buf) {
+      uint8_t *to = s_kv[buf];
+      {
+        const float z = (float)(km & 255);
+        const half2v scale = both(meta_scale(km)), low = both(-1024.0f - z), high = both(-64.0f - z);
+        const int w0 = KW * (2 * (wave >> 1) + hi);
+#pragma unroll
+        for (int x = 0; x < KW; ++x)
+          *reinterpret_cast<half8 *>(to + (wave & 1) * KB + (w0 + x) * 512 + r * 16) = key_values(kw[x], low, high, scale);
+      }
+      const int tok = t0 + 32 * (wave & 1) + 16 * (wave >> 1) + 4 * hi;
+      half2v scale[4], low[4], high[4];
+      uint32_t marks[2] = {0, 0};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t two[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int n = 2 * (e & 1) + s;  // token of the quad
+          two[s] = vm[e / 2][n / 2] >> (16 * (n & 1)) & 0xFFFF;
+          // tokens that no row sees must not reach the products, whatever their bytes are
+          if (!v_held || tok + 8 * (e / 2) + n >= end) two[s] = 0;
+          marks[e / 2] |= (two[s] >> 8) == 255 ? 1u << (8 * n) : 0u;
+        }
+        scale[e] = half2v{(_Float16)__uint_as_float(((two[0] >> 8) + 848) << 20), (_Float16)__uint_as_float(((two[1] >> 8) + 848) << 20)};
+        const half2v z = half2v{(_Float16)(float)(two[0] & 255), (_Float16)(float)(two[1] & 255)};
+        low[e] = both(-1024.0f) - z;
+        high[e] = both(-64.0f) - z;
+      }
+      const half2v sixteenth = both(0.0625f);
+      const int shift = r % (8 / NB) * (4 * NB);
+#pragma unroll
+      for (int bt = 0; bt < NB / 2; ++bt) {
+        half8 v0, v1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t x0 = vw[e / 2][2 * (e & 1)] >> shift, x1 = vw[e / 2][2 * (e & 1) + 1] >> shift;
+          const uint32_t x = __builtin_amdgcn_perm(x1, x0, 0x0C000C00u | bt | (uint32_t)(4 + bt) << 16);
+          const half2v a0 = (low_nibbles(x) + low[e]) * scale[e];
+          const half2v a1 = __builtin_elementwise_fma(high_nibbles(x), sixteenth, high[e]) * scale[e];
+          v0[2 * e] = a0[0], v0[2 * e + 1] = a0[1];
+          v1[2 * e] = a1[0], v1[2 * e + 1] = a1[1];
+        }
+        uint8_t *at = to + 2 * KB + (wave & 1) * KB + (wave >> 1) * 1024 + lane * 16;
+        *reinterpret_cast<half8 *>(at + (2 * bt) * 2048) = v0;
+        *reinterpret_cast<half8 *>(at + (2 * bt + 1) * 2048) = v1;
+      }
+      const uint64_t any = __builtin_amdgcn_ballot_w64(marks[0] | marks[1]);
+      if (lane == 0) s_any[buf][wave] = any != 0;
+      if (r % 8 == 0) {   // a lane of each group of 32 dimensions (D 64: of each half)
+        const int grp = r / (8 / NB) / 4;
+        uint8_t *mp = &s_mark[buf][grp][32 * (wave & 1) + 16 * (wave >> 1) + 4 * hi];
+        *reinterpret_cast<uint32_t *>(mp) = marks[0];
+        *reinterpret_cast<uint32_t *>(mp + 8) = marks[1];
+      }
+    };
+
+    int t0 = (int)blockIdx.z * kPromptTile, buf = 0;
+    if (t0 < end) {
+      fetch(t0);
+      stage(t0, 0);
+      if (t0 + stride < end) fetch(t0 + stride);
+    }
+    for (; t0 < end; t0 += stride, buf ^= 1) {
+      __syncthreads();
+      const uint8_t *from = s_kv[buf];
+      if (t0 + stride < end) {
+        stage(t0 + stride, buf ^ 1);
+        if (t0 + 2 * stride < end) fetch(t0 + 2 * stride);
+      }
+      if (t0 >= wend) continue;
+      __builtin_amdgcn_sched_barrier(0);   // staging's registers are free again before the scores take theirs
+      floatx16 s[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        if (x) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[x][i] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < KS; ++t) {
+          const half8 k = *reinterpret_cast<const half8 *>(from + x * KB + t * 1024 + lane * 16);
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[p][t], s[x], 0, 0, 0);
+        }
+      }
+      bool whole = t0 + kPromptTile - 1 <= wfirst;
+      bool held[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        page_of(t0 + 16 * x, held[x]);
+        whole &= held[x];
+      }
+      if (!whole) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int at = 32 * x + 8 * (i / 4) + 4 * hi + i % 4;
+            if (t0 + at > last || !held[2 * x + i / 8]) s[x][i] = -__builtin_inff();
+          }
+      }
+      float top = m;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[x][i]);
+      top = max_of_halves(top);
+      const float ref = top == -__builtin_inff() ? 0.0f : top;
+      if (__builtin_amdgcn_ballot_w64(top > m)) {
+        const float keep = __builtin_amdgcn_exp2f((m - ref) * rs.down);
+        l *= keep;
+#pragma unroll
+        for (int u = 0; u < NB; ++u) o[u] *= keep;
+      }
+      m = top;
+      const half2v one = both(1.0f);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          half8 p[PARTS];
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const float v0 = power(s[x][8 * h + e], ref, rs.down), v1 = power(s[x][8 * h + e + 1], ref, rs.down);
+            const half2v hp = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(v0, v1));
+            p[0][e] = hp[0], p[0][e + 1] = hp[1];
+            l = __builtin_amdgcn_fdot2(hp, one, l, false);
+            if constexpr (PARTS == 2) {
+              const half2v lp = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(v0 - (float)hp[0], v1 - (float)hp[1]));
+              p[1][e] = lp[0], p[1][e + 1] = lp[1];
+              l = __builtin_amdgcn_fdot2(lp, one, l, false);
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < NB; ++u) {
+            const half8 v = *reinterpret_cast<const half8 *>(from + 2 * KB + x * KB + u * 2048 + h * 1024 + lane * 16);
+#pragma unroll
+            for (int part = PARTS - 1; part >= 0; --part) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[part], o[u], 0, 0, 0);
+          }
+        }
+      // Groups marked as not stored: counted for the rows that see them, as in
+      // the kernel above.
+      if (s_any[buf][0] | s_any[buf][1] | s_any[buf][2] | s_any[buf][3]) {
+        floatx16 count;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) count[i] = 0.0f;
+        const uint8_t *marks = s_mark[buf][r / (8 / NB) / 4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          half8 mark, seen;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int at = 16 * x + 8 * (e / 4) + 4 * hi + e % 4;
+            mark[e] = (_Float16)(float)marks[at];
+            seen[e] = (_Float16)(t0 + at <= last ? 1.0f : 0.0f);
+          }
+          count = __builtin_amdgcn_mfma_f32_32x32x16_f16(mark, seen, count, 0, 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < NB; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[u][i] = count[i] > 0.0f ? __builtin_nanf("") : o[u][i];
+      }
+    }
+    __syncthreads();   // the tiles of the next block of rows go to the same LDS
+    l += __shfl_xor(l, 32, kWave);
+    if (wrow + r >= seq.rows) continue;
+    const int64_t at = (int64_t)blockIdx.z * a.kv.tokens * a.heads + (int64_t)token * a.heads + head;
+    const float inv = a.splits > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      // block x of output rows: NB * 4 consecutive dimensions
+      float f[4 * NB];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int u = 0; u < NB; ++u) f[NB * i + u] = o[u][4 * x + i] * inv;
+      const int dim = (8 * NB) * x + 4 * NB * hi;
+#pragma unroll
+      for (int e = 0; e < 4 * NB; e += 8) {
+        if (a.splits > 1) store8(a.part + at * D + dim + e, f + e);
+        else store8(static_cast<T *>(a.o) + token * a.o_stride + head * D + dim + e, f + e);
+      }
+    }
+    if (a.splits > 1 && hi == 0) {
+      a.ml[2 * at] = m * rs.unit;
+      a.ml[2 * at + 1] = l;
+    }
+  }
+}
+
 // Joins the splits of a row; D / 4 lanes a row.
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads) void kv4_join_kernel(KvAttnArgs a) {
@@ -317,13 +635,14 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(KvAttnArgs a) {
   const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes;
   if (row >= rows) return;
   const int dim = threadIdx.x % kLanes * 4;
+  const float factor = exponent_factor(a.scale);
   float top = -__builtin_inff(), total = 0.0f;
   float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.ml[2 * (s * rows + row)]);
   for (int s = 0; s < a.splits; ++s) {
     const float m = a.ml[2 * (s * rows + row)], l = a.ml[2 * (s * rows + row) + 1];
     if (m == -__builtin_inff() && l == 0.0f) continue;
-    const float f = m == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+    const float f = m == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m - top) * factor);
     const float4 o = *reinterpret_cast<const float4 *>(a.part + (s * rows + row) * D + dim);
     total += l * f;
     acc.x += o.x * f, acc.y += o.y * f, acc.z += o.z * f, acc.w += o.w * f;
@@ -337,7 +656,8 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(KvAttnArgs a) {
 template <int D, typename T>
 void launch(const KvAttnArgs &a, hipStream_t s) {
   const dim3 grid(a.kv.seqs * a.kv.kv_heads, a.row_blocks, a.splits);
-  hipLaunchKernelGGL((kv4_attention_kernel<D, T>), grid, dim3(kThreads), 0, s, a);
+  if (a.prompt) hipLaunchKernelGGL((kv4_prompt_kernel<D, T>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((kv4_attention_kernel<D, T>), grid, dim3(kThreads), 0, s, a);
   if (a.splits > 1) {
     const int64_t lanes = (int64_t)a.kv.tokens * a.heads * (D / 4);
     hipLaunchKernelGGL((kv4_join_kernel<D, T>), dim3((unsigned)((lanes + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a);
@@ -346,15 +666,21 @@ void launch(const KvAttnArgs &a, hipStream_t s) {
 
 }  // namespace
 
-// Enough workgroups for four on each of the 256 compute units, none with less
-// than one block of 32 tokens a wave.
-void kv4_attention_shape(int seqs, int kv_heads, int heads, int max_new, int max_len, int *splits, int *row_blocks) {
+// Rows in blocks of 16, or of 128 from 64 rows a sequence and kv head on; enough
+// workgroups for four (two with large blocks) on each of the 256 compute units,
+// none with less than one block of 32 tokens a wave (one tile).
+KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int max_new, int max_len) {
+  KvAttnShape s;
   const int64_t rows = (int64_t)max_new * (heads / kv_heads);
-  *row_blocks = (int)((rows + 15) / 16 < 1 ? 1 : (rows + 15) / 16 > 65535 ? 65535 : (rows + 15) / 16);
-  const int64_t units = (int64_t)seqs * kv_heads * *row_blocks, most = ((int64_t)max_len + kWaves * kTile - 1) / (kWaves * kTile);
-  int64_t n = 1024 / units;
+  s.prompt = rows >= 64;
+  const int per = s.prompt ? kPromptRows : 16, tile = s.prompt ? kPromptTile : kWaves * kTile;
+  const int64_t blocks = (rows + per - 1) / per;
+  s.row_blocks = (int)(blocks > 65535 ? 65535 : blocks);
+  const int64_t units = (int64_t)seqs * kv_heads * s.row_blocks, most = ((int64_t)max_len + tile - 1) / tile;
+  int64_t n = (s.prompt ? 512 : 1024) / units;
   n = n > most ? most : n;
-  *splits = (int)(n < 1 ? 1 : n);
+  s.splits = (int)(n < 1 ? 1 : n);
+  return s;
 }
 
 hipError_t launch_kv4_attention(const KvAttnArgs &a, int head_dim, bool f32, hipStream_t s) {
