@@ -74,6 +74,26 @@ __device__ __forceinline__ float sum_over_j(float v) {
   return v + __shfl_xor(v, 32, kWave);
 }
 
+// A workgroup's split, block of rows and (sequence, kv head), in this order in a
+// launch's one dimension.  Workgroups go to the XCDs, and there to the shader
+// engines, in turn: with the sequences in the first place four of them, one
+// long, put all of its work on one engine of each XCD (682 us instead of 239
+// for prompts of 2048 tokens over 2048 and three shorter ones).
+struct Place {
+  int split, block, seq, kv_head;
+};
+__device__ __forceinline__ Place place(const KvAttnArgs &a) {
+  Place p;
+  uint32_t id = blockIdx.x;
+  p.split = id % (uint32_t)a.splits;
+  id /= (uint32_t)a.splits;
+  p.block = id % (uint32_t)a.row_blocks;
+  id /= (uint32_t)a.row_blocks;
+  p.kv_head = id % (uint32_t)a.kv.kv_heads;
+  p.seq = id / (uint32_t)a.kv.kv_heads;
+  return p;
+}
+
 // What a workgroup needs to know of its sequence.
 struct Seq {
   int start, rows;   // first new token; rows = new tokens * heads a kv head
@@ -110,7 +130,8 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane & 15, j = lane >> 4;
-  const int b = blockIdx.x / a.kv.kv_heads, g = blockIdx.x % a.kv.kv_heads;
+  const Place where = place(a);
+  const int b = where.seq, g = where.kv_head, split = where.split;
   const int group = a.heads / a.kv.kv_heads;
   const Seq seq = sequence(a, b, group);
   const size_t page_bytes = (size_t)(D * 9 / 8) << a.kv.page_log2;
@@ -118,7 +139,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
   const int page_mask = (1 << a.kv.page_log2) - 1;
   const float factor = exponent_factor(a.scale);
 
-  for (int row0 = blockIdx.y * 16; row0 < seq.rows; row0 += gridDim.y * 16) {
+  for (int row0 = where.block * 16; row0 < seq.rows; row0 += a.row_blocks * 16) {
     const int row = min(row0 + r, seq.rows - 1);
     const int token = seq.start + row / group, head = g * group + row % group;
     const int last = min(seq.first + row / group, seq.held - 1);  // this row's last position
@@ -150,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
 
     float m = -__builtin_inff(), l = 0.0f;
     floatx4 o[NU] = {};
-    for (int t0 = ((int)blockIdx.z * kWaves + wave) * kTile; t0 < end; t0 += a.splits * kWaves * kTile) {
+    for (int t0 = (split * kWaves + wave) * kTile; t0 < end; t0 += a.splits * kWaves * kTile) {
       float s[2][4];
       uint32_t vw[2][4], vm[2][4];   // value words and metas of the lane's eight tokens
       const int c = r, oct = D == 64 ? c & 7 : c;
@@ -310,7 +331,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
           else out[e] = (uint16_t)bf16_pair(acc[e] * inv, 0.0f);
         }
       } else {
-        const int64_t at = (int64_t)blockIdx.z * a.kv.tokens * a.heads + out_row;
+        const int64_t at = (int64_t)split * a.kv.tokens * a.heads + out_row;
 #pragma unroll
         for (int e = 0; e < kPer; ++e) a.part[at * D + dim + e] = acc[e];
         if (dim == 0) {
@@ -353,7 +374,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane & 31, hi = lane >> 5;
-  const int b = blockIdx.x / a.kv.kv_heads, g = blockIdx.x % a.kv.kv_heads;
+  const Place where = place(a);
+  const int b = where.seq, g = where.kv_head, split = where.split;
   const int group = a.heads / a.kv.kv_heads;
   const Seq seq = sequence(a, b, group);
   const size_t page_bytes = (size_t)(D * 9 / 8) << a.kv.page_log2;
@@ -370,7 +392,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
     return a.kv.pool + ((size_t)(held ? page : 0) * a.kv.kv_heads + g) * page_bytes;
   };
 
-  for (int block = gridDim.y - 1 - blockIdx.y; block * kPromptRows < seq.rows; block += gridDim.y) {
+  for (int block = a.row_blocks - 1 - where.block; block * kPromptRows < seq.rows; block += a.row_blocks) {
     const int wrow = block * kPromptRows + wave * 32;   // the wave's first row
     const int row = min(wrow + r, seq.rows - 1);
     const int token = seq.start + row / group, head = g * group + row % group;
@@ -493,7 +515,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
       }
     };
 
-    int t0 = (int)blockIdx.z * kPromptTile, buf = 0;
+    int t0 = split * kPromptTile, buf = 0;
     if (t0 < end) {
       fetch(t0);
       stage(t0, 0);
@@ -603,7 +625,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
     __syncthreads();   // the tiles of the next block of rows go to the same LDS
     l += __shfl_xor(l, 32, kWave);
     if (wrow + r >= seq.rows) continue;
-    const int64_t at = (int64_t)blockIdx.z * a.kv.tokens * a.heads + (int64_t)token * a.heads + head;
+    const int64_t at = (int64_t)split * a.kv.tokens * a.heads + (int64_t)token * a.heads + head;
     const float inv = a.splits > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -627,25 +649,51 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
   }
 }
 
-// Joins the splits of a row; D / 4 lanes a row.
-template <int D, typename T>
+// Joins the splits of a row, D / 4 lanes over its dimensions.  With WIDE a
+// workgroup has one row and its groups of lanes share out the splits (few rows,
+// many splits); otherwise every group has a row of its own.
+template <int D, typename T, bool WIDE>
 __global__ __launch_bounds__(kThreads) void kv4_join_kernel(KvAttnArgs a) {
-  constexpr int kLanes = D / 4;
+  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
   const int64_t rows = (int64_t)a.kv.tokens * a.heads;
-  const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes;
+  const int grp = threadIdx.x / kLanes, dim = threadIdx.x % kLanes * 4;
+  const int64_t row = WIDE ? blockIdx.x : (int64_t)blockIdx.x * kGroups + grp;
   if (row >= rows) return;
-  const int dim = threadIdx.x % kLanes * 4;
   const float factor = exponent_factor(a.scale);
-  float top = -__builtin_inff(), total = 0.0f;
+  const float2 *ml = reinterpret_cast<const float2 *>(a.ml) + row;
+  float top = -__builtin_inff();
+  if constexpr (WIDE) {
+    for (int s = threadIdx.x % kWave; s < a.splits; s += kWave) top = fmaxf(top, ml[s * rows].x);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+  } else {
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s * rows].x);
+  }
+  float total = 0.0f;
   float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.ml[2 * (s * rows + row)]);
-  for (int s = 0; s < a.splits; ++s) {
-    const float m = a.ml[2 * (s * rows + row)], l = a.ml[2 * (s * rows + row) + 1];
-    if (m == -__builtin_inff() && l == 0.0f) continue;
-    const float f = m == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((m - top) * factor);
+#pragma unroll 4
+  for (int s = WIDE ? grp : 0; s < a.splits; s += WIDE ? kGroups : 1) {
+    const float2 v = ml[s * rows];
     const float4 o = *reinterpret_cast<const float4 *>(a.part + (s * rows + row) * D + dim);
-    total += l * f;
+    // a split without tokens has no sum; one of NaN scores alone has no maximum
+    const float f = v.x == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((v.x - top) * factor);
+    if (v.y == 0.0f) continue;
+    total += v.y * f;
     acc.x += o.x * f, acc.y += o.y * f, acc.z += o.z * f, acc.w += o.w * f;
+  }
+  if constexpr (WIDE) {
+    __shared__ float4 s_acc[kGroups][kLanes];
+    __shared__ float s_total[kGroups];
+    s_acc[grp][dim / 4] = acc;
+    if (dim == 0) s_total[grp] = total;
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int i = 1; i < kGroups; ++i) {
+      const float4 o = s_acc[i][dim / 4];
+      total += s_total[i];
+      acc.x += o.x, acc.y += o.y, acc.z += o.z, acc.w += o.w;
+    }
   }
   const float inv = total == 0.0f ? 0.0f : 1.0f / total;
   T *out = static_cast<T *>(a.o) + row / a.heads * a.o_stride + row % a.heads * D + dim;
@@ -655,13 +703,14 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(KvAttnArgs a) {
 
 template <int D, typename T>
 void launch(const KvAttnArgs &a, hipStream_t s) {
-  const dim3 grid(a.kv.seqs * a.kv.kv_heads, a.row_blocks, a.splits);
+  const dim3 grid((unsigned)a.kv.seqs * a.kv.kv_heads * a.row_blocks * a.splits);
   if (a.prompt) hipLaunchKernelGGL((kv4_prompt_kernel<D, T>), grid, dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL((kv4_attention_kernel<D, T>), grid, dim3(kThreads), 0, s, a);
-  if (a.splits > 1) {
-    const int64_t lanes = (int64_t)a.kv.tokens * a.heads * (D / 4);
-    hipLaunchKernelGGL((kv4_join_kernel<D, T>), dim3((unsigned)((lanes + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a);
-  }
+  if (a.splits == 1) return;
+  const int64_t rows = (int64_t)a.kv.tokens * a.heads;
+  constexpr int kGroups = kThreads / (D / 4);
+  if (a.splits >= kGroups) hipLaunchKernelGGL((kv4_join_kernel<D, T, true>), dim3((unsigned)rows), dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((kv4_join_kernel<D, T, false>), dim3((unsigned)((rows + kGroups - 1) / kGroups)), dim3(kThreads), 0, s, a);
 }
 
 }  // namespace
@@ -675,8 +724,9 @@ KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int max_new, 
   s.prompt = rows >= 64;
   const int per = s.prompt ? kPromptRows : 16, tile = s.prompt ? kPromptTile : kWaves * kTile;
   const int64_t blocks = (rows + per - 1) / per;
-  s.row_blocks = (int)(blocks > 65535 ? 65535 : blocks);
-  const int64_t units = (int64_t)seqs * kv_heads * s.row_blocks, most = ((int64_t)max_len + tile - 1) / tile;
+  const int64_t pairs = (int64_t)seqs * kv_heads, room = ((int64_t)1 << 30) / pairs;  // of a launch's workgroups
+  s.row_blocks = (int)(blocks > room ? (room < 1 ? 1 : room) : blocks);
+  const int64_t units = pairs * s.row_blocks, most = ((int64_t)max_len + tile - 1) / tile;
   int64_t n = (s.prompt ? 512 : 1024) / units;
   n = n > most ? most : n;
   s.splits = (int)(n < 1 ? 1 : n);
