@@ -10,6 +10,9 @@ namespace {
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
@@ -29,6 +32,23 @@ __device__ __forceinline__ float power(float dot, float top, float down) {
 __device__ __forceinline__ half2v low_nibbles(uint32_t w) { return __builtin_bit_cast(half2v, (w & 0x000F000Fu) | 0x64006400u); }
 __device__ __forceinline__ half2v high_nibbles(uint32_t w) { return __builtin_bit_cast(half2v, (w & 0x00F000F0u) | 0x64006400u); }
 __device__ __forceinline__ half2v both(float v) { return half2v{(_Float16)v, (_Float16)v}; }
+
+// Elements i and i + 1 of the operand p from two probabilities, as one fp16
+// number each (rounded toward zero, in one instruction) or two that add up to
+// it; returns the sum of what the operand holds, so that the weights of a row
+// add up to one and the rounding's bias cancels.
+template <int PARTS>
+__device__ __forceinline__ float add_pair(float v0, float v1, int i, half8 (&p)[PARTS]) {
+  const half2v one = both(1.0f), h = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(v0, v1));
+  p[0][i] = h[0], p[0][i + 1] = h[1];
+  float sum = __builtin_amdgcn_fdot2(h, one, 0.0f, false);
+  if constexpr (PARTS == 2) {
+    const half2v rest = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(v0 - (float)h[0], v1 - (float)h[1]));
+    p[1][i] = rest[0], p[1][i + 1] = rest[1];
+    sum = __builtin_amdgcn_fdot2(rest, one, sum, false);
+  }
+  return sum;
+}
 
 // A row of q goes to fp16 times a power of two that brings its largest element
 // to 2^9 .. 2^10 (and the sign of the scale).  Its dot products times `unit`,
@@ -77,7 +97,7 @@ __device__ __forceinline__ float sum_over_j(float v) {
 // A workgroup's split, block of rows and (sequence, kv head), in this order in a
 // launch's one dimension.  Workgroups go to the XCDs, and there to the shader
 // engines, in turn: with the sequences in the first place four of them, one
-// long, put all of its work on one engine of each XCD (682 us instead of 239
+// long, put all of its work on one engine of each XCD (682 us instead of 240
 // for prompts of 2048 tokens over 2048 and three shorter ones).
 struct Place {
   int split, block, seq, kv_head;
@@ -121,7 +141,7 @@ __device__ __forceinline__ Seq sequence(const KvAttnArgs &a, int b, int group) {
 // are exact in fp16; q (and p, in fp32 calls) is one fp16 number or, for fp32
 // calls, the sum of two.
 template <int D, typename T>
-__global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attention_kernel(KvAttnArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
   constexpr int KW = D / 32;   // words of codes of a lane's part of a key, steps of the dot product
   constexpr int NU = D / 16;   // output blocks of 16 dimensions
@@ -135,6 +155,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
   const int group = a.heads / a.kv.kv_heads;
   const Seq seq = sequence(a, b, group);
   const size_t page_bytes = (size_t)(D * 9 / 8) << a.kv.page_log2;
+  const uint32_t values = (uint32_t)(D / 2) << a.kv.page_log2, kmetas = 2 * values, vmetas = kmetas + ((uint32_t)(D / 16) << a.kv.page_log2);
   const int32_t *table = a.kv.page_table + b * a.kv.table_stride;
   const int page_mask = (1 << a.kv.page_log2) - 1;
   const float factor = exponent_factor(a.scale);
@@ -171,80 +192,112 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
 
     float m = -__builtin_inff(), l = 0.0f;
     floatx4 o[NU] = {};
-    for (int t0 = (split * kWaves + wave) * kTile; t0 < end; t0 += a.splits * kWaves * kTile) {
-      float s[2][4];
-      uint32_t vw[2][4], vm[2][4];   // value words and metas of the lane's eight tokens
-      const int c = r, oct = D == 64 ? c & 7 : c;
+    // The bytes of a block, by halves of 16 tokens (whose page is the wave's):
+    // of key `at + r` dimensions (D / 4) j .., of values `at + 4 j ..` the octet
+    // of dimensions that the lane's output rows lie in.
+    const int c = r;
+    const uint32_t oct = D == 64 ? c & 7 : c;
+    uint32_t kw[2][KW], km[2], vw[2][4];
+    u32x2 vm[2];
+    bool held[2], next_held[2];
+    int page[2];
+    auto find = [&](int t0) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int at = t0 + 16 * h, in_page = at & page_mask;
-        int page = (at >> a.kv.page_log2) < a.kv.table_cols ? table[at >> a.kv.page_log2] : -1;
-        page = __builtin_amdgcn_readfirstlane(page);
-        const bool held = page >= 0 && page < a.kv.pages;
-        const uint8_t *rec = a.kv.pool + ((size_t)(held ? page : 0) * a.kv.kv_heads + g) * page_bytes;
-        const uint8_t *metas = rec + ((size_t)D << a.kv.page_log2);
-        // keys: lane (r, j) has dimensions (D / 4) j .. of token at + r
-        uint32_t kw[KW];
-        const uint8_t *kp = rec + (size_t)(in_page + r) * (D / 2) + (D / 8) * j;
-        if constexpr (KW == 4) *reinterpret_cast<uint4 *>(kw) = *reinterpret_cast<const uint4 *>(kp);
-        else *reinterpret_cast<uint2 *>(kw) = *reinterpret_cast<const uint2 *>(kp);
-        const uint32_t km = *reinterpret_cast<const uint16_t *>(metas + (in_page + r) * (D / 16) + (D == 128 ? j : j / 2) * 2);
-        // values: lane (c, j) has dimensions 8 oct .. of tokens at + 4 j ..
-        const int quad = (in_page >> 2) + j;
-        *reinterpret_cast<uint4 *>(vw[h]) = *reinterpret_cast<const uint4 *>(
-            rec + ((size_t)(D / 2) << a.kv.page_log2) + (size_t)quad * (2 * D) + oct * 16);
-        const uint2 mm = *reinterpret_cast<const uint2 *>(metas + ((size_t)(D / 16) << a.kv.page_log2) + quad * (D / 4) + (oct / 4) * 8);
-        vm[h][0] = mm.x & 0xFFFF, vm[h][1] = mm.x >> 16, vm[h][2] = mm.y & 0xFFFF, vm[h][3] = mm.y >> 16;
-
-        const float z = (float)(km & 255);
-        const half2v scale = both(meta_scale(km)), low = both(-1024.0f - z), high = both(-64.0f - z);
+        const int col = (t0 + 16 * h) >> a.kv.page_log2;
+        page[h] = __builtin_amdgcn_readfirstlane(col < a.kv.table_cols ? table[col] : -1);
+      }
+    };
+    auto record = [&](int h) {
+      next_held[h] = page[h] >= 0 && page[h] < a.kv.pages;
+      return a.kv.pool + ((size_t)(next_held[h] ? page[h] : 0) * a.kv.kv_heads + g) * page_bytes;
+    };
+    auto fetch_keys = [&](int t0) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t *rec = record(h);
+        const uint32_t in = (t0 + 16 * h) & page_mask;
+        const uint8_t *kp = rec + (in + r) * (D / 2) + (D / 8) * j;
+        if constexpr (KW == 4) *reinterpret_cast<u32x4 *>(kw[h]) = *reinterpret_cast<const u32x4 *>(kp);
+        else *reinterpret_cast<u32x2 *>(kw[h]) = *reinterpret_cast<const u32x2 *>(kp);
+        km[h] = *reinterpret_cast<const uint16_t *>(rec + kmetas + (in + r) * (D / 16) + (D == 128 ? j : j / 2) * 2);
+      }
+    };
+    auto fetch_values = [&](int t0) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint8_t *rec = record(h);
+        const uint32_t quad = (((t0 + 16 * h) & page_mask) >> 2) + j;
+        *reinterpret_cast<u32x4 *>(vw[h]) = *reinterpret_cast<const u32x4 *>(rec + values + quad * (2 * D) + oct * 16);
+        vm[h] = *reinterpret_cast<const u32x2 *>(rec + vmetas + quad * (D / 4) + oct / 4 * 8);
+      }
+    };
+    const int step = a.splits * kWaves * kTile;
+    int t0 = (split * kWaves + wave) * kTile;
+    if (t0 < end) {
+      find(t0);
+      fetch_keys(t0);
+      fetch_values(t0);
+      if (t0 + step < end) find(t0 + step);
+    }
+    for (; t0 < end; t0 += step) {
+      const bool more = t0 + step < end;
+      float s[2][4];
+      held[0] = next_held[0], held[1] = next_held[1];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = t0 + 16 * h;
+        const float z = (float)(km[h] & 255);
+        const half2v scale = both(meta_scale(km[h])), low = both(-1024.0f - z), high = both(-64.0f - z);
         floatx4 acc = {};
 #pragma unroll
         for (int t = 0; t < KW; ++t) {
-          const half8 k = key_values(kw[t], low, high, scale);
+          const half8 k = key_values(kw[h][t], low, high, scale);
 #pragma unroll
           for (int p = PARTS - 1; p >= 0; --p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[p][t], acc, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[h][i] = held && at + 4 * j + i <= last ? acc[i] : -__builtin_inff();
-        // tokens that no row of the tile sees must not reach the products, whatever their bytes are
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!held || at + 4 * j + i >= end) vm[h][i] = 0;
+        for (int i = 0; i < 4; ++i) s[h][i] = held[h] && at + 4 * j + i <= last ? acc[i] : -__builtin_inff();
       }
+      if (more) fetch_keys(t0 + step);
       // softmax of the block
       float top = s[0][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i / 4][i % 4]);
       top = fmaxf(m, max_over_j(top));
       const float ref = top == -__builtin_inff() ? 0.0f : top;
-      const float keep = __builtin_amdgcn_exp2f((m - ref) * down);
+      if (__builtin_amdgcn_ballot_w64(top > m)) {
+        const float keep = __builtin_amdgcn_exp2f((m - ref) * down);
+        l *= keep;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) o[u] *= keep;
+      }
       m = top;
       half8 p[PARTS];
-      float add = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float v = power(s[i / 4][i % 4], ref, down);
-        p[0][i] = (_Float16)v;
-        float used = (float)p[0][i];
-        if constexpr (PARTS == 2) {
-          p[1][i] = (_Float16)(v - used);
-          used += (float)p[1][i];
-        }
-        add += used;
+      for (int i = 0; i < 8; i += 2) {
+        const float v0 = power(s[i / 4][i % 4], ref, down), v1 = power(s[i / 4][i % 4 + 1], ref, down);
+        l += add_pair<PARTS>(v0, v1, i, p);
       }
-      l = l * keep + add;
-#pragma unroll
-      for (int u = 0; u < NU; ++u) o[u] *= keep;
-      // values: word of token e, dimension u in nibble u
+      // values: word of token e, dimension u in nibble u; tokens that no row of
+      // the tile sees must not reach the products, whatever their bytes are
+      const bool inside = held[0] && held[1] && t0 + kTile <= end;
       half2v scale[4], low[4], high[4];
+      uint32_t metas[4];   // of two tokens each
       bool marked = false;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t m0 = vm[e / 2][e % 2 * 2], m1 = vm[e / 2][e % 2 * 2 + 1];
-        marked |= (m0 >> 8) == 255 || (m1 >> 8) == 255;
-        scale[e] = half2v{(_Float16)__uint_as_float(((m0 >> 8) + 848) << 20), (_Float16)__uint_as_float(((m1 >> 8) + 848) << 20)};
-        const half2v z = half2v{(_Float16)(float)(m0 & 255), (_Float16)(float)(m1 & 255)};
+        uint32_t two = vm[e / 2][e % 2];
+        if (!inside) {
+          const int at = t0 + 16 * (e / 2) + 4 * j + 2 * (e % 2);
+          if (!held[e / 2] || at >= end) two = 0;
+          else if (at + 1 >= end) two &= 0xFFFF;
+        }
+        metas[e] = two;
+        const uint32_t k0 = two >> 8 & 255, k1 = two >> 24;
+        marked |= k0 == 255 || k1 == 255;
+        scale[e] = half2v{(_Float16)__uint_as_float((k0 + 848) << 20), (_Float16)__uint_as_float((k1 + 848) << 20)};
+        const half2v z = half2v{(_Float16)(float)(two & 255), (_Float16)(float)(two >> 16 & 255)};
         low[e] = both(-1024.0f) - z;
         high[e] = both(-64.0f) - z;
       }
@@ -271,6 +324,10 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
           o[2 * bt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[part], o[2 * bt + 1], 0, 0, 0);
         }
       }
+      if (more) {
+        fetch_values(t0 + step);
+        if (t0 + 2 * step < end) find(t0 + 2 * step);
+      }
       // A group marked as not stored counts as NaN for the rows that see it and
       // must not touch the others, which multiply it with a zero.  It took part
       // above with a finite scale; here the marked tokens that a row sees are
@@ -279,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
         half8 mark, seen;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          mark[e] = (_Float16)((vm[e / 4][e % 4] >> 8) == 255 ? 1.0f : 0.0f);
+          mark[e] = (_Float16)((metas[e / 2] >> (16 * (e % 2) + 8) & 255) == 255 ? 1.0f : 0.0f);
           seen[e] = (_Float16)(t0 + 16 * (e / 4) + 4 * j + e % 4 <= last ? 1.0f : 0.0f);
         }
         floatx4 count = {};
@@ -354,10 +411,6 @@ __global__ __launch_bounds__(kThreads) void kv4_attention_kernel(KvAttnArgs a) {
 // order.  Two tiles of LDS, one barrier a tile; the bytes of the tile after
 // next are on their way to registers.
 constexpr int kPromptTile = 64, kPromptRows = 128;
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 // Maximum and sum of the two lanes that share a row.
 __device__ __forceinline__ float max_of_halves(float v) { return fmaxf(v, __shfl_xor(v, 32, kWave)); }
 
@@ -370,7 +423,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
   constexpr int KB = 32 * D * 2;       // LDS bytes of 32 keys, or of 32 values
   __shared__ __align__(16) uint8_t s_kv[2][4 * KB];          // keys of both blocks, values of both
   __shared__ __align__(16) uint8_t s_mark[2][D / 32][kPromptTile];  // value groups that are marked as not stored
-  __shared__ uint32_t s_any[2][kWaves];
+  __shared__ __align__(16) uint32_t s_any[2][kWaves];        // bit 0: marks in the wave's share, bit 1: a page is missing
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane & 31, hi = lane >> 5;
@@ -379,7 +432,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
   const int group = a.heads / a.kv.kv_heads;
   const Seq seq = sequence(a, b, group);
   const size_t page_bytes = (size_t)(D * 9 / 8) << a.kv.page_log2;
-  const size_t values = (size_t)(D / 2) << a.kv.page_log2, kmetas = (size_t)D << a.kv.page_log2, vmetas = kmetas + ((size_t)(D / 16) << a.kv.page_log2);
+  const uint32_t values = (uint32_t)(D / 2) << a.kv.page_log2, kmetas = 2 * values, vmetas = kmetas + ((uint32_t)(D / 16) << a.kv.page_log2);
   const int32_t *table = a.kv.page_table + b * a.kv.table_stride;
   const int page_mask = (1 << a.kv.page_log2) - 1;
   const int stride = a.splits * kPromptTile;
@@ -437,24 +490,24 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
     uint32_t kw[KW], km;
     u32x4 vw[2];
     u32x2 vm[2];
-    bool k_held, v_held;
+    bool v_held, both_held;
     auto fetch = [&](int t0) {
       const int sub = t0 + 32 * (wave & 1);
       bool h0, h1;
       const uint8_t *p0 = page_of(sub, h0), *p1 = page_of(sub + 16, h1);
       const uint8_t *rec = r < 16 ? p0 : p1;
-      k_held = r < 16 ? h0 : h1;
-      const int in = (sub + r) & page_mask, part = 2 * (wave >> 1) + hi;
-      const uint8_t *kp = rec + (size_t)in * (D / 2) + KW * 4 * part;
+      const uint32_t in = (sub + r) & page_mask, part = 2 * (wave >> 1) + hi;
+      const uint8_t *kp = rec + in * (D / 2) + KW * 4 * part;
       if constexpr (KW == 4) *reinterpret_cast<u32x4 *>(kw) = *reinterpret_cast<const u32x4 *>(kp);
       else *reinterpret_cast<u32x2 *>(kw) = *reinterpret_cast<const u32x2 *>(kp);
       km = *reinterpret_cast<const uint16_t *>(rec + kmetas + in * (D / 16) + (D == 128 ? part : part / 2) * 2);
       const uint8_t *vrec = wave >> 1 ? p1 : p0;
       v_held = wave >> 1 ? h1 : h0;
-      const int quad = (((sub + 16 * (wave >> 1)) & page_mask) >> 2) + hi, oct = r / (8 / NB);
+      both_held = h0 && h1;
+      const uint32_t quad = (((sub + 16 * (wave >> 1)) & page_mask) >> 2) + hi, oct = (uint32_t)r / (8 / NB);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        vw[x] = *reinterpret_cast<const u32x4 *>(vrec + values + (size_t)(quad + 2 * x) * (2 * D) + oct * 16);
+        vw[x] = *reinterpret_cast<const u32x4 *>(vrec + values + (quad + 2 * x) * (2 * D) + oct * 16);
         vm[x] = *reinterpret_cast<const u32x2 *>(vrec + vmetas + (quad + 2 * x) * (D / 4) + oct / 4 * 8);
       }
     };
@@ -506,7 +559,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
         *reinterpret_cast<half8 *>(at + (2 * bt + 1) * 2048) = v1;
       }
       const uint64_t any = __builtin_amdgcn_ballot_w64(marks[0] | marks[1]);
-      if (lane == 0) s_any[buf][wave] = any != 0;
+      if (lane == 0) s_any[buf][wave] = (any ? 1u : 0u) | (both_held ? 0u : 2u);
       if (r % 8 == 0) {   // a lane of each group of 32 dimensions (D 64: of each half)
         const int grp = r / (8 / NB) / 4;
         uint8_t *mp = &s_mark[buf][grp][32 * (wave & 1) + 16 * (wave >> 1) + 4 * hi];
@@ -515,20 +568,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
       }
     };
 
-    int t0 = split * kPromptTile, buf = 0;
-    if (t0 < end) {
-      fetch(t0);
-      stage(t0, 0);
-      if (t0 + stride < end) fetch(t0 + stride);
-    }
-    for (; t0 < end; t0 += stride, buf ^= 1) {
-      __syncthreads();
+    // the first pass only stages; t0 is then negative
+    int t0 = (split - a.splits) * kPromptTile, buf = 1;
+    if (t0 + stride < end) fetch(t0 + stride);
+    for (; t0 < end; t0 += stride, buf ^= 1, __syncthreads()) {
       const uint8_t *from = s_kv[buf];
       if (t0 + stride < end) {
         stage(t0 + stride, buf ^ 1);
         if (t0 + 2 * stride < end) fetch(t0 + 2 * stride);
       }
-      if (t0 >= wend) continue;
+      if (t0 < 0 || t0 >= wend) continue;
       __builtin_amdgcn_sched_barrier(0);   // staging's registers are free again before the scores take theirs
       floatx16 s[2];
 #pragma unroll
@@ -543,21 +592,19 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
           for (int p = PARTS - 1; p >= 0; --p) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[p][t], s[x], 0, 0, 0);
         }
       }
-      bool whole = t0 + kPromptTile - 1 <= wfirst;
-      bool held[4];
+      const u32x4 any4 = *reinterpret_cast<const u32x4 *>(s_any[buf]);
+      const uint32_t any = __builtin_amdgcn_readfirstlane(any4[0] | any4[1] | any4[2] | any4[3]);
+      if (t0 + kPromptTile - 1 > wfirst || (any & 2)) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        page_of(t0 + 16 * x, held[x]);
-        whole &= held[x];
-      }
-      if (!whole) {
+        for (int x = 0; x < 4; ++x) {
+          bool held;
+          page_of(t0 + 16 * x, held);
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int at = 32 * x + 8 * (i / 4) + 4 * hi + i % 4;
-            if (t0 + at > last || !held[2 * x + i / 8]) s[x][i] = -__builtin_inff();
+          for (int i = 0; i < 8; ++i) {
+            const int at = t0 + 16 * x + 8 * (i / 4) + 4 * hi + i % 4;
+            if (at > last || !held) s[x / 2][8 * (x % 2) + i] = -__builtin_inff();
           }
+        }
       }
       float top = m;
 #pragma unroll
@@ -573,24 +620,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
         for (int u = 0; u < NB; ++u) o[u] *= keep;
       }
       m = top;
-      const half2v one = both(1.0f);
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           half8 p[PARTS];
 #pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            const float v0 = power(s[x][8 * h + e], ref, rs.down), v1 = power(s[x][8 * h + e + 1], ref, rs.down);
-            const half2v hp = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(v0, v1));
-            p[0][e] = hp[0], p[0][e + 1] = hp[1];
-            l = __builtin_amdgcn_fdot2(hp, one, l, false);
-            if constexpr (PARTS == 2) {
-              const half2v lp = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(v0 - (float)hp[0], v1 - (float)hp[1]));
-              p[1][e] = lp[0], p[1][e + 1] = lp[1];
-              l = __builtin_amdgcn_fdot2(lp, one, l, false);
-            }
-          }
+          for (int e = 0; e < 8; e += 2)
+            l += add_pair<PARTS>(power(s[x][8 * h + e], ref, rs.down), power(s[x][8 * h + e + 1], ref, rs.down), e, p);
 #pragma unroll
           for (int u = 0; u < NB; ++u) {
             const half8 v = *reinterpret_cast<const half8 *>(from + 2 * KB + x * KB + u * 2048 + h * 1024 + lane * 16);
@@ -600,7 +637,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
         }
       // Groups marked as not stored: counted for the rows that see them, as in
       // the kernel above.
-      if (s_any[buf][0] | s_any[buf][1] | s_any[buf][2] | s_any[buf][3]) {
+      if (any & 1) {
         floatx16 count;
 #pragma unroll
         for (int i = 0; i < 16; ++i) count[i] = 0.0f;
@@ -622,7 +659,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
           for (int i = 0; i < 16; ++i) o[u][i] = count[i] > 0.0f ? __builtin_nanf("") : o[u][i];
       }
     }
-    __syncthreads();   // the tiles of the next block of rows go to the same LDS
     l += __shfl_xor(l, 32, kWave);
     if (wrow + r >= seq.rows) continue;
     const int64_t at = (int64_t)split * a.kv.tokens * a.heads + (int64_t)token * a.heads + head;
@@ -649,15 +685,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
   }
 }
 
-// Joins the splits of a row, D / 4 lanes over its dimensions.  With WIDE a
-// workgroup has one row and its groups of lanes share out the splits (few rows,
-// many splits); otherwise every group has a row of its own.
+// Joins the splits of a row.  With WIDE a workgroup has 32 dimensions of one row
+// and its groups of 8 lanes share out the splits (few rows, many splits);
+// otherwise D / 4 lanes take a row.
 template <int D, typename T, bool WIDE>
 __global__ __launch_bounds__(kThreads) void kv4_join_kernel(KvAttnArgs a) {
-  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
+  constexpr int kLanes = WIDE ? 8 : D / 4, kGroups = kThreads / kLanes;
   const int64_t rows = (int64_t)a.kv.tokens * a.heads;
-  const int grp = threadIdx.x / kLanes, dim = threadIdx.x % kLanes * 4;
-  const int64_t row = WIDE ? blockIdx.x : (int64_t)blockIdx.x * kGroups + grp;
+  const int grp = threadIdx.x / kLanes, dim = threadIdx.x % kLanes * 4 + (WIDE ? blockIdx.x % (D / 32) * 32 : 0);
+  const int64_t row = WIDE ? blockIdx.x / (D / 32) : (int64_t)blockIdx.x * kGroups + grp;
   if (row >= rows) return;
   const float factor = exponent_factor(a.scale);
   const float2 *ml = reinterpret_cast<const float2 *>(a.ml) + row;
@@ -684,13 +720,13 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(KvAttnArgs a) {
   if constexpr (WIDE) {
     __shared__ float4 s_acc[kGroups][kLanes];
     __shared__ float s_total[kGroups];
-    s_acc[grp][dim / 4] = acc;
-    if (dim == 0) s_total[grp] = total;
+    s_acc[grp][dim / 4 % kLanes] = acc;
+    if (threadIdx.x % kLanes == 0) s_total[grp] = total;
     __syncthreads();
     if (grp) return;
 #pragma unroll
     for (int i = 1; i < kGroups; ++i) {
-      const float4 o = s_acc[i][dim / 4];
+      const float4 o = s_acc[i][dim / 4 % kLanes];
       total += s_total[i];
       acc.x += o.x, acc.y += o.y, acc.z += o.z, acc.w += o.w;
     }
@@ -709,7 +745,7 @@ void launch(const KvAttnArgs &a, hipStream_t s) {
   if (a.splits == 1) return;
   const int64_t rows = (int64_t)a.kv.tokens * a.heads;
   constexpr int kGroups = kThreads / (D / 4);
-  if (a.splits >= kGroups) hipLaunchKernelGGL((kv4_join_kernel<D, T, true>), dim3((unsigned)rows), dim3(kThreads), 0, s, a);
+  if (a.splits >= 16) hipLaunchKernelGGL((kv4_join_kernel<D, T, true>), dim3((unsigned)(rows * (D / 32))), dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL((kv4_join_kernel<D, T, false>), dim3((unsigned)((rows + kGroups - 1) / kGroups)), dim3(kThreads), 0, s, a);
 }
 
