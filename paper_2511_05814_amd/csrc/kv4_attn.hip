@@ -35,19 +35,18 @@ __device__ __forceinline__ half2v both(float v) { return half2v{(_Float16)v, (_F
 
 // Elements i and i + 1 of the operand p from two probabilities, as one fp16
 // number each (rounded toward zero, in one instruction) or two that add up to
-// it; returns the sum of what the operand holds, so that the weights of a row
-// add up to one and the rounding's bias cancels.
+// it; adds what the operand holds to `sum`, so that the weights of a row add up
+// to one and the rounding's bias cancels.
 template <int PARTS>
-__device__ __forceinline__ float add_pair(float v0, float v1, int i, half8 (&p)[PARTS]) {
+__device__ __forceinline__ void add_pair(float v0, float v1, int i, half8 (&p)[PARTS], float &sum) {
   const half2v one = both(1.0f), h = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(v0, v1));
   p[0][i] = h[0], p[0][i + 1] = h[1];
-  float sum = __builtin_amdgcn_fdot2(h, one, 0.0f, false);
+  sum = __builtin_amdgcn_fdot2(h, one, sum, false);
   if constexpr (PARTS == 2) {
     const half2v rest = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(v0 - (float)h[0], v1 - (float)h[1]));
     p[1][i] = rest[0], p[1][i + 1] = rest[1];
     sum = __builtin_amdgcn_fdot2(rest, one, sum, false);
   }
-  return sum;
 }
 
 // A row of q goes to fp16 times a power of two that brings its largest element
@@ -73,25 +72,117 @@ __device__ __forceinline__ float meta_scale(uint32_t meta) {
   return k == 255 ? __builtin_nanf("") : __uint_as_float((k + 848) << 20);
 }
 
+// What two metas (uint16 k << 8 | z each) turn codes into values with.
+struct Pair {
+  half2v scale, low, high;   // of 1024 + q: + low, times scale; of 1024 + 16 q: / 16 + high, times scale
+};
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+// For 8 <= k < 248, k << 7 are the bits of scale(k) * 2^6 in fp16.  `far` grows to
+// 0x7800 or more in the half of a k outside that range (a step below 2^-20 or
+// from 2^10 on, or a mark), for which far_pair has the scale.
+__device__ __forceinline__ Pair pair_of(uint32_t two, ushort2v &far) {
+  const uint32_t k = two >> 1 & 0x7F807F80u;
+  far = __builtin_elementwise_max(far, (ushort2v)(__builtin_bit_cast(ushort2v, k) - (unsigned short)0x0400));
+  Pair p;
+  p.scale = __builtin_bit_cast(half2v, k) * both(0.015625f);
+  p.low = __builtin_bit_cast(half2v, (two & 0x00FF00FFu) | 0xE400E400u);        // -(1024 + z)
+  p.high = __builtin_bit_cast(half2v, (two << 4 & 0x0FF00FF0u) | 0xD400D400u);  // -(64 + z)
+  return p;
+}
+__device__ __forceinline__ bool is_far(ushort2v far) { return far[0] >= 0x7800 || far[1] >= 0x7800; }
+constexpr uint32_t kPlainMeta = 8u << 8;   // k = 8, z = 0
+
 // Eight key codes as fp16 values, dimensions in the order 0 4 1 5 2 6 3 7.
 // Every step is exact.
-__device__ __forceinline__ half8 key_values(uint32_t w, half2v minus_low, half2v minus_high, half2v scale) {
+__device__ __forceinline__ half8 key_values(uint32_t w, const Pair &m) {
   const half2v sixteenth = both(0.0625f);
   half2v v[4];
-  v[0] = (low_nibbles(w) + minus_low) * scale;
-  v[1] = __builtin_elementwise_fma(high_nibbles(w), sixteenth, minus_high) * scale;
-  v[2] = (low_nibbles(w >> 8) + minus_low) * scale;
-  v[3] = __builtin_elementwise_fma(high_nibbles(w >> 8), sixteenth, minus_high) * scale;
+  v[0] = (low_nibbles(w) + m.low) * m.scale;
+  v[1] = __builtin_elementwise_fma(high_nibbles(w), sixteenth, m.high) * m.scale;
+  v[2] = (low_nibbles(w >> 8) + m.low) * m.scale;
+  v[3] = __builtin_elementwise_fma(high_nibbles(w >> 8), sixteenth, m.high) * m.scale;
   return half8{v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
 }
 
+// The meta of a key's group, for both halves of a pair; NaN where it is marked.
+__device__ __forceinline__ Pair key_pair(uint32_t meta) {
+  ushort2v far = {0, 0};
+  Pair p = pair_of(meta | meta << 16, far);
+  if (__builtin_amdgcn_ballot_w64(is_far(far)) != 0) p.scale = both(meta_scale(meta));
+  return p;
+}
+
+// What four pairs of metas of a lane's eight value tokens say.  Returns whether
+// one is marked as not stored; its values are finite all the same.
+__device__ __forceinline__ bool value_pairs(const uint32_t (&two)[4], Pair (&p)[4]) {
+  ushort2v far = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) p[e] = pair_of(two[e], far);
+  bool marked = false;
+  if (__builtin_amdgcn_ballot_w64(is_far(far)) != 0) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t k0 = two[e] >> 8 & 255, k1 = two[e] >> 24;
+      marked |= k0 == 255 || k1 == 255;
+      p[e].scale = half2v{(_Float16)__uint_as_float((k0 + 848) << 20), (_Float16)__uint_as_float((k1 + 848) << 20)};
+    }
+  }
+  return marked;
+}
+
+// Two dimensions (the nibbles of a byte) of eight tokens as fp16 values;
+// `pick`: that byte of two tokens' words, each in a half.
+__device__ __forceinline__ void value_byte(const u32x4 (&w)[2], uint32_t pick, const Pair (&p)[4], half8 &v0, half8 &v1) {
+  const half2v sixteenth = both(0.0625f);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t x = __builtin_amdgcn_perm(w[e / 2][e % 2 * 2 + 1], w[e / 2][e % 2 * 2], pick);
+    const half2v a0 = (low_nibbles(x) + p[e].low) * p[e].scale;
+    const half2v a1 = __builtin_elementwise_fma(high_nibbles(x), sixteenth, p[e].high) * p[e].scale;
+    v0[2 * e] = a0[0], v0[2 * e + 1] = a0[1];
+    v1[2 * e] = a1[0], v1[2 * e + 1] = a1[1];
+  }
+}
+__device__ __forceinline__ uint32_t pick_byte(uint32_t b) { return 0x0C000C00u | b | (b + 4) << 16; }
+
+// Metas of tokens at .. at + 1 that may lie at or past `end`, or on no page.
+__device__ __forceinline__ uint32_t inside(uint32_t two, int at, int end) {
+  if (at >= end) return kPlainMeta | kPlainMeta << 16;
+  return at + 1 >= end ? (two & 0xFFFF) | kPlainMeta << 16 : two;
+}
+
+// The other operand of a reduction over lanes i and i ^ 32 (i ^ 16), without the
+// LDS: the halves (the rows of 16 lanes) of a copy swapped.
+__device__ __forceinline__ void swap32(float v, float &a, float &b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  a = __uint_as_float(r[0]);
+  b = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ void swap16(float v, float &a, float &b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  a = __uint_as_float(r[0]);
+  b = __uint_as_float(r[1]);
+}
+// Over the two lanes of a row of 32, and the four of a row of 16.
+__device__ __forceinline__ float max_of_halves(float v) {
+  float a, b;
+  swap32(v, a, b);
+  return fmaxf(a, b);
+}
+__device__ __forceinline__ float sum_of_halves(float v) {
+  float a, b;
+  swap32(v, a, b);
+  return a + b;
+}
 __device__ __forceinline__ float max_over_j(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, kWave));
-  return fmaxf(v, __shfl_xor(v, 32, kWave));
+  float a, b;
+  swap16(v, a, b);
+  return max_of_halves(fmaxf(a, b));
 }
 __device__ __forceinline__ float sum_over_j(float v) {
-  v += __shfl_xor(v, 16, kWave);
-  return v + __shfl_xor(v, 32, kWave);
+  float a, b;
+  swap16(v, a, b);
+  return sum_of_halves(a + b);
 }
 
 // A workgroup's split, block of rows and (sequence, kv head), in this order in a
@@ -164,6 +255,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
     const int row = min(row0 + r, seq.rows - 1);
     const int token = seq.start + row / group, head = g * group + row % group;
     const int last = min(seq.first + row / group, seq.held - 1);  // this row's last position
+    const int least = min(seq.first + row0 / group, seq.held - 1);  // the first row's
     const int end = min(seq.first + (min(row0 + 15, seq.rows - 1)) / group, seq.held - 1) + 1;
 
     // the row of q, scaled by a power of two to a largest value of 2^9 .. 2^10
@@ -197,10 +289,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
     // of dimensions that the lane's output rows lie in.
     const int c = r;
     const uint32_t oct = D == 64 ? c & 7 : c;
-    uint32_t kw[2][KW], km[2], vw[2][4];
+    uint32_t kw[2][KW], km[2];
+    u32x4 vw[2];
     u32x2 vm[2];
     bool held[2], next_held[2];
     int page[2];
+    const uint32_t k_lane = r * (D / 2) + (D / 8) * j, km_lane = kmetas + r * (D / 16) + (D == 128 ? j : j / 2) * 2;
+    const uint32_t v_lane = values + j * (2 * D) + oct * 16, vm_lane = vmetas + j * (D / 4) + oct / 4 * 8;
     auto find = [&](int t0) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -217,21 +312,23 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
       for (int h = 0; h < 2; ++h) {
         const uint8_t *rec = record(h);
         const uint32_t in = (t0 + 16 * h) & page_mask;
-        const uint8_t *kp = rec + (in + r) * (D / 2) + (D / 8) * j;
+        const uint8_t *kp = rec + in * (D / 2) + k_lane;
         if constexpr (KW == 4) *reinterpret_cast<u32x4 *>(kw[h]) = *reinterpret_cast<const u32x4 *>(kp);
         else *reinterpret_cast<u32x2 *>(kw[h]) = *reinterpret_cast<const u32x2 *>(kp);
-        km[h] = *reinterpret_cast<const uint16_t *>(rec + kmetas + (in + r) * (D / 16) + (D == 128 ? j : j / 2) * 2);
+        km[h] = *reinterpret_cast<const uint16_t *>(rec + in * (D / 16) + km_lane);
       }
     };
     auto fetch_values = [&](int t0) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint8_t *rec = record(h);
-        const uint32_t quad = (((t0 + 16 * h) & page_mask) >> 2) + j;
-        *reinterpret_cast<u32x4 *>(vw[h]) = *reinterpret_cast<const u32x4 *>(rec + values + quad * (2 * D) + oct * 16);
-        vm[h] = *reinterpret_cast<const u32x2 *>(rec + vmetas + quad * (D / 4) + oct / 4 * 8);
+        const uint32_t in = (t0 + 16 * h) & page_mask;
+        vw[h] = *reinterpret_cast<const u32x4 *>(rec + in * (D / 2) + v_lane);
+        vm[h] = *reinterpret_cast<const u32x2 *>(rec + in * (D / 16) + vm_lane);
       }
     };
+    // D 64: lanes 8 .. 15 of a row take dimensions 4 .. 7 of their octet
+    const uint32_t first_byte = pick_byte(D == 64 ? (c >> 3) * 2 : 0);
     const int step = a.splits * kWaves * kTile;
     int t0 = (split * kWaves + wave) * kTile;
     if (t0 < end) {
@@ -246,18 +343,24 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
       held[0] = next_held[0], held[1] = next_held[1];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int at = t0 + 16 * h;
-        const float z = (float)(km[h] & 255);
-        const half2v scale = both(meta_scale(km[h])), low = both(-1024.0f - z), high = both(-64.0f - z);
+        const Pair km_ = key_pair(km[h]);
         floatx4 acc = {};
 #pragma unroll
         for (int t = 0; t < KW; ++t) {
-          const half8 k = key_values(kw[h][t], low, high, scale);
+          const half8 k = key_values(kw[h][t], km_);
 #pragma unroll
           for (int p = PARTS - 1; p >= 0; --p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[p][t], acc, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[h][i] = held[h] && at + 4 * j + i <= last ? acc[i] : -__builtin_inff();
+        for (int i = 0; i < 4; ++i) s[h][i] = acc[i];
+      }
+      const bool whole = held[0] && held[1] && t0 + kTile - 1 <= least;
+      if (!whole) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!held[h] || t0 + 16 * h + 4 * j + i > last) s[h][i] = -__builtin_inff();
       }
       if (more) fetch_keys(t0 + step);
       // softmax of the block
@@ -277,47 +380,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
         const float v0 = power(s[i / 4][i % 4], ref, down), v1 = power(s[i / 4][i % 4 + 1], ref, down);
-        l += add_pair<PARTS>(v0, v1, i, p);
+        add_pair<PARTS>(v0, v1, i, p, l);
       }
       // values: word of token e, dimension u in nibble u; tokens that no row of
       // the tile sees must not reach the products, whatever their bytes are
-      const bool inside = held[0] && held[1] && t0 + kTile <= end;
-      half2v scale[4], low[4], high[4];
-      uint32_t metas[4];   // of two tokens each
-      bool marked = false;
+      uint32_t metas[4] = {vm[0][0], vm[0][1], vm[1][0], vm[1][1]};   // of two tokens each
+      if (!whole) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        uint32_t two = vm[e / 2][e % 2];
-        if (!inside) {
-          const int at = t0 + 16 * (e / 2) + 4 * j + 2 * (e % 2);
-          if (!held[e / 2] || at >= end) two = 0;
-          else if (at + 1 >= end) two &= 0xFFFF;
-        }
-        metas[e] = two;
-        const uint32_t k0 = two >> 8 & 255, k1 = two >> 24;
-        marked |= k0 == 255 || k1 == 255;
-        scale[e] = half2v{(_Float16)__uint_as_float((k0 + 848) << 20), (_Float16)__uint_as_float((k1 + 848) << 20)};
-        const half2v z = half2v{(_Float16)(float)(two & 255), (_Float16)(float)(two >> 16 & 255)};
-        low[e] = both(-1024.0f) - z;
-        high[e] = both(-64.0f) - z;
+        for (int e = 0; e < 4; ++e) metas[e] = inside(metas[e], t0 + 16 * (e / 2) + 4 * j + 2 * (e % 2), held[e / 2] ? end : 0);
       }
-      const half2v sixteenth = both(0.0625f);
+      Pair pairs[4];
+      const bool marked = value_pairs(metas, pairs);
 #pragma unroll
       for (int bt = 0; bt < NU / 2; ++bt) {
         half8 v0, v1;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          uint32_t w0 = vw[e / 2][e % 2 * 2], w1 = vw[e / 2][e % 2 * 2 + 1];
-          if constexpr (D == 64) {  // lanes 8 .. 15 of a row take dimensions 4 .. 7
-            w0 >>= (c >> 3) * 16;
-            w1 >>= (c >> 3) * 16;
-          }
-          const uint32_t x = __builtin_amdgcn_perm(w1, w0, 0x0C000C00u | bt | (uint32_t)(4 + bt) << 16);
-          const half2v a0 = (low_nibbles(x) + low[e]) * scale[e];
-          const half2v a1 = __builtin_elementwise_fma(high_nibbles(x), sixteenth, high[e]) * scale[e];
-          v0[2 * e] = a0[0], v0[2 * e + 1] = a0[1];
-          v1[2 * e] = a1[0], v1[2 * e + 1] = a1[1];
-        }
+        value_byte(vw, first_byte + bt * 0x00010001u, pairs, v0, v1);
 #pragma unroll
         for (int part = PARTS - 1; part >= 0; --part) {
           o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[part], o[2 * bt], 0, 0, 0);
@@ -411,9 +488,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
 // order.  Two tiles of LDS, one barrier a tile; the bytes of the tile after
 // next are on their way to registers.
 constexpr int kPromptTile = 64, kPromptRows = 128;
-// Maximum and sum of the two lanes that share a row.
-__device__ __forceinline__ float max_of_halves(float v) { return fmaxf(v, __shfl_xor(v, 32, kWave)); }
-
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_kernel(KvAttnArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
@@ -514,57 +588,39 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
     auto stage = [&](int t0, int buf) {
       uint8_t *to = s_kv[buf];
       {
-        const float z = (float)(km & 255);
-        const half2v scale = both(meta_scale(km)), low = both(-1024.0f - z), high = both(-64.0f - z);
+        const Pair pair = key_pair(km);
         const int w0 = KW * (2 * (wave >> 1) + hi);
 #pragma unroll
         for (int x = 0; x < KW; ++x)
-          *reinterpret_cast<half8 *>(to + (wave & 1) * KB + (w0 + x) * 512 + r * 16) = key_values(kw[x], low, high, scale);
+          *reinterpret_cast<half8 *>(to + (wave & 1) * KB + (w0 + x) * 512 + r * 16) = key_values(kw[x], pair);
       }
-      const int tok = t0 + 32 * (wave & 1) + 16 * (wave >> 1) + 4 * hi;
-      half2v scale[4], low[4], high[4];
-      uint32_t marks[2] = {0, 0};
+      // tokens that no row sees must not reach the products, whatever their bytes are
+      uint32_t metas[4] = {vm[0][0], vm[0][1], vm[1][0], vm[1][1]};
+      if (!v_held || t0 + kPromptTile > end) {
+        const int tok = t0 + 32 * (wave & 1) + 16 * (wave >> 1) + 4 * hi;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        uint32_t two[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const int n = 2 * (e & 1) + s;  // token of the quad
-          two[s] = vm[e / 2][n / 2] >> (16 * (n & 1)) & 0xFFFF;
-          // tokens that no row sees must not reach the products, whatever their bytes are
-          if (!v_held || tok + 8 * (e / 2) + n >= end) two[s] = 0;
-          marks[e / 2] |= (two[s] >> 8) == 255 ? 1u << (8 * n) : 0u;
-        }
-        scale[e] = half2v{(_Float16)__uint_as_float(((two[0] >> 8) + 848) << 20), (_Float16)__uint_as_float(((two[1] >> 8) + 848) << 20)};
-        const half2v z = half2v{(_Float16)(float)(two[0] & 255), (_Float16)(float)(two[1] & 255)};
-        low[e] = both(-1024.0f) - z;
-        high[e] = both(-64.0f) - z;
+        for (int e = 0; e < 4; ++e) metas[e] = inside(metas[e], tok + 8 * (e / 2) + 2 * (e % 2), v_held ? end : 0);
       }
-      const half2v sixteenth = both(0.0625f);
-      const int shift = r % (8 / NB) * (4 * NB);
+      Pair pairs[4];
+      const bool marked = value_pairs(metas, pairs);
+      const uint32_t first_byte = pick_byte(r % (8 / NB) * (NB / 2));
 #pragma unroll
       for (int bt = 0; bt < NB / 2; ++bt) {
         half8 v0, v1;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t x0 = vw[e / 2][2 * (e & 1)] >> shift, x1 = vw[e / 2][2 * (e & 1) + 1] >> shift;
-          const uint32_t x = __builtin_amdgcn_perm(x1, x0, 0x0C000C00u | bt | (uint32_t)(4 + bt) << 16);
-          const half2v a0 = (low_nibbles(x) + low[e]) * scale[e];
-          const half2v a1 = __builtin_elementwise_fma(high_nibbles(x), sixteenth, high[e]) * scale[e];
-          v0[2 * e] = a0[0], v0[2 * e + 1] = a0[1];
-          v1[2 * e] = a1[0], v1[2 * e + 1] = a1[1];
-        }
+        value_byte(vw, first_byte + bt * 0x00010001u, pairs, v0, v1);
         uint8_t *at = to + 2 * KB + (wave & 1) * KB + (wave >> 1) * 1024 + lane * 16;
         *reinterpret_cast<half8 *>(at + (2 * bt) * 2048) = v0;
         *reinterpret_cast<half8 *>(at + (2 * bt + 1) * 2048) = v1;
       }
-      const uint64_t any = __builtin_amdgcn_ballot_w64(marks[0] | marks[1]);
+      const bool any = __builtin_amdgcn_ballot_w64(marked) != 0;
       if (lane == 0) s_any[buf][wave] = (any ? 1u : 0u) | (both_held ? 0u : 2u);
       if (r % 8 == 0) {   // a lane of each group of 32 dimensions (D 64: of each half)
-        const int grp = r / (8 / NB) / 4;
-        uint8_t *mp = &s_mark[buf][grp][32 * (wave & 1) + 16 * (wave >> 1) + 4 * hi];
-        *reinterpret_cast<uint32_t *>(mp) = marks[0];
-        *reinterpret_cast<uint32_t *>(mp + 8) = marks[1];
+        uint8_t *mp = &s_mark[buf][r / (8 / NB) / 4][32 * (wave & 1) + 16 * (wave >> 1) + 4 * hi];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t two = metas[e];
+          *reinterpret_cast<uint16_t *>(mp + 8 * (e / 2) + 2 * (e % 2)) = (uint16_t)((two >> 8 & 255) == 255 ? 1 : 0) | (uint16_t)(two >> 24 == 255 ? 256 : 0);
+        }
       }
     };
 
@@ -627,7 +683,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
           half8 p[PARTS];
 #pragma unroll
           for (int e = 0; e < 8; e += 2)
-            l += add_pair<PARTS>(power(s[x][8 * h + e], ref, rs.down), power(s[x][8 * h + e + 1], ref, rs.down), e, p);
+            add_pair<PARTS>(power(s[x][8 * h + e], ref, rs.down), power(s[x][8 * h + e + 1], ref, rs.down), e, p, l);
 #pragma unroll
           for (int u = 0; u < NB; ++u) {
             const half8 v = *reinterpret_cast<const half8 *>(from + 2 * KB + x * KB + u * 2048 + h * 1024 + lane * 16);
@@ -659,7 +715,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
           for (int i = 0; i < 16; ++i) o[u][i] = count[i] > 0.0f ? __builtin_nanf("") : o[u][i];
       }
     }
-    l += __shfl_xor(l, 32, kWave);
+    l = sum_of_halves(l);
     if (wrow + r >= seq.rows) continue;
     const int64_t at = (int64_t)split * a.kv.tokens * a.heads + (int64_t)token * a.heads + head;
     const float inv = a.splits > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;

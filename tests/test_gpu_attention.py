@@ -294,6 +294,29 @@ def test_marked_entries_reach_only_rows_that_see_them(new, D):
         assert np.isnan(o[new - 1, :2]).all() and not np.isnan(o[:, 2:]).any()
 
 
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_with_scales_from_end_to_end(new, D):
+    """Groups whose scale code is any of 0 .. 254: the smallest and the largest
+    steps, among zeros and ordinary ones."""
+    bt = Batch([new, 1], [90, 250], 4, 2, D, 16, seed=13).fill(0.3)
+    rng = np.random.default_rng(13)
+    for page in range(bt.pool.shape[0]):
+        for h in range(2):
+            rec = [np.array(x) for x in oa.unpack_record(bt.pool[page, h], 16, D)]
+            for i in (1, 3):    # a sixth of the groups small, large or all zero
+                pick = rng.random(rec[i].shape)
+                k = np.where(pick < 0.05, rng.integers(0, 10, rec[i].shape), rec[i] >> 8)
+                k = np.where(pick > 0.95, rng.integers(244, 255, rec[i].shape) if i == 3 else k, k)
+                rec[i] = (k << 8 | (rec[i] & 255)).astype(np.uint16)
+                zero = np.repeat((pick > 0.5) & (pick < 0.55), 32, 1)
+                rec[i - 1][zero] = 0
+                rec[i][(pick > 0.5) & (pick < 0.55)] = 0
+            bt.pool[page, h] = oa.record(*rec)
+    for dtype in ("f32", "bf16"):
+        check_attention(bt, dtype)
+
+
 def test_attention_scores_far_apart_and_equal():
     """Softmax where one key takes all, where all are alike, and with scales of either sign or none."""
     bt = Batch([1, 30], [400, 300], 4, 2, 64, 16, seed=9).fill(1.5)
