@@ -29,8 +29,18 @@ __device__ __forceinline__ float power(float dot, float top, float down) {
 
 // Codes of a word that lie 16 bits apart, as pairs of fp16 1024 + q (low
 // nibbles) or 1024 + 16 q (high ones): 0x6400 is 1024, whose last place is 1.
-__device__ __forceinline__ half2v low_nibbles(uint32_t w) { return __builtin_bit_cast(half2v, (w & 0x000F000Fu) | 0x64006400u); }
-__device__ __forceinline__ half2v high_nibbles(uint32_t w) { return __builtin_bit_cast(half2v, (w & 0x00F000F0u) | 0x64006400u); }
+// The constants live in registers, the masks in scalar ones, which one
+// v_and_or_b32 can name together; as literals they take two instructions.
+struct Masks {
+  uint32_t low, high, magic;
+};
+__device__ __forceinline__ Masks masks() {
+  Masks m = {0x000F000Fu, 0x00F000F0u, 0x64006400u};
+  asm volatile("" : "+s"(m.low), "+s"(m.high), "+v"(m.magic));
+  return m;
+}
+__device__ __forceinline__ half2v low_nibbles(uint32_t w, const Masks &m) { return __builtin_bit_cast(half2v, (w & m.low) | m.magic); }
+__device__ __forceinline__ half2v high_nibbles(uint32_t w, const Masks &m) { return __builtin_bit_cast(half2v, (w & m.high) | m.magic); }
 __device__ __forceinline__ half2v both(float v) { return half2v{(_Float16)v, (_Float16)v}; }
 
 // Elements i and i + 1 of the operand p from two probabilities, as one fp16
@@ -94,13 +104,13 @@ constexpr uint32_t kPlainMeta = 8u << 8;   // k = 8, z = 0
 
 // Eight key codes as fp16 values, dimensions in the order 0 4 1 5 2 6 3 7.
 // Every step is exact.
-__device__ __forceinline__ half8 key_values(uint32_t w, const Pair &m) {
+__device__ __forceinline__ half8 key_values(uint32_t w, const Pair &m, const Masks &k) {
   const half2v sixteenth = both(0.0625f);
   half2v v[4];
-  v[0] = (low_nibbles(w) + m.low) * m.scale;
-  v[1] = __builtin_elementwise_fma(high_nibbles(w), sixteenth, m.high) * m.scale;
-  v[2] = (low_nibbles(w >> 8) + m.low) * m.scale;
-  v[3] = __builtin_elementwise_fma(high_nibbles(w >> 8), sixteenth, m.high) * m.scale;
+  v[0] = (low_nibbles(w, k) + m.low) * m.scale;
+  v[1] = __builtin_elementwise_fma(high_nibbles(w, k), sixteenth, m.high) * m.scale;
+  v[2] = (low_nibbles(w >> 8, k) + m.low) * m.scale;
+  v[3] = __builtin_elementwise_fma(high_nibbles(w >> 8, k), sixteenth, m.high) * m.scale;
   return half8{v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
 }
 
@@ -132,13 +142,13 @@ __device__ __forceinline__ bool value_pairs(const uint32_t (&two)[4], Pair (&p)[
 
 // Two dimensions (the nibbles of a byte) of eight tokens as fp16 values;
 // `pick`: that byte of two tokens' words, each in a half.
-__device__ __forceinline__ void value_byte(const u32x4 (&w)[2], uint32_t pick, const Pair (&p)[4], half8 &v0, half8 &v1) {
+__device__ __forceinline__ void value_byte(const u32x4 (&w)[2], uint32_t pick, const Pair (&p)[4], const Masks &k, half8 &v0, half8 &v1) {
   const half2v sixteenth = both(0.0625f);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const uint32_t x = __builtin_amdgcn_perm(w[e / 2][e % 2 * 2 + 1], w[e / 2][e % 2 * 2], pick);
-    const half2v a0 = (low_nibbles(x) + p[e].low) * p[e].scale;
-    const half2v a1 = __builtin_elementwise_fma(high_nibbles(x), sixteenth, p[e].high) * p[e].scale;
+    const half2v a0 = (low_nibbles(x, k) + p[e].low) * p[e].scale;
+    const half2v a1 = __builtin_elementwise_fma(high_nibbles(x, k), sixteenth, p[e].high) * p[e].scale;
     v0[2 * e] = a0[0], v0[2 * e + 1] = a0[1];
     v1[2 * e] = a1[0], v1[2 * e + 1] = a1[1];
   }
@@ -205,6 +215,11 @@ __device__ __forceinline__ Place place(const KvAttnArgs &a) {
   return p;
 }
 
+// Arrays that a launch only reads, at addresses that a wave agrees on: scalar
+// loads, which wait for nothing but themselves.
+typedef const int32_t __attribute__((address_space(4))) *ScalarInts;
+__device__ __forceinline__ ScalarInts scalar_ints(const int32_t *p) { return (ScalarInts)(uintptr_t)p; }
+
 // What a workgroup needs to know of its sequence.
 struct Seq {
   int start, rows;   // first new token; rows = new tokens * heads a kv head
@@ -212,9 +227,10 @@ struct Seq {
 };
 __device__ __forceinline__ Seq sequence(const KvAttnArgs &a, int b, int group) {
   Seq s;
-  s.start = min(max(a.kv.q_start[b], 0), a.kv.tokens);
-  const int end = min(max(a.kv.q_start[b + 1], s.start), a.kv.tokens);
-  const int len = max(a.kv.kv_len[b], 0);
+  const ScalarInts start = scalar_ints(a.kv.q_start) + b;
+  s.start = min(max(start[0], 0), a.kv.tokens);
+  const int end = min(max(start[1], s.start), a.kv.tokens);
+  const int len = max(scalar_ints(a.kv.kv_len)[b], 0);
   s.rows = (end - s.start) * group;
   s.first = len - (end - s.start);
   s.held = (int)min((int64_t)len, (int64_t)a.kv.table_cols << a.kv.page_log2);
@@ -241,13 +257,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane & 15, j = lane >> 4;
+  const Masks masks_ = masks();
   const Place where = place(a);
   const int b = where.seq, g = where.kv_head, split = where.split;
   const int group = a.heads / a.kv.kv_heads;
   const Seq seq = sequence(a, b, group);
   const size_t page_bytes = (size_t)(D * 9 / 8) << a.kv.page_log2;
   const uint32_t values = (uint32_t)(D / 2) << a.kv.page_log2, kmetas = 2 * values, vmetas = kmetas + ((uint32_t)(D / 16) << a.kv.page_log2);
-  const int32_t *table = a.kv.page_table + b * a.kv.table_stride;
+  const ScalarInts table = scalar_ints(a.kv.page_table + b * a.kv.table_stride);
   const int page_mask = (1 << a.kv.page_log2) - 1;
   const float factor = exponent_factor(a.scale);
 
@@ -300,7 +317,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int col = (t0 + 16 * h) >> a.kv.page_log2;
-        page[h] = __builtin_amdgcn_readfirstlane(col < a.kv.table_cols ? table[col] : -1);
+        page[h] = col < a.kv.table_cols ? table[col] : -1;
       }
     };
     auto record = [&](int h) {
@@ -335,19 +352,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
       find(t0);
       fetch_keys(t0);
       fetch_values(t0);
-      if (t0 + step < end) find(t0 + step);
+      find(t0 + step);
     }
+    // Fetches past the end read some page again (no branch: behind one the wait
+    // for the values would be for the next keys too).
     for (; t0 < end; t0 += step) {
-      const bool more = t0 + step < end;
       float s[2][4];
       held[0] = next_held[0], held[1] = next_held[1];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const Pair km_ = key_pair(km[h]);
+        const Pair pair = key_pair(km[h]);
         floatx4 acc = {};
 #pragma unroll
         for (int t = 0; t < KW; ++t) {
-          const half8 k = key_values(kw[h][t], km_);
+          const half8 k = key_values(kw[h][t], pair, masks_);
 #pragma unroll
           for (int p = PARTS - 1; p >= 0; --p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[p][t], acc, 0, 0, 0);
         }
@@ -362,7 +380,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
           for (int i = 0; i < 4; ++i)
             if (!held[h] || t0 + 16 * h + 4 * j + i > last) s[h][i] = -__builtin_inff();
       }
-      if (more) fetch_keys(t0 + step);
+      fetch_keys(t0 + step);
       // softmax of the block
       float top = s[0][0];
 #pragma unroll
@@ -394,17 +412,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
 #pragma unroll
       for (int bt = 0; bt < NU / 2; ++bt) {
         half8 v0, v1;
-        value_byte(vw, first_byte + bt * 0x00010001u, pairs, v0, v1);
+        value_byte(vw, first_byte + bt * 0x00010001u, pairs, masks_, v0, v1);
 #pragma unroll
         for (int part = PARTS - 1; part >= 0; --part) {
           o[2 * bt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[part], o[2 * bt], 0, 0, 0);
           o[2 * bt + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[part], o[2 * bt + 1], 0, 0, 0);
         }
       }
-      if (more) {
-        fetch_values(t0 + step);
-        if (t0 + 2 * step < end) find(t0 + 2 * step);
-      }
+      fetch_values(t0 + step);
+      find(t0 + 2 * step);
       // A group marked as not stored counts as NaN for the rows that see it and
       // must not touch the others, which multiply it with a zero.  It took part
       // above with a finite scale; here the marked tokens that a row sees are
@@ -501,20 +517,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane & 31, hi = lane >> 5;
+  const Masks masks_ = masks();
   const Place where = place(a);
   const int b = where.seq, g = where.kv_head, split = where.split;
   const int group = a.heads / a.kv.kv_heads;
   const Seq seq = sequence(a, b, group);
   const size_t page_bytes = (size_t)(D * 9 / 8) << a.kv.page_log2;
   const uint32_t values = (uint32_t)(D / 2) << a.kv.page_log2, kmetas = 2 * values, vmetas = kmetas + ((uint32_t)(D / 16) << a.kv.page_log2);
-  const int32_t *table = a.kv.page_table + b * a.kv.table_stride;
+  const ScalarInts table = scalar_ints(a.kv.page_table + b * a.kv.table_stride);
   const int page_mask = (1 << a.kv.page_log2) - 1;
   const int stride = a.splits * kPromptTile;
 
   // the page of token `at`, and whether there is one
   auto page_of = [&](int at, bool &held) {
     const int col = at >> a.kv.page_log2;
-    const int page = __builtin_amdgcn_readfirstlane(col < a.kv.table_cols ? table[col] : -1);
+    const int page = col < a.kv.table_cols ? table[col] : -1;
     held = page >= 0 && page < a.kv.pages;
     return a.kv.pool + ((size_t)(held ? page : 0) * a.kv.kv_heads + g) * page_bytes;
   };
@@ -592,7 +609,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
         const int w0 = KW * (2 * (wave >> 1) + hi);
 #pragma unroll
         for (int x = 0; x < KW; ++x)
-          *reinterpret_cast<half8 *>(to + (wave & 1) * KB + (w0 + x) * 512 + r * 16) = key_values(kw[x], pair);
+          *reinterpret_cast<half8 *>(to + (wave & 1) * KB + (w0 + x) * 512 + r * 16) = key_values(kw[x], pair, masks_);
       }
       // tokens that no row sees must not reach the products, whatever their bytes are
       uint32_t metas[4] = {vm[0][0], vm[0][1], vm[1][0], vm[1][1]};
@@ -607,7 +624,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
 #pragma unroll
       for (int bt = 0; bt < NB / 2; ++bt) {
         half8 v0, v1;
-        value_byte(vw, first_byte + bt * 0x00010001u, pairs, v0, v1);
+        value_byte(vw, first_byte + bt * 0x00010001u, pairs, masks_, v0, v1);
         uint8_t *at = to + 2 * KB + (wave & 1) * KB + (wave >> 1) * 1024 + lane * 16;
         *reinterpret_cast<half8 *>(at + (2 * bt) * 2048) = v0;
         *reinterpret_cast<half8 *>(at + (2 * bt + 1) * 2048) = v1;
