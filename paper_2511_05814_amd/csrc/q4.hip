@@ -45,29 +45,54 @@ __device__ __forceinline__ bf16x8 codes_plus_16(uint32_t w) {
   return __builtin_bit_cast(bf16x8, v);
 }
 
-// Eight elements of x in that order as PARTS bf16 numbers each.
-template <int PARTS>
-__device__ __forceinline__ void split8(const float *f, bf16x8 *out) {
-  float r[8] = {f[0], f[4], f[1], f[5], f[2], f[6], f[3], f[7]};
+// Sixteen elements of x in that order, eight by eight, as PARTS bf16 numbers each.
+__device__ __forceinline__ void load_x(const uint16_t *p, u32x4 (&raw)[2]) {
+  raw[0] = reinterpret_cast<const u32x4 *>(p)[0], raw[1] = reinterpret_cast<const u32x4 *>(p)[1];
+}
+__device__ __forceinline__ void load_x(const float *p, u32x4 (&raw)[4]) {
 #pragma unroll
-  for (int p = 0; p < PARTS; ++p)
+  for (int i = 0; i < 4; ++i) raw[i] = reinterpret_cast<const u32x4 *>(p)[i];
+}
+__device__ __forceinline__ void split_x(const u32x4 (&raw)[2], bf16x8 (&out)[2][1]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      out[p][e] = (__bf16)r[e];
-      if (p + 1 < PARTS) r[e] -= (float)out[p][e];
+  for (int h = 0; h < 2; ++h) {
+    const u32x4 v = raw[h];
+    const u32x4 o = {__builtin_amdgcn_perm(v[2], v[0], 0x05040100u), __builtin_amdgcn_perm(v[2], v[0], 0x07060302u),
+                     __builtin_amdgcn_perm(v[3], v[1], 0x05040100u), __builtin_amdgcn_perm(v[3], v[1], 0x07060302u)};
+    out[h][0] = __builtin_bit_cast(bf16x8, o);
+  }
+}
+__device__ __forceinline__ void split_x(const u32x4 (&raw)[4], bf16x8 (&out)[2][3]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      float a = __uint_as_float(raw[2 * h][e / 2]), b = __uint_as_float(raw[2 * h + 1][e / 2]);  // elements e / 2 and 4 + e / 2
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        out[h][p][e] = (__bf16)a, out[h][p][e + 1] = (__bf16)b;
+        a -= (float)out[h][p][e], b -= (float)out[h][p][e + 1];
+      }
     }
 }
 
-template <int MT, typename T>
+// Scales and zeros of CH groups of a row, as they are.
+template <int CH>
+struct Metas {
+  uint16_t s[CH];
+  uint8_t z[CH];
+};
+
+template <int MT, int CH, typename T>
 __global__ __launch_bounds__(kSmallWaves * kWave) void q4_small_kernel(Q4Args a) {
   constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
   __shared__ float sums[kSmallWaves][MT][16][17];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c = lane & 15, j = lane >> 4;
   const int n0 = blockIdx.x * 16, t0 = blockIdx.y * (16 * MT);
   const int row = min(n0 + c, a.n - 1), groups = a.k / 64;
   const uint8_t *codes = a.codes + (size_t)row * (a.k / 2) + 8 * j;
-  const _Float16 *scales = reinterpret_cast<const _Float16 *>(a.scales) + (size_t)row * groups;
+  const uint16_t *scales = reinterpret_cast<const uint16_t *>(a.scales) + (size_t)row * groups;
   const uint8_t *zeros = a.zeros + (size_t)row * groups;
   const T *x[MT];
 #pragma unroll
@@ -75,29 +100,62 @@ __global__ __launch_bounds__(kSmallWaves * kWave) void q4_small_kernel(Q4Args a)
   bf16x8 ones;
 #pragma unroll
   for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
-  floatx4 y[MT] = {};
-  for (int g = wave; g < groups; g += kSmallWaves) {
-    const uint2 w = *reinterpret_cast<const uint2 *>(codes + (size_t)g * 32);
-    const float scale = (float)scales[g], zero = 16.0f + (float)zeros[g] * (1.0f / 16.0f);
-    const bf16x8 q0 = codes_plus_16(w.x), q1 = codes_plus_16(w.y);
+
+  // A wave takes runs of CH groups, so that the CH loads of a row's codes share
+  // a line; the next run's codes are fetched behind this one's products.
+  uint2 w[CH];
+  Metas<CH> meta;
+  auto fetch = [&](int g0) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      float f[16];
-      load8(x[m] + (size_t)g * 64, f);
-      load8(x[m] + (size_t)g * 64 + 8, f + 8);
-      bf16x8 x0[PARTS], x1[PARTS];
-      split8<PARTS>(f, x0);
-      split8<PARTS>(f + 8, x1);
-      floatx4 dot = {}, sum = {};
+    for (int i = 0; i < CH; ++i) w[i] = *reinterpret_cast<const uint2 *>(codes + (size_t)min(g0 + i, groups - 1) * 32);
+    if (CH > 1 && groups % CH == 0) {
+      g0 = min(g0, groups - CH);
+      __builtin_memcpy(meta.s, __builtin_assume_aligned(scales + g0, 2 * CH), sizeof meta.s);
+      __builtin_memcpy(meta.z, __builtin_assume_aligned(zeros + g0, CH), sizeof meta.z);
+    } else {
 #pragma unroll
-      for (int p = PARTS - 1; p >= 0; --p) {
-        dot = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x0[p], q0, dot, 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x0[p], ones, sum, 0, 0, 0);
-        dot = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x1[p], q1, dot, 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x1[p], ones, sum, 0, 0, 0);
+      for (int i = 0; i < CH; ++i) {
+        meta.s[i] = scales[min(g0 + i, groups - 1)];
+        meta.z[i] = zeros[min(g0 + i, groups - 1)];
       }
+    }
+  };
+  floatx4 y[MT] = {};
+  int g0 = wave * CH;
+  if (g0 < groups) fetch(g0);
+  for (; g0 < groups; g0 += kSmallWaves * CH) {
+    uint2 now[CH];
+    float scale[CH], zero[CH];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[m][i] = fmaf(scale, fmaf(-zero, sum[i], dot[i]), y[m][i]);
+    for (int i = 0; i < CH; ++i) {
+      now[i] = w[i];
+      scale[i] = g0 + i < groups ? (float)__builtin_bit_cast(_Float16, meta.s[i]) : 0.0f;
+      zero[i] = 16.0f + (float)meta.z[i] * (1.0f / 16.0f);
+    }
+    u32x4 raw[MT][CH][sizeof(T)];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int i = 0; i < CH; ++i) load_x(x[m] + (size_t)min(g0 + i, groups - 1) * 64, raw[m][i]);
+    fetch(g0 + kSmallWaves * CH);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const bf16x8 q[2] = {codes_plus_16(now[i].x), codes_plus_16(now[i].y)};
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        bf16x8 xs[2][PARTS];
+        split_x(raw[m][i], xs);
+        floatx4 dot = {}, sum = {};
+#pragma unroll
+        for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            dot = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xs[h][p], q[h], dot, 0, 0, 0);
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xs[h][p], ones, sum, 0, 0, 0);
+          }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[m][e] = fmaf(scale[i], fmaf(-zero[i], sum[e], dot[e]), y[m][e]);
+      }
     }
   }
 #pragma unroll
@@ -109,7 +167,7 @@ __global__ __launch_bounds__(kSmallWaves * kWave) void q4_small_kernel(Q4Args a)
     const int m = o / 256, r = o / 16 % 16, n = n0 + o % 16, t = t0 + 16 * m + r;
     float v = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kSmallWaves; ++w) v += sums[w][m][r][o % 16];
+    for (int i = 0; i < kSmallWaves; ++i) v += sums[i][m][r][o % 16];
     if (n < a.n && t < a.rows) {
       store_result(static_cast<T *>(a.y) + t * a.y_stride + n, v);
     }
@@ -326,9 +384,16 @@ hipError_t launch_tile(const Q4Args &a, hipStream_t s) {
 
 template <int MT>
 void launch_small(const Q4Args &a, bool f32, hipStream_t s) {
-  const dim3 grid((a.n + 15) / 16, (a.rows + 16 * MT - 1) / (16 * MT));
-  if (f32) hipLaunchKernelGGL((q4_small_kernel<MT, float>), grid, dim3(kSmallWaves * kWave), 0, s, a);
-  else hipLaunchKernelGGL((q4_small_kernel<MT, uint16_t>), grid, dim3(kSmallWaves * kWave), 0, s, a);
+  const dim3 grid((a.n + 15) / 16, (a.rows + 16 * MT - 1) / (16 * MT)), block(kSmallWaves * kWave);
+  constexpr int CH = MT == 1 ? 4 : 2;
+  const bool runs = a.k >= 64 * CH * kSmallWaves;  // a run for every wave
+  if (f32) {
+    if (runs) hipLaunchKernelGGL((q4_small_kernel<MT, CH, float>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((q4_small_kernel<MT, 1, float>), grid, block, 0, s, a);
+  } else {
+    if (runs) hipLaunchKernelGGL((q4_small_kernel<MT, CH, uint16_t>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((q4_small_kernel<MT, 1, uint16_t>), grid, block, 0, s, a);
+  }
 }
 
 }  // namespace
