@@ -21,7 +21,7 @@ from __future__ import annotations
 from typing import Optional
 
 import torch
-from torch._C import _cuda_getCurrentRawStream
+from torch._C import _cuda_getCurrentRawStream, _cuda_getDevice
 
 from . import binding as b
 
@@ -37,40 +37,41 @@ def _place(t: torch.Tensor, dtype):
     """(device, stream, MOE_DTYPE_* of dtype) of a call on t: its device, which
     must be the current one, and torch's current stream there."""
     device = t.get_device()
-    if device < 0 or device != torch.cuda.current_device():
+    if device < 0 or device != _cuda_getDevice():
         raise ValueError(f"tensors must be on the current GPU, not on {t.device}")
-    code = _DTYPES.get(dtype)
-    if code is None:
+    if dtype not in _DTYPES:
         raise ValueError(f"tensors must be float32 or bfloat16, not {dtype}")
-    return device, _cuda_getCurrentRawStream(device), code
+    return device, _cuda_getCurrentRawStream(device), _DTYPES[dtype]
 
 
-def _rows(name: str, t: torch.Tensor, device: int, dtype, shape) -> int:
+def _bad(name, t, device, dtype, shape):
+    raise ValueError(f"{name} must be {dtype} {tuple(shape)} with contiguous rows on device {device}, "
+                     f"not {t.dtype} {tuple(t.shape)} of strides {t.stride()} on device {t.get_device()}")
+
+
+def _rows2(name: str, t: torch.Tensor, device: int, dtype, shape) -> int:
     """Elements between the rows of t, which must be of this device, type and
-    shape (2 or 3 dimensions), each row contiguous."""
-    if t.dtype != dtype or t.get_device() != device or t.shape != shape:
-        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on device {device}, "
-                         f"not {t.dtype} {tuple(t.shape)} on device {t.get_device()}")
-    stride, inner = t.stride(), 1
-    if len(shape) == 3:
-        inner = shape[2]
-        if stride[2] != 1 and inner > 1 or stride[1] != inner and shape[1] > 1:
-            raise ValueError(f"{name}: rows must be contiguous")
-        inner *= shape[1]
-    else:
-        inner = shape[1]
-        if stride[1] != 1 and inner > 1:
-            raise ValueError(f"{name}: rows must be contiguous")
-    return stride[0] if shape[0] > 1 else inner
+    shape [rows, columns], each row contiguous."""
+    outer, inner = t.stride()
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or (inner != 1 and shape[1] > 1):
+        _bad(name, t, device, dtype, shape)
+    return outer if shape[0] > 1 else shape[1]
 
 
-def _vector(name: str, t: Optional[torch.Tensor], device: int, dtype, n: int) -> Optional[int]:
-    """Address of a contiguous vector of n elements, None for None."""
-    if t is None:
-        return None
-    if t.dtype != dtype or t.get_device() != device or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} [{n}] on device {device}, "
-                         f"not {t.dtype} {tuple(t.shape)} on device {t.get_device()}")
+def _rows3(name: str, t: torch.Tensor, device: int, dtype, shape) -> int:
+    """The same of shape [tokens, heads, head_dim], a token's heads side by side."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _bad(name, t, device, dtype, shape)
+    outer, mid, inner = t.stride()
+    if inner != 1 or (mid != shape[2] and shape[1] > 1):
+        _bad(name, t, device, dtype, shape)
+    return outer if shape[0] > 1 else shape[1] * shape[2]
+
+
+def _vector(name: str, t: torch.Tensor, device: int, dtype, n: int) -> int:
+    """Address of a contiguous vector of n elements."""
+    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != device or not t.is_contiguous():
+        _bad(name, t, device, dtype, (n,))
     return t.data_ptr()
 
 
@@ -87,8 +88,8 @@ def q4_matmul(x: torch.Tensor, w: torch.Tensor, n: int, out: Optional[torch.Tens
     if out is None:
         out, out_stride = x.new_empty((rows, n)), n
     else:
-        out_stride = _rows("out", out, device, x.dtype, (rows, n))
-    b.moe_q4_matmul(x.data_ptr(), _rows("x", x, device, x.dtype, shape), weights, out.data_ptr(), out_stride, rows, n, k,
+        out_stride = _rows2("out", out, device, x.dtype, (rows, n))
+    b.moe_q4_matmul(x.data_ptr(), _rows2("x", x, device, x.dtype, shape), weights, out.data_ptr(), out_stride, rows, n, k,
                     code, stream)
     return out
 
@@ -113,7 +114,7 @@ def _batch(device, pool, page_table, q_start, kv_len, tokens, head_dim) -> b.moe
     if page_table.dim() != 2:
         raise ValueError("page_table must be [sequences, columns]")
     seqs, cols = page_table.shape
-    stride = _rows("page_table", page_table, device, torch.int32, (seqs, cols))
+    stride = _rows2("page_table", page_table, device, torch.int32, (seqs, cols))
     return b.moe_kv4_batch(pool.data_ptr(), page_table.data_ptr(), _vector("q_start", q_start, device, torch.int32, seqs + 1),
                            _vector("kv_len", kv_len, device, torch.int32, seqs), stride, pages, page_size, kv_heads, head_dim,
                            cols, seqs, tokens)
@@ -132,16 +133,16 @@ def kv4_append(q, k, v, cos, sin, pool, page_table, q_start, kv_len, out: Option
     batch = _batch(device, pool, page_table, q_start, kv_len, tokens, head_dim)
     kv_shape = (tokens, batch.kv_heads, head_dim)
     positions, half = cos.shape
-    _rows("cos", cos, device, torch.float32, (positions, half))
-    _rows("sin", sin, device, torch.float32, (positions, half))
+    _rows2("cos", cos, device, torch.float32, (positions, half))
+    _rows2("sin", sin, device, torch.float32, (positions, half))
     if not cos.is_contiguous() or not sin.is_contiguous():
         raise ValueError("cos and sin must be contiguous")
     if out is None:
         out, out_stride = q.new_empty(shape), heads * head_dim
     else:
-        out_stride = _rows("out", out, device, dtype, shape)
-    b.moe_kv4_append(batch, q.data_ptr(), _rows("q", q, device, dtype, shape), k.data_ptr(),
-                     _rows("k", k, device, dtype, kv_shape), v.data_ptr(), _rows("v", v, device, dtype, kv_shape),
+        out_stride = _rows3("out", out, device, dtype, shape)
+    b.moe_kv4_append(batch, q.data_ptr(), _rows3("q", q, device, dtype, shape), k.data_ptr(),
+                     _rows3("k", k, device, dtype, kv_shape), v.data_ptr(), _rows3("v", v, device, dtype, kv_shape),
                      cos.data_ptr(), sin.data_ptr(), positions, 2 * half, out.data_ptr(), out_stride, heads, code, stream)
     return out
 
@@ -178,7 +179,7 @@ def kv4_attention(q, pool, page_table, q_start, kv_len, scale: float, max_new: O
     if out is None:
         out, out_stride = q.new_empty(shape), heads * head_dim
     else:
-        out_stride = _rows("out", out, device, dtype, shape)
+        out_stride = _rows3("out", out, device, dtype, shape)
     if workspace is None:
         need = b.moe_kv4_attention_workspace_bytes(batch, heads, max_new, max_len)
         if need:
@@ -186,7 +187,7 @@ def kv4_attention(q, pool, page_table, q_start, kv_len, scale: float, max_new: O
     else:
         need = workspace.numel()
         _vector("workspace", workspace, device, torch.uint8, need)
-    b.moe_kv4_attention(batch, q.data_ptr(), _rows("q", q, device, dtype, shape), out.data_ptr(), out_stride, heads, scale,
+    b.moe_kv4_attention(batch, q.data_ptr(), _rows3("q", q, device, dtype, shape), out.data_ptr(), out_stride, heads, scale,
                         code, max_new, max_len, workspace.data_ptr() if need else None, need, stream)
     return out
 
@@ -210,22 +211,25 @@ def norm_residual(h, y=None, gate=None, post=None, pre=None, residual_scale: flo
     elif dtype is None:
         dtype = torch.float32
     device, stream, code = _place(h, dtype)
-    h_stride = _rows("h", h, device, torch.float32, shape)
-    y_ptr, y_stride = (y.data_ptr(), _rows("y", y, device, dtype, shape)) if y is not None else (None, d)
+    h_stride = _rows2("h", h, device, torch.float32, shape)
+    y_ptr, y_stride = (y.data_ptr(), _rows2("y", y, device, dtype, shape)) if y is not None else (None, d)
     gate_ptr, gate_stride = None, 0
     if gate is not None:
         if gate.dim() == 1:
             gate_ptr = _vector("gate", gate, device, torch.float32, d)
         else:
-            gate_ptr, gate_stride = gate.data_ptr(), _rows("gate", gate, device, torch.float32, shape)
-    h_out_stride = d
+            gate_ptr, gate_stride = gate.data_ptr(), _rows2("gate", gate, device, torch.float32, shape)
+    h_out_ptr, h_out_stride, x, x_ptr = None, d, None, None
     if h_out is not None:
-        h_out_stride = _rows("h_out", h_out, device, torch.float32, shape)
+        h_out_ptr, h_out_stride = h_out.data_ptr(), _rows2("h_out", h_out, device, torch.float32, shape)
     elif want_h:
         h_out = h.new_empty(shape)
-    x = h.new_empty(shape, dtype=dtype) if want_x else None
+        h_out_ptr = h_out.data_ptr()
+    if want_x:
+        x = h.new_empty(shape, dtype=dtype)
+        x_ptr = x.data_ptr()
     b.moe_norm_residual(h.data_ptr(), h_stride, y_ptr, y_stride, gate_ptr, gate_stride,
-                        _vector("post", post, device, torch.float32, d), _vector("pre", pre, device, torch.float32, d),
-                        residual_scale, eps, h_out.data_ptr() if h_out is not None else None, h_out_stride,
-                        x.data_ptr() if want_x else None, d, rows, d, code, stream)
+                        None if post is None else _vector("post", post, device, torch.float32, d),
+                        None if pre is None else _vector("pre", pre, device, torch.float32, d),
+                        residual_scale, eps, h_out_ptr, h_out_stride, x_ptr, d, rows, d, code, stream)
     return h_out, x

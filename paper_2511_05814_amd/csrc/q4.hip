@@ -5,6 +5,8 @@
 // uint8 zero codes [n][k/64]; weight = (q - zero / 16) * scale.
 #include "common.hpp"
 
+#include <type_traits>
+
 namespace moe {
 namespace {
 
@@ -76,16 +78,22 @@ __device__ __forceinline__ void split_x(const u32x4 (&raw)[4], bf16x8 (&out)[2][
     }
 }
 
-// Scales and zeros of CH groups of a row, as they are.
-template <int CH>
-struct Metas {
-  uint16_t s[CH];
-  uint8_t z[CH];
-};
+// Unsigned integers of CH fp16 scales and of CH zeros.
+template <int CH> struct MetaWords;
+template <> struct MetaWords<1> { typedef uint16_t S; typedef uint8_t Z; };
+template <> struct MetaWords<2> { typedef uint32_t S; typedef uint16_t Z; };
+template <> struct MetaWords<4> { typedef uint64_t S; typedef uint32_t Z; };
 
+// A wave takes runs of CH groups: four (rows of a multiple of 256 columns) fill
+// a line of a row's codes, whose four loads follow one another.  With single
+// groups the waves ask for parts of the same lines at different times, 16 rows
+// apart by a power of two where k is one: one token by 6144 x 4096 takes 14.5 us
+// so, 9.4 with runs (by 6144 x 4160 9.6).  The next run's codes and the next
+// group's x are on their way while a group is multiplied.  Two workgroups fit a
+// compute unit for 16 rows (runs of two groups in fp32).
 template <int MT, int CH, typename T>
-__global__ __launch_bounds__(kSmallWaves * kWave) void q4_small_kernel(Q4Args a) {
-  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+__global__ __launch_bounds__(kSmallWaves * kWave, MT == 1 ? 4 : 2) void q4_small_kernel(Q4Args a) {
+  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, kStep = kSmallWaves * CH;
   __shared__ float sums[kSmallWaves][MT][16][17];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int c = lane & 15, j = lane >> 4;
@@ -101,61 +109,78 @@ __global__ __launch_bounds__(kSmallWaves * kWave) void q4_small_kernel(Q4Args a)
 #pragma unroll
   for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.0f;
 
-  // A wave takes runs of CH groups, so that the CH loads of a row's codes share
-  // a line; the next run's codes are fetched behind this one's products.
-  uint2 w[CH];
-  Metas<CH> meta;
-  auto fetch = [&](int g0) {
+  struct Run {
+    uint2 w[CH];
+    typename MetaWords<CH>::S s;
+    typename MetaWords<CH>::Z z;
+  };
+  struct Rows {
+    u32x4 x[MT][sizeof(T)];
+  };
+  auto fetch_run = [&](Run &r, int g) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) w[i] = *reinterpret_cast<const uint2 *>(codes + (size_t)min(g0 + i, groups - 1) * 32);
-    if (CH > 1 && groups % CH == 0) {
-      g0 = min(g0, groups - CH);
-      __builtin_memcpy(meta.s, __builtin_assume_aligned(scales + g0, 2 * CH), sizeof meta.s);
-      __builtin_memcpy(meta.z, __builtin_assume_aligned(zeros + g0, CH), sizeof meta.z);
-    } else {
+    for (int i = 0; i < CH; ++i) r.w[i] = *reinterpret_cast<const uint2 *>(codes + (size_t)(g + i) * 32);
+    r.s = *reinterpret_cast<const decltype(r.s) *>(scales + g);
+    r.z = *reinterpret_cast<const decltype(r.z) *>(zeros + g);
+  };
+  auto fetch_rows = [&](Rows &r, int g) {
 #pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        meta.s[i] = scales[min(g0 + i, groups - 1)];
-        meta.z[i] = zeros[min(g0 + i, groups - 1)];
-      }
-    }
+    for (int m = 0; m < MT; ++m) load_x(x[m] + (size_t)g * 64, r.x[m]);
   };
   floatx4 y[MT] = {};
-  int g0 = wave * CH;
-  if (g0 < groups) fetch(g0);
-  for (; g0 < groups; g0 += kSmallWaves * CH) {
-    uint2 now[CH];
-    float scale[CH], zero[CH];
+  auto multiply = [&](const Run &run, int i, const Rows &r) {
+    const float scale = (float)__builtin_bit_cast(_Float16, (uint16_t)(run.s >> (16 * i)));
+    const float zero = 16.0f + (float)(uint8_t)(run.z >> (8 * i)) * (1.0f / 16.0f);
+    const bf16x8 q[2] = {codes_plus_16(run.w[i].x), codes_plus_16(run.w[i].y)};
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      now[i] = w[i];
-      scale[i] = g0 + i < groups ? (float)__builtin_bit_cast(_Float16, meta.s[i]) : 0.0f;
-      zero[i] = 16.0f + (float)meta.z[i] * (1.0f / 16.0f);
+    for (int m = 0; m < MT; ++m) {
+      bf16x8 xs[2][PARTS];
+      split_x(r.x[m], xs);
+      floatx4 dot = {}, sum = {};
+#pragma unroll
+      for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          dot = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xs[h][p], q[h], dot, 0, 0, 0);
+          sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xs[h][p], ones, sum, 0, 0, 0);
+        }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[m][e] = fmaf(scale, fmaf(-zero, sum[e], dot[e]), y[m][e]);
     }
-    u32x4 raw[MT][CH][sizeof(T)];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int i = 0; i < CH; ++i) load_x(x[m] + (size_t)min(g0 + i, groups - 1) * 64, raw[m][i]);
-    fetch(g0 + kSmallWaves * CH);
+  };
+  // One run, `next` its successor's first group; with MORE that one is fetched.
+  // Group i's x is in rows[(FIRST + i) % 2].
+  Run run[2];
+  Rows rows[2];
+  auto step = [&](const Run &now, Run &after, int g, auto more, auto first) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const bf16x8 q[2] = {codes_plus_16(now[i].x), codes_plus_16(now[i].y)};
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        bf16x8 xs[2][PARTS];
-        split_x(raw[m][i], xs);
-        floatx4 dot = {}, sum = {};
-#pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            dot = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xs[h][p], q[h], dot, 0, 0, 0);
-            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xs[h][p], ones, sum, 0, 0, 0);
-          }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[m][e] = fmaf(scale[i], fmaf(-zero[i], sum[e], dot[e]), y[m][e]);
+      constexpr int kFirst = decltype(first)::value;
+      if (i + 1 < CH) fetch_rows(rows[(kFirst + i + 1) % 2], g + i + 1);
+      else if (decltype(more)::value) fetch_rows(rows[(kFirst + CH) % 2], g + kStep);
+      if (i == 0 && decltype(more)::value) fetch_run(after, g + kStep);
+      multiply(now, i, rows[(kFirst + i) % 2]);
+    }
+  };
+  typedef std::integral_constant<bool, true> Yes;
+  typedef std::integral_constant<bool, false> No;
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, CH % 2> Other;
+  int g = wave * CH;
+  if (g < groups) {
+    fetch_run(run[0], g);
+    fetch_rows(rows[0], g);
+    for (;; g += 2 * kStep) {
+      if (g + kStep >= groups) {
+        step(run[0], run[1], g, No(), Even());
+        break;
       }
+      step(run[0], run[1], g, Yes(), Even());
+      if (g + 2 * kStep >= groups) {
+        step(run[1], run[0], g + kStep, No(), Other());
+        break;
+      }
+      step(run[1], run[0], g + kStep, Yes(), Other());
     }
   }
 #pragma unroll
@@ -382,25 +407,20 @@ hipError_t launch_tile(const Q4Args &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int MT>
-void launch_small(const Q4Args &a, bool f32, hipStream_t s) {
+template <int MT, typename T>
+void launch_small(const Q4Args &a, hipStream_t s) {
   const dim3 grid((a.n + 15) / 16, (a.rows + 16 * MT - 1) / (16 * MT)), block(kSmallWaves * kWave);
-  constexpr int CH = MT == 1 ? 4 : 2;
-  const bool runs = a.k >= 64 * CH * kSmallWaves;  // a run for every wave
-  if (f32) {
-    if (runs) hipLaunchKernelGGL((q4_small_kernel<MT, CH, float>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((q4_small_kernel<MT, 1, float>), grid, block, 0, s, a);
-  } else {
-    if (runs) hipLaunchKernelGGL((q4_small_kernel<MT, CH, uint16_t>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((q4_small_kernel<MT, 1, uint16_t>), grid, block, 0, s, a);
-  }
+  // runs where rows of W are a multiple of them and give every wave one
+  constexpr int CH = MT == 1 && sizeof(T) == 4 ? 2 : 4;
+  if (a.k % (64 * CH) == 0 && a.k >= 64 * CH * kSmallWaves) hipLaunchKernelGGL((q4_small_kernel<MT, CH, T>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((q4_small_kernel<MT, 1, T>), grid, block, 0, s, a);
 }
 
 }  // namespace
 
 hipError_t launch_q4_matmul(const Q4Args &a, bool f32, hipStream_t s) {
-  if (a.rows <= 16) launch_small<1>(a, f32, s);
-  else if (a.rows <= 32) launch_small<2>(a, f32, s);
+  if (a.rows <= 16) f32 ? launch_small<1, float>(a, s) : launch_small<1, uint16_t>(a, s);
+  else if (a.rows <= 32) f32 ? launch_small<2, float>(a, s) : launch_small<2, uint16_t>(a, s);
   else if (f32) return a.rows <= 64 ? launch_tile<64, float>(a, s) : launch_tile<128, float>(a, s);
   else return a.rows <= 64 ? launch_tile<64, uint16_t>(a, s) : a.rows <= 128000 ? launch_tile<128, uint16_t>(a, s) : launch_tile<256, uint16_t>(a, s);
   return hipGetLastError();
