@@ -401,10 +401,9 @@ __global__ __launch_bounds__(256, BM <= 128 && sizeof(T) == 2 ? 2 : 1) void q4_t
 }
 
 template <int BM, typename T>
-hipError_t launch_tile(const Q4Args &a, hipStream_t s) {
+void launch_tile(const Q4Args &a, hipStream_t s) {
   const int mb = (a.rows + BM - 1) / BM, nb = (a.n + kTileN - 1) / kTileN;
   hipLaunchKernelGGL((q4_tile_kernel<BM, T>), dim3((unsigned)mb * nb), dim3(256), 0, s, a, mb, nb);
-  return hipGetLastError();
 }
 
 template <int MT, typename T>
@@ -416,13 +415,48 @@ void launch_small(const Q4Args &a, hipStream_t s) {
   else hipLaunchKernelGGL((q4_small_kernel<MT, 1, T>), grid, block, 0, s, a);
 }
 
+// Estimated times (us) on the 256 compute units, each with `load` workgroups of
+// a launch one after another (two at a time for tiles of bf16).  Measured, us
+// small 16 / 32 / 64 rows a workgroup, tiles of 64 / 128 rows, and the choice:
+//   bf16, 6144 x 4096,   17 rows:  18.0  17.0  21.0  48.4  60.0   32
+//                        64:       39.4  32.4  36.5  49.5  60.7   32
+//                       128:       75.9  63.1  54.0  49.7  60.7   64-row tiles
+//                       384:      221   186   159    63.7  61.0   128-row tiles
+//   bf16, 4096 x 14336,  64:       85.3  68.6  59.3  170   200    64
+//                       200:      266   223   202   170   200     64-row tiles
+//   bf16, 513 x 8192,   128:       27.1  21.2  35.3  94.3  115    32
+//   bf16, 512 x 512,    512:        6.5   4.8   4.7   9.3  11.7   64
+//   f32,  2048 x 2048,   48:       13.2  11.0    -   42.1  71.4   32
+//                       512:       88.4  75.3    -   44.7  72.2   64-row tiles
+constexpr float kNever = 1e30f;
+struct Cost {
+  float first, pair;  // us a column (small) or a step of 64 columns (tiles): one workgroup, two at a time
+};
+float small_cost(const Q4Args &a, int mt, float column) {
+  const int64_t wgs = (int64_t)((a.n + 15) / 16) * ((a.rows + 16 * mt - 1) / (16 * mt));
+  return 2.0f + column * (float)a.k * (float)((wgs + 255) / 256);
+}
+float tile_cost(const Q4Args &a, int bm, Cost c) {
+  const int64_t load = ((int64_t)((a.n + kTileN - 1) / kTileN) * ((a.rows + bm - 1) / bm) + 255) / 256;
+  return 3.0f + (float)(a.k / 64) * ((float)(load / 2) * c.pair + (float)(load % 2) * c.first);
+}
+
 }  // namespace
 
 hipError_t launch_q4_matmul(const Q4Args &a, bool f32, hipStream_t s) {
-  if (a.rows <= 16) f32 ? launch_small<1, float>(a, s) : launch_small<1, uint16_t>(a, s);
-  else if (a.rows <= 32) f32 ? launch_small<2, float>(a, s) : launch_small<2, uint16_t>(a, s);
-  else if (f32) return a.rows <= 64 ? launch_tile<64, float>(a, s) : launch_tile<128, float>(a, s);
-  else return a.rows <= 64 ? launch_tile<64, uint16_t>(a, s) : a.rows <= 128000 ? launch_tile<128, uint16_t>(a, s) : launch_tile<256, uint16_t>(a, s);
+  const float cost[5] = {small_cost(a, 1, f32 ? 2.8e-3f : 1.6e-3f), small_cost(a, 2, f32 ? 4.4e-3f : 2.5e-3f),
+                         f32 ? kNever : small_cost(a, 4, 4.25e-3f), tile_cost(a, 64, f32 ? Cost{1.27f, 2.54f} : Cost{0.77f, 1.0f}),
+                         tile_cost(a, 128, f32 ? Cost{2.17f, 4.34f} : Cost{0.93f, 1.31f})};
+  int best = 0;
+  for (int i = 1; i < 5; ++i)
+    if (cost[i] < cost[best]) best = i;
+  switch (best) {
+    case 0: f32 ? launch_small<1, float>(a, s) : launch_small<1, uint16_t>(a, s); break;
+    case 1: f32 ? launch_small<2, float>(a, s) : launch_small<2, uint16_t>(a, s); break;
+    case 2: launch_small<4, uint16_t>(a, s); break;
+    case 3: f32 ? launch_tile<64, float>(a, s) : launch_tile<64, uint16_t>(a, s); break;
+    default: f32 ? launch_tile<128, float>(a, s) : launch_tile<128, uint16_t>(a, s);
+  }
   return hipGetLastError();
 }
 

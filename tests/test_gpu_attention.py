@@ -75,6 +75,35 @@ def test_q4_matmul(rows, n, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n,k", [(1000, 2000, 128), (2000, 2001, 192), (700, 3001, 1088), (700, 3001, 1024), (333, 5003, 576),
+                                      (1025, 1929, 64), (100, 16384, 512)])
+def test_q4_matmul_many_rows(rows, n, k, dtype):
+    """Shapes that go by tiles of 64 and of 128 rows, with their odd ends; rows
+    of scales that are and are not multiples of eight groups."""
+    rng = np.random.default_rng(n + k)
+    buf = matrix(rng, n, k)
+    x = rng.standard_normal((rows, k)).astype(np.float32) * np.exp(rng.standard_normal(k)).astype(np.float32)
+    x = bf16(x) if dtype == "bf16" else x
+    wide = torch.zeros((rows, k + 8), dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+    wide[:, :k] = device(x, dtype)
+    out = torch.full((rows, n + 3), 7.0, dtype=wide.dtype, device="cuda")
+    y = ops().q4_matmul(wide[:, :k], torch.from_numpy(buf).cuda(), n, out=out[:, 1:1 + n])
+    check_product(x.astype(np.float64), buf, n, k, y, dtype)
+    assert (out[:, 0] == 7).all() and (out[:, 1 + n:] == 7).all()
+
+
+def test_q4_matmul_many_rows_keeps_rows_apart():
+    rng = np.random.default_rng(5)
+    rows, n, k = 700, 3001, 128
+    w = torch.from_numpy(matrix(rng, n, k)).cuda()
+    x = rng.standard_normal((rows, k)).astype(np.float32)
+    x[3, 70], x[400, 0], x[699, 127] = np.nan, np.inf, -np.inf
+    for dtype in ("f32", "bf16"):
+        bad = np.isnan(host(ops().q4_matmul(device(x, dtype), w, n)))
+        assert bad[[3, 400, 699]].all() and bad.sum() == 3 * n
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [1, 3, 9, 40, 150])
 def test_q4_matmul_strided(rows, dtype):
     """x a slice of wider rows, y inside a larger tensor whose other columns stay."""
