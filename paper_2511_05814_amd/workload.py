@@ -172,6 +172,26 @@ def _draw_into(rng: np.random.Generator, out: np.ndarray, dtype: str) -> None:
         out[i:i + m] = v if dtype == "f32" else f32_to_bf16_bits(v)
 
 
+def quantize_q4g64(w: np.ndarray) -> np.ndarray:
+    """Round-to-nearest 4-bit quantisation of fp32 rows [n x k] in groups of 64
+    consecutive columns, as the bytes moe_q4_matmul reads: codes [n][k/2] (column
+    c in nibble c % 2 of byte c / 2), fp16 scales [n][k/64], uint8 zero codes
+    [n][k/64] (zero point = code / 16).  scale = (max - min) / 15 rounded to fp16,
+    zero code = round(-min / scale * 16) clipped to [0, 255], code = round(w /
+    scale + zero) clipped to [0, 15]."""
+    n, k = w.shape
+    if k % 64:
+        raise ValueError("4-bit rows need a multiple of 64 columns")
+    g = np.ascontiguousarray(w, dtype=np.float32).reshape(n, k // 64, 64)
+    lo, hi = g.min(-1), g.max(-1)
+    scale = ((hi - lo) / np.float32(15)).astype(np.float16)
+    step = np.where(scale == 0, np.float32(1), scale.astype(np.float32))
+    zero = np.clip(np.rint(-lo / step * 16), 0, 255).astype(np.uint8)
+    q = np.rint(g / step[..., None] + zero[..., None].astype(np.float32) / 16)
+    q = np.clip(q, 0, 15).astype(np.uint8).reshape(n, k)
+    return np.concatenate([(q[:, 0::2] | q[:, 1::2] << 4).reshape(-1), scale.reshape(-1).view(np.uint8), zero.reshape(-1)])
+
+
 def quantize_q2g16(w: np.ndarray):
     """Round-to-nearest 2-bit quantisation of fp32 rows in groups of 16
     consecutive columns: scale = (max - min) / 3 rounded to fp16, zero code =

@@ -64,3 +64,18 @@ def test_attention_and_norm_formulas():
     h, x = oa.norm_residual(q, q, gate=2.0, post=np.ones(8), residual_scale=0.5)
     want = 0.5 * q + 2 * q / np.sqrt((q * q).mean(1, keepdims=True) + 1e-5)
     assert np.allclose(h, want) and np.allclose(x, want / np.sqrt((want * want).mean(1, keepdims=True) + 1e-5))
+
+
+def test_quantize_q4g64_reads_back():
+    from paper_2511_05814_amd import workload as wl
+    rng = np.random.default_rng(4)
+    w = rng.standard_normal((5, 192)).astype(np.float32) * 0.02
+    w[2] = 0
+    back = oa.q4_dequantize(wl.quantize_q4g64(w), 5, 192)
+    g = w.reshape(5, 3, 64)
+    step = (g.max(-1) - g.min(-1)) / 15
+    # half a step, the zero point's 1/32 of one and the scale's fp16 rounding over 15
+    assert (np.abs(back - w) <= np.repeat(step, 64, 1) * (0.5 + 1 / 32 + 15 * 2.0 ** -10) + 1e-12).all()
+    assert (back[2] == 0).all()
+    with pytest.raises(ValueError):
+        wl.quantize_q4g64(w[:, :100])
