@@ -18,13 +18,21 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = 32;           // tokens of a wave's step
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr float kPShift = 14.0f;    // probabilities are held times 2^14: fp16 keeps 2^-38 of the largest
 
-// 2^((dot - top) down) in that scale.  The difference of dot products is exact
-// near the top, so that 2^14 is not passed even where the last place of a score
-// is worth more than 1.
-__device__ __forceinline__ float power(float dot, float top, float down) {
-  return __builtin_amdgcn_exp2f(fmaf(dot - top, down, kPShift));
+// Probabilities are held times 2^shift, relative to a row's reference score: its
+// largest up to now, or one at most `slack` powers of two below it, so that sums
+// are rescaled only now and then.  fp16 then keeps at least 2^-(24 + shift) of
+// the largest and 2^(shift + slack) does not pass its range.  (fp32 calls, which
+// hold a probability as two numbers, need the finer end.)
+template <int PARTS> struct Hold { static constexpr float shift = 8.0f, slack = 7.0f; };
+template <> struct Hold<2> { static constexpr float shift = 14.0f, slack = 1.0f; };
+
+// 2^((dot - ref) down) in that scale.  The difference of dot products is exact
+// near the reference, so that the range is kept even where the last place of a
+// score is worth more than 1.
+template <int PARTS>
+__device__ __forceinline__ float power(float dot, float ref, float down) {
+  return __builtin_amdgcn_exp2f(fmaf(dot - ref, down, Hold<PARTS>::shift));
 }
 
 // Codes of a word that lie 16 bits apart, as pairs of fp16 1024 + q (low
@@ -195,11 +203,15 @@ __device__ __forceinline__ float sum_over_j(float v) {
   return sum_of_halves(a + b);
 }
 
-// A workgroup's split, block of rows and (sequence, kv head), in this order in a
-// launch's one dimension.  Workgroups go to the XCDs, and there to the shader
-// engines, in turn: with the sequences in the first place four of them, one
-// long, put all of its work on one engine of each XCD (682 us instead of 240
-// for prompts of 2048 tokens over 2048 and three shorter ones).
+// A workgroup's split, kv head, sequence and block of rows, from a launch's one
+// dimension.  Workgroups start in its order and go to the XCDs, and there to the
+// four shader engines, in turn.  Short calls: splits first, so that every
+// sequence is spread over all of them.  Prompts: blocks last and the later rows,
+// which see most, first, so that the longest work starts first; the sequences of
+// a block rotate with it, or one in four, long, would put all of its work on one
+// engine of each XCD (prompts of 2048 tokens over 2048 and three shorter ones:
+// 682 us so, 188 with the blocks of a sequence one after another, 183 as it is;
+// measured before the steps that came after).
 struct Place {
   int split, block, seq, kv_head;
 };
@@ -208,10 +220,18 @@ __device__ __forceinline__ Place place(const KvAttnArgs &a) {
   uint32_t id = blockIdx.x;
   p.split = id % (uint32_t)a.splits;
   id /= (uint32_t)a.splits;
-  p.block = id % (uint32_t)a.row_blocks;
-  id /= (uint32_t)a.row_blocks;
-  p.kv_head = id % (uint32_t)a.kv.kv_heads;
-  p.seq = id / (uint32_t)a.kv.kv_heads;
+  if (a.prompt) {
+    p.kv_head = id % (uint32_t)a.kv.kv_heads;
+    id /= (uint32_t)a.kv.kv_heads;
+    const uint32_t turn = id / (uint32_t)a.kv.seqs;
+    p.seq = (id + turn) % (uint32_t)a.kv.seqs;
+    p.block = a.row_blocks - 1 - (int)turn;
+  } else {
+    p.block = id % (uint32_t)a.row_blocks;
+    id /= (uint32_t)a.row_blocks;
+    p.kv_head = id % (uint32_t)a.kv.kv_heads;
+    p.seq = id / (uint32_t)a.kv.kv_heads;
+  }
   return p;
 }
 
@@ -385,19 +405,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
       float top = s[0][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i / 4][i % 4]);
-      top = fmaxf(m, max_over_j(top));
-      const float ref = top == -__builtin_inff() ? 0.0f : top;
-      if (__builtin_amdgcn_ballot_w64(top > m)) {
-        const float keep = __builtin_amdgcn_exp2f((m - ref) * down);
+      top = max_over_j(top);
+      if (__builtin_amdgcn_ballot_w64((top - m) * down > Hold<PARTS>::slack)) {
+        top = fmaxf(m, top);
+        const float keep = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - top) * down);
+        m = top;
         l *= keep;
 #pragma unroll
         for (int u = 0; u < NU; ++u) o[u] *= keep;
       }
-      m = top;
+      const float ref = m == -__builtin_inff() ? 0.0f : m;
       half8 p[PARTS];
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
-        const float v0 = power(s[i / 4][i % 4], ref, down), v1 = power(s[i / 4][i % 4 + 1], ref, down);
+        const float v0 = power<PARTS>(s[i / 4][i % 4], ref, down), v1 = power<PARTS>(s[i / 4][i % 4 + 1], ref, down);
         add_pair<PARTS>(v0, v1, i, p, l);
       }
       // values: word of token e, dimension u in nibble u; tokens that no row of
@@ -512,7 +533,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
   constexpr int KW = D / 32;           // words of a key that a thread expands
   constexpr int KB = 32 * D * 2;       // LDS bytes of 32 keys, or of 32 values
   __shared__ __align__(16) uint8_t s_kv[2][4 * KB];          // keys of both blocks, values of both
-  __shared__ __align__(16) uint8_t s_mark[2][D / 32][kPromptTile];  // value groups that are marked as not stored
+  __shared__ __align__(16) uint8_t s_mark[2][D / 32][kPromptTile];  // marks of value groups, where s_any says there are
   __shared__ __align__(16) uint32_t s_any[2][kWaves];        // bit 0: marks in the wave's share, bit 1: a page is missing
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -536,7 +557,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
     return a.kv.pool + ((size_t)(held ? page : 0) * a.kv.kv_heads + g) * page_bytes;
   };
 
-  for (int block = a.row_blocks - 1 - where.block; block * kPromptRows < seq.rows; block += a.row_blocks) {
+  for (int block = where.block; block * kPromptRows < seq.rows; block += a.row_blocks) {
     const int wrow = block * kPromptRows + wave * 32;   // the wave's first row
     const int row = min(wrow + r, seq.rows - 1);
     const int token = seq.start + row / group, head = g * group + row % group;
@@ -631,7 +652,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
       }
       const bool any = __builtin_amdgcn_ballot_w64(marked) != 0;
       if (lane == 0) s_any[buf][wave] = (any ? 1u : 0u) | (both_held ? 0u : 2u);
-      if (r % 8 == 0) {   // a lane of each group of 32 dimensions (D 64: of each half)
+      if (any && r % 8 == 0) {   // a lane of each group of 32 dimensions (D 64: of each half)
         uint8_t *mp = &s_mark[buf][r / (8 / NB) / 4][32 * (wave & 1) + 16 * (wave >> 1) + 4 * hi];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -652,19 +673,32 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
       }
       if (t0 < 0 || t0 >= wend) continue;
       __builtin_amdgcn_sched_barrier(0);   // staging's registers are free again before the scores take theirs
+      // two chains of products, the operands of the next two steps on their way
       floatx16 s[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        if (x) __builtin_amdgcn_sched_barrier(0);
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[x][i] = 0.0f;
+      half8 k[3][2];
+      auto keys = [&](int x, int t) { return *reinterpret_cast<const half8 *>(from + x * KB + t * 1024 + lane * 16); };
 #pragma unroll
-        for (int t = 0; t < KS; ++t) {
-          const half8 k = *reinterpret_cast<const half8 *>(from + x * KB + t * 1024 + lane * 16);
+      for (int t = 0; t < 2; ++t) k[t][0] = keys(0, t), k[t][1] = keys(1, t);
 #pragma unroll
-          for (int p = PARTS - 1; p >= 0; --p) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[p][t], s[x], 0, 0, 0);
-        }
+      for (int t = 0; t < KS; ++t) {
+        if (t + 2 < KS) k[(t + 2) % 3][0] = keys(0, t + 2), k[(t + 2) % 3][1] = keys(1, t + 2);
+#pragma unroll
+        for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[t % 3][x], q[p][t], s[x], 0, 0, 0);
       }
+      // in this order: left to itself the compiler reads an operand, waits and multiplies
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);   // reads of LDS
+#pragma unroll
+      for (int t = 0; t < KS; ++t) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 2 * PARTS, 0);   // matrix instructions
+        if (t + 2 < KS) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
       const u32x4 any4 = *reinterpret_cast<const u32x4 *>(s_any[buf]);
       const uint32_t any = __builtin_amdgcn_readfirstlane(any4[0] | any4[1] | any4[2] | any4[3]);
       if (t0 + kPromptTile - 1 > wfirst || (any & 2)) {
@@ -679,34 +713,33 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
           }
         }
       }
-      float top = m;
+      float top = s[0][0];
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[x][i]);
+      for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
       top = max_of_halves(top);
-      const float ref = top == -__builtin_inff() ? 0.0f : top;
-      if (__builtin_amdgcn_ballot_w64(top > m)) {
-        const float keep = __builtin_amdgcn_exp2f((m - ref) * rs.down);
+      if (__builtin_amdgcn_ballot_w64((top - m) * rs.down > Hold<PARTS>::slack)) {
+        top = fmaxf(m, top);
+        const float keep = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - top) * rs.down);
+        m = top;
         l *= keep;
 #pragma unroll
         for (int u = 0; u < NB; ++u) o[u] *= keep;
       }
-      m = top;
+      const float ref = m == -__builtin_inff() ? 0.0f : m;
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          half8 p[PARTS];
+          half8 v[NB], p[PARTS];
+#pragma unroll
+          for (int u = 0; u < NB; ++u) v[u] = *reinterpret_cast<const half8 *>(from + 2 * KB + x * KB + u * 2048 + h * 1024 + lane * 16);
 #pragma unroll
           for (int e = 0; e < 8; e += 2)
-            add_pair<PARTS>(power(s[x][8 * h + e], ref, rs.down), power(s[x][8 * h + e + 1], ref, rs.down), e, p, l);
+            add_pair<PARTS>(power<PARTS>(s[x][8 * h + e], ref, rs.down), power<PARTS>(s[x][8 * h + e + 1], ref, rs.down), e, p, l);
 #pragma unroll
-          for (int u = 0; u < NB; ++u) {
-            const half8 v = *reinterpret_cast<const half8 *>(from + 2 * KB + x * KB + u * 2048 + h * 1024 + lane * 16);
+          for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
-            for (int part = PARTS - 1; part >= 0; --part) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[part], o[u], 0, 0, 0);
-          }
+            for (int u = 0; u < NB; ++u) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[u], p[part], o[u], 0, 0, 0);
         }
       // Groups marked as not stored: counted for the rows that see them, as in
       // the kernel above.
@@ -721,7 +754,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const int at = 16 * x + 8 * (e / 4) + 4 * hi + e % 4;
-            mark[e] = (_Float16)(float)marks[at];
+            mark[e] = (_Float16)(any4[x / 2 + 2 * (x % 2)] & 1 ? (float)marks[at] : 0.0f);
             seen[e] = (_Float16)(t0 + at <= last ? 1.0f : 0.0f);
           }
           count = __builtin_amdgcn_mfma_f32_32x32x16_f16(mark, seen, count, 0, 0, 0);
