@@ -1,8 +1,10 @@
 """Build the HIP library in-tree: paper_2511_05814_amd/_lib/libmoe_offload.so.
 
-Compiles every source under csrc/ for gfx950 with hipcc into one shared
-library exporting the C ABI of include/moe_offload.h.  Run as a module
-(`python -m paper_2511_05814_amd.build`) or through __graft_entry__.build().
+Compiles every HIP source under csrc/ for gfx950 with hipcc into one shared
+library exporting the C ABI of include/moe_offload.h, and csrc/attention_ops.cpp
+(host code: the torch calls of `attention`) into a CPython module beside it that
+links to it.  Run as a module (`python -m paper_2511_05814_amd.build`) or through
+__graft_entry__.build().
 """
 from __future__ import annotations
 
@@ -16,6 +18,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_lib")
 OUT = os.path.join(OUT_DIR, "libmoe_offload.so")
+OPS = os.path.join(OUT_DIR, "_attention_ops.so")
 ARCH = "gfx950"
 
 FLAGS = [
@@ -31,6 +34,28 @@ def hipcc() -> str:
         if cand and (os.path.sep not in cand or os.path.exists(cand)):
             return cand
     raise RuntimeError("hipcc not found")
+
+
+def build_ops(verbose: bool = False) -> str:
+    """The CPython module, against this interpreter's and torch's headers."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    tmp = OPS + ".tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"],
+           *[f for d in cpp_extension.include_paths() for f in ("-isystem", d)],
+           os.path.join(CSRC, "attention_ops.cpp"), "-o", tmp, OUT, "-Wl,-rpath,$ORIGIN",
+           *["-L" + d for d in cpp_extension.library_paths()], "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + "\n".join(res.stderr.splitlines()[-60:]))
+    os.replace(tmp, OPS)
+    return OPS
 
 
 def build(verbose: bool = False) -> str:
@@ -49,6 +74,7 @@ def build(verbose: bool = False) -> str:
     if verbose and errs:
         print("\n".join(errs[-40:]))
     os.replace(tmp, OUT)
+    build_ops(verbose)
     return OUT
 
 
