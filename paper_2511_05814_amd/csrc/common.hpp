@@ -313,7 +313,7 @@ hipError_t launch_kv4_read(const KvReadArgs &a, int head_dim, bool f32, hipStrea
 struct KvAttnShape {
   int splits, row_blocks, prompt;
 };
-KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int max_new, int max_len);
+KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len);
 hipError_t launch_kv4_attention(const KvAttnArgs &a, int head_dim, bool f32, hipStream_t s);
 
 struct Q4Args {

@@ -875,21 +875,30 @@ void launch(const KvAttnArgs &a, hipStream_t s) {
 
 }  // namespace
 
-// Rows in blocks of 16, or of 128 from 64 rows a sequence and kv head on; enough
-// workgroups for four (two with large blocks) on each of the 256 compute units,
-// none with less than one block of 32 tokens a wave (one tile).  Up to 512 tokens
-// are not split: what the second launch costs is more than it saves (32 heads,
-// 300 tokens 9.0 us split, 7.4 not; 1023 tokens 12.1 and 12.8).
-KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int max_new, int max_len) {
+// Rows in blocks of 16, or of 128 from 64 rows a sequence and kv head on.  Enough
+// workgroups for four on each of the 256 compute units, two with large blocks
+// (four from eight sequences on, whose lengths differ: 45 sequences of up to 67
+// new tokens over 22502, us with two / four / eight: 238 / 152 / 122; 11 of 32
+// over 23050: 151 / 89 / 99; 3 of 100 over 6000: 55 / 60 / 79).  What counts are
+// blocks that can have rows: 215 tokens of one sequence of 28854 and single ones
+// of seven others, 20 heads to 4, take 1145 us cut as 288 blocks and 171 as 68.
+// No split has less than one block of 32 tokens a wave, or four tiles (512 tokens
+// over 2048, 4 heads, fp32: 42 us with one, 30 with four, 36 with eight).  Short
+// calls of up to 512 tokens are not split: what the second launch costs is more
+// than it saves (32 heads, 300 tokens 9.0 us split, 7.4 not; 1023 tokens 12.1 and
+// 12.8).
+KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len) {
   KvAttnShape s;
   const int64_t rows = (int64_t)max_new * (heads / kv_heads);
   s.prompt = rows >= 64;
-  const int per = s.prompt ? kPromptRows : 16, tile = s.prompt ? kPromptTile : kWaves * kTile;
+  const int per = s.prompt ? kPromptRows : 16, tile = s.prompt ? 4 * kPromptTile : kWaves * kTile;
   const int64_t blocks = (rows + per - 1) / per;
   const int64_t pairs = (int64_t)seqs * kv_heads, room = ((int64_t)1 << 30) / pairs;  // of a launch's workgroups
   s.row_blocks = (int)(blocks > room ? (room < 1 ? 1 : room) : blocks);
-  const int64_t units = pairs * s.row_blocks, most = ((int64_t)max_len + tile - 1) / tile;
-  int64_t n = (s.prompt ? 512 : 1024) / units;
+  // blocks with rows: no more than the batch's tokens fill, and one more a sequence
+  const int64_t filled = (int64_t)tokens * (heads / kv_heads) / per + seqs, all = (int64_t)seqs * s.row_blocks;
+  const int64_t units = kv_heads * (filled < all ? filled : all), most = ((int64_t)max_len + tile - 1) / tile;
+  int64_t n = (s.prompt && seqs < 8 ? 512 : 1024) / units;
   n = n > most ? most : n;
   if (!s.prompt && max_len <= 512) n = 1;
   s.splits = (int)(n < 1 ? 1 : n);

@@ -164,7 +164,7 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
 
 size_t moe_kv4_attention_workspace_bytes(const moe_kv4_batch *b, int heads, int max_new, int max_len) {
   if (check_batch(b) != MOE_OK || check_heads(b, heads) != MOE_OK || max_new < 1 || max_len < 1) return 0;
-  const int splits = kv4_attention_shape(b->seqs, b->kv_heads, heads, max_new, max_len).splits;
+  const int splits = kv4_attention_shape(b->seqs, b->kv_heads, heads, b->tokens, max_new, max_len).splits;
   return splits == 1 ? 0 : (size_t)splits * b->tokens * heads * (b->head_dim + 2) * sizeof(float);
 }
 
@@ -188,7 +188,7 @@ int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, v
   a.o_stride = o_stride;
   a.scale = scale;
   a.heads = heads;
-  const KvAttnShape shape = kv4_attention_shape(b->seqs, b->kv_heads, heads, max_new, max_len);
+  const KvAttnShape shape = kv4_attention_shape(b->seqs, b->kv_heads, heads, b->tokens, max_new, max_len);
   a.splits = shape.splits;
   a.row_blocks = shape.row_blocks;
   a.prompt = shape.prompt;
