@@ -476,7 +476,8 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
 
 /* Attention of every new token over its sequence's cache, itself and what is
  * before it: o[t][h] = sum_j softmax_j(scale q[t][h] . K[j][h']) V[j][h'], h'
- * = h / (heads / kv_heads); heads a multiple of kv_heads.  A row that sees no
+ * = h / (heads / kv_heads); heads a multiple of kv_heads, at most 2^30 tokens
+ * times heads and sequences times kv_heads.  A row that sees no
  * token gets zeros.  What a row does not see does not reach it, NaN included.
  * max_new (new tokens of a sequence) and max_len (tokens of a sequence) say how
  * the work is best cut; results are right whatever they are.  The workspace

@@ -892,11 +892,12 @@ KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int tokens, i
   const int64_t rows = (int64_t)max_new * (heads / kv_heads);
   s.prompt = rows >= 64;
   const int per = s.prompt ? kPromptRows : 16, tile = s.prompt ? 4 * kPromptTile : kWaves * kTile;
-  const int64_t blocks = (rows + per - 1) / per;
+  const int64_t full = (int64_t)tokens * (heads / kv_heads);   // rows, were they all of one sequence
+  const int64_t blocks = ((rows < full ? rows : full) + per - 1) / per;
   const int64_t pairs = (int64_t)seqs * kv_heads, room = ((int64_t)1 << 30) / pairs;  // of a launch's workgroups
-  s.row_blocks = (int)(blocks > room ? (room < 1 ? 1 : room) : blocks);
+  s.row_blocks = (int)(blocks < 1 || room < 1 ? 1 : blocks > room ? room : blocks);
   // blocks with rows: no more than the batch's tokens fill, and one more a sequence
-  const int64_t filled = (int64_t)tokens * (heads / kv_heads) / per + seqs, all = (int64_t)seqs * s.row_blocks;
+  const int64_t filled = full / per + seqs, all = (int64_t)seqs * s.row_blocks;
   const int64_t units = kv_heads * (filled < all ? filled : all), most = ((int64_t)max_len + tile - 1) / tile;
   int64_t n = (s.prompt && seqs < 8 ? 512 : 1024) / units;
   n = n > most ? most : n;

@@ -178,8 +178,8 @@ int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, v
   CHECK(check_rows("q", q, q_stride, (int64_t)heads * d, bytes, 16));
   CHECK(check_rows("o", o, o_stride, (int64_t)heads * d, bytes, 16));
   if (max_new < 1 || max_len < 1) return fail(MOE_ERR_ARG, "max_new and max_len must be >= 1");
-  if (product(b->seqs, b->kv_heads) >= (int64_t)1 << 31 || product(b->tokens, heads, d / 4) >= (int64_t)256 << 31)
-    return fail(MOE_ERR_ARG, "too many sequences or tokens times heads");
+  if (product(b->seqs, b->kv_heads) > (int64_t)1 << 30 || product(b->tokens, heads) > (int64_t)1 << 30)
+    return fail(MOE_ERR_ARG, "sequences times kv_heads and tokens times heads must be at most 2^30");
   KvAttnArgs a;
   a.kv = kv_of(b);
   a.q = q;

@@ -97,8 +97,11 @@ class DecoderStack:
     def step(self, H: torch.Tensor, batch: dict, snapshots: Optional[torch.Tensor] = None) -> None:
         """The batch's new tokens H [tokens][d_model] (fp32, device) through all
         layers, in place.  snapshots (optional, [layers][2][tokens][d_model])
-        receives h entering and leaving every attention block."""
+        receives h entering and leaving every attention block.  The work is only
+        enqueued, on moe.compute: moe.sync() waits for it."""
         moe = self.moe
+        for t in (H, batch["page_table"], batch["q_start"], batch["kv_len"]):
+            t.record_stream(moe.compute)   # the caller may let go of them before it is done
         moe.compute.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(moe.compute):
             for l in range(moe.L):

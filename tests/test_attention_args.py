@@ -101,6 +101,15 @@ def test_attention_workspace():
     assert b.moe_kv4_attention_workspace_bytes(batch(), 3, 1, 4096) == 0
 
 
+def test_attention_limits():
+    # rows that an int could not count
+    big = batch(tokens=1 << 24)
+    refused(b.moe_kv4_attention, *attend(big, heads=128, qs=128 * 64, os=128 * 64, ws=P, wsb=1 << 60))
+    # hints far past the batch do not size the work past its tokens
+    small = b.moe_kv4_attention_workspace_bytes(batch(tokens=1), 4, 1 << 24, 1 << 29)
+    assert 0 < small <= 1024 * 4 * 66 * 4
+
+
 def norm(**kw):
     a = dict(h=P, hs=64, y=P, ys=64, gate=P, gs=0, post=P, pre=P, scale=1.0, eps=1e-5, ho=P, hos=64, x=P, xs=64, rows=3,
              d=64, dtype=BF16, stream=0)
