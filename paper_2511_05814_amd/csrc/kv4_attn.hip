@@ -68,10 +68,10 @@ __device__ __forceinline__ void add_pair(float v0, float v1, int i, half8 (&p)[P
 }
 
 // A row of q goes to fp16 times a power of two that brings its largest element
-// to 2^9 .. 2^10 (and the sign of the scale).  Its dot products times `unit`,
+// to 2^9 .. 2^10 (and the sign of the scale).  Its dot products times unit(),
 // exactly, are those of q and k, and times `down` the exponents of 2.
 struct RowScale {
-  float up, unit, down;
+  float up, down;
 };
 // |scale| log2(e), kept off zero so that a masked score is minus infinity in any scale
 __device__ __forceinline__ float exponent_factor(float scale) { return fmaxf(fabsf(scale) * kLog2e, 0x1p-50f); }
@@ -79,9 +79,12 @@ __device__ __forceinline__ RowScale row_scale(float amax, float scale) {
   const int exponent = min(max((int)(__float_as_uint(amax) >> 23) - 127, -60), 127);
   RowScale r;
   r.up = copysignf(ldexpf(1.0f, 9 - exponent), scale);
-  r.unit = ldexpf(1.0f, exponent - 9);
-  r.down = exponent_factor(scale) * r.unit;
+  r.down = exponent_factor(scale) * ldexpf(1.0f, exponent - 9);
   return r;
+}
+// The power of two in `down`, from the exponents alone (a register less in loops).
+__device__ __forceinline__ float unit(float down, float factor) {
+  return __uint_as_float((__float_as_uint(down) & 0x7F800000u) - (__float_as_uint(factor) & 0x7F800000u) + 0x3F800000u);
 }
 
 // scale(k), which fp16 holds exactly; NaN for the mark of a group that could not be stored
@@ -268,7 +271,7 @@ __device__ __forceinline__ Seq sequence(const KvAttnArgs &a, int b, int group) {
 // are exact in fp16; q (and p, in fp32 calls) is one fp16 number or, for fp32
 // calls, the sum of two.
 template <int D, typename T>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attention_kernel(KvAttnArgs a) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void kv4_attention_kernel(KvAttnArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
   constexpr int KW = D / 32;   // words of codes of a lane's part of a key, steps of the dot product
   constexpr int NU = D / 16;   // output blocks of 16 dimensions
@@ -344,24 +347,32 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
       next_held[h] = page[h] >= 0 && page[h] < a.kv.pages;
       return a.kv.pool + ((size_t)(next_held[h] ? page[h] : 0) * a.kv.kv_heads + g) * page_bytes;
     };
+    // Offsets stay 32 bits wide, added to scalar bases; widened ahead of the loop
+    // they would take two registers each.
+    auto here = [](uint32_t offset) {
+      asm volatile("" : "+v"(offset));
+      return offset;
+    };
     auto fetch_keys = [&](int t0) {
+      const uint32_t ko = here(k_lane), mo = here(km_lane);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint8_t *rec = record(h);
         const uint32_t in = (t0 + 16 * h) & page_mask;
-        const uint8_t *kp = rec + in * (D / 2) + k_lane;
+        const uint8_t *kp = rec + in * (D / 2) + ko;
         if constexpr (KW == 4) *reinterpret_cast<u32x4 *>(kw[h]) = *reinterpret_cast<const u32x4 *>(kp);
         else *reinterpret_cast<u32x2 *>(kw[h]) = *reinterpret_cast<const u32x2 *>(kp);
-        km[h] = *reinterpret_cast<const uint16_t *>(rec + in * (D / 16) + km_lane);
+        km[h] = *reinterpret_cast<const uint16_t *>(rec + in * (D / 16) + mo);
       }
     };
     auto fetch_values = [&](int t0) {
+      const uint32_t vo = here(v_lane), mo = here(vm_lane);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint8_t *rec = record(h);
         const uint32_t in = (t0 + 16 * h) & page_mask;
-        vw[h] = *reinterpret_cast<const u32x4 *>(rec + in * (D / 2) + v_lane);
-        vm[h] = *reinterpret_cast<const u32x2 *>(rec + in * (D / 16) + vm_lane);
+        vw[h] = *reinterpret_cast<const u32x4 *>(rec + in * (D / 2) + vo);
+        vm[h] = *reinterpret_cast<const u32x2 *>(rec + in * (D / 16) + mo);
       }
     };
     // D 64: lanes 8 .. 15 of a row take dimensions 4 .. 7 of their octet
@@ -472,7 +483,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void kv4_attentio
         *reinterpret_cast<float4 *>(&s_o[wave][r][dim + u]) = make_float4(o[u][i], o[u + 1][i], o[u + 2][i], o[u + 3][i]);
     }
     if (j == 0) {
-      s_ml[wave][r][0] = m * rs.unit;
+      s_ml[wave][r][0] = m * unit(down, factor);
       s_ml[wave][r][1] = l;
     }
     __syncthreads();
@@ -785,7 +796,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
       }
     }
     if (a.splits > 1 && hi == 0) {
-      a.ml[2 * at] = m * rs.unit;
+      a.ml[2 * at] = m * unit(rs.down, exponent_factor(a.scale));
       a.ml[2 * at + 1] = l;
     }
   }
