@@ -737,21 +737,26 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
         for (int u = 0; u < NB; ++u) o[u] *= keep;
       }
       const float ref = m == -__builtin_inff() ? 0.0f : m;
+      // probabilities of the next 16 tokens ahead of the products of these
+      half8 p[4][PARTS];
+      auto weigh = [&](int part) {
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+        for (int e = 0; e < 8; e += 2)
+          add_pair<PARTS>(power<PARTS>(s[part / 2][8 * (part % 2) + e], ref, rs.down), power<PARTS>(s[part / 2][8 * (part % 2) + e + 1], ref, rs.down), e,
+                          p[part], l);
+      };
+      weigh(0);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          half8 v[NB], p[PARTS];
+      for (int part = 0; part < 4; ++part) {
+        half8 v[NB];
 #pragma unroll
-          for (int u = 0; u < NB; ++u) v[u] = *reinterpret_cast<const half8 *>(from + 2 * KB + x * KB + u * 2048 + h * 1024 + lane * 16);
+        for (int u = 0; u < NB; ++u) v[u] = *reinterpret_cast<const half8 *>(from + 2 * KB + part / 2 * KB + u * 2048 + part % 2 * 1024 + lane * 16);
+        if (part < 3) weigh(part + 1);
 #pragma unroll
-          for (int e = 0; e < 8; e += 2)
-            add_pair<PARTS>(power<PARTS>(s[x][8 * h + e], ref, rs.down), power<PARTS>(s[x][8 * h + e + 1], ref, rs.down), e, p, l);
+        for (int n = PARTS - 1; n >= 0; --n)
 #pragma unroll
-          for (int part = PARTS - 1; part >= 0; --part)
-#pragma unroll
-            for (int u = 0; u < NB; ++u) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[u], p[part], o[u], 0, 0, 0);
-        }
+          for (int u = 0; u < NB; ++u) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[u], p[part][n], o[u], 0, 0, 0);
+      }
       // Groups marked as not stored: counted for the rows that see them, as in
       // the kernel above.
       if (any & 1) {
