@@ -213,8 +213,8 @@ __device__ __forceinline__ float sum_over_j(float v) {
 // which see most, first, so that the longest work starts first; the sequences of
 // a block rotate with it, or one in four, long, would put all of its work on one
 // engine of each XCD (prompts of 2048 tokens over 2048 and three shorter ones:
-// 682 us so, 188 with the blocks of a sequence one after another, 183 as it is;
-// measured before the steps that came after).
+// 682 us so, 188 with the blocks of a sequence one after another, 183 as it is,
+// all three before the products were reordered, since when it takes 166).
 struct Place {
   int split, block, seq, kv_head;
 };
@@ -270,6 +270,10 @@ __device__ __forceinline__ Seq sequence(const KvAttnArgs &a, int b, int group) {
 // lanes, and the rows' maxima and sums rescale lane-locally.  Keys and values
 // are exact in fp16; q (and p, in fp32 calls) is one fp16 number or, for fp32
 // calls, the sum of two.
+// It reads the cache once; the vector instructions that expand it (about 360 a
+// wave and block) and the latency of its loads bound it before HBM does: 32
+// sequences of up to 4096 tokens, 91 MB, in 29 us (3.1 TB/s), one of 131072, 151
+// MB, in 40 us with the join (3.7 TB/s).
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void kv4_attention_kernel(KvAttnArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
@@ -535,6 +539,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void 
 // which is the operand of O^T = V^T P^T when its sum takes the tokens in that
 // order.  Two tiles of LDS, one barrier a tile; the bytes of the tile after
 // next are on their way to registers.
+// Vector instructions bound it (an exponential a score, the expansion), which
+// little of the matrix work runs beside: four prompts of up to 2048 tokens over
+// 2048, 32 heads to 8, 103 GFLOP, in 166 us, 620 TFLOP/s.
 constexpr int kPromptTile = 64, kPromptRows = 128;
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_kernel(KvAttnArgs a) {
@@ -892,10 +899,12 @@ void launch(const KvAttnArgs &a, hipStream_t s) {
 }  // namespace
 
 // Rows in blocks of 16, or of 128 from 64 rows a sequence and kv head on.  Enough
-// workgroups for four on each of the 256 compute units, two with large blocks
-// (four from eight sequences on, whose lengths differ: 45 sequences of up to 67
-// new tokens over 22502, us with two / four / eight: 238 / 152 / 122; 11 of 32
-// over 23050: 151 / 89 / 99; 3 of 100 over 6000: 55 / 60 / 79).  What counts are
+// workgroups for four on each of the 256 compute units, two with large blocks,
+// or again four from eight sequences on, whose lengths differ, as long as a split
+// keeps 768 tokens (us with two / with four: a third of 11 sequences with 32 new
+// tokens over up to 23050, 32 heads to 4, 154 / 115; of 4096, 32 heads to 8, half
+// of 24 with 256 new ones 243 / 237 and all of 24 with 24 97 / 93, but all of 8
+// with 24 44 / 57; below eight, 3 with up to 100 over 6000: 55 / 60).  What counts are
 // blocks that can have rows: 215 tokens of one sequence of 28854 and single ones
 // of seven others, 20 heads to 4, take 1145 us cut as 288 blocks and 171 as 68.
 // No split has less than one block of 32 tokens a wave, or four tiles (512 tokens
@@ -915,7 +924,12 @@ KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int tokens, i
   // blocks with rows: no more than the batch's tokens fill, and one more a sequence
   const int64_t filled = full / per + seqs, all = (int64_t)seqs * s.row_blocks;
   const int64_t units = kv_heads * (filled < all ? filled : all), most = ((int64_t)max_len + tile - 1) / tile;
-  int64_t n = (s.prompt && seqs < 8 ? 512 : 1024) / units;
+  int64_t n = (s.prompt ? 512 : 1024) / units;
+  if (s.prompt && seqs >= 8) {  // finer, down to 768 tokens a split
+    const int64_t fine = 1024 / units, longest = max_len / 768;
+    const int64_t m = fine < longest ? fine : longest;
+    n = m > n ? m : n;
+  }
   n = n > most ? most : n;
   if (!s.prompt && max_len <= 512) n = 1;
   s.splits = (int)(n < 1 ? 1 : n);

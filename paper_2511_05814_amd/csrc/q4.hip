@@ -208,7 +208,9 @@ __global__ __launch_bounds__(kSmallWaves * kWave, MT == 1 ? 4 : 2) void q4_small
 // themselves and added to the result with the group's scale / 16, one fp32
 // fused multiply-add an element and group.  The next step's bytes are on their
 // way to registers while a step is multiplied; two LDS buffers, one barrier a
-// step.
+// step.  What bounds it is that expansion, LDS and products of a wave run mostly
+// one after another: 2037 rows by 6144 x 4096 in bf16 take 143 us, 720 TFLOP/s,
+// where a bf16 product of 8192 cubed reaches 1165.
 constexpr int kTileN = 128;
 
 // Sixteen codes as bf16 16 q - zero, in column order.
