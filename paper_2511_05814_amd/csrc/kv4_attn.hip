@@ -498,9 +498,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void 
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_ml[w][orow][0]);
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float f = s_ml[w][orow][0] == -__builtin_inff() ? (s_ml[w][orow][1] == 0.0f ? 0.0f : 1.0f)
-                                                             : __builtin_amdgcn_exp2f((s_ml[w][orow][0] - top) * factor);
-      if (f == 0.0f) continue;
+      // no sum: no tokens; one of NaN scores alone has no maximum.  A wave far
+      // below the others counts all the same: its NaN times 0 is NaN.
+      if (s_ml[w][orow][1] == 0.0f) continue;
+      const float f = s_ml[w][orow][0] == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((s_ml[w][orow][0] - top) * factor);
       total += s_ml[w][orow][1] * f;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) acc[e] += s_o[w][orow][dim + e] * f;

@@ -1,0 +1,53 @@
+"""Edges of the attention entry points on an MI355X: NaN and infinities, extreme
+scales, empty tensors, refusals, and the paths that only some shapes take.
+
+Tolerances are those of test_gpu_attention, derived there."""
+import numpy as np
+import pytest
+
+from oracle import attention as oa
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from tests._attention_rig import Batch  # noqa: E402
+from tests.test_gpu_attention import check_attention  # noqa: E402
+
+
+def change(bt, seq, pos, head, f):
+    """Runs f(record's parts, token) on the entry of position pos."""
+    page = bt.table[seq, pos // bt.P]
+    rec = [np.array(x) for x in oa.unpack_record(bt.pool[page, head], bt.P, bt.D)]
+    f(rec, pos % bt.P)
+    bt.pool[page, head] = oa.record(*rec)
+
+
+def mark(part):
+    """Marks the second group of a key (part 0) or a value (2) as not stored."""
+    def f(rec, at):
+        rec[part + 1][at, 1] = 255 << 8
+        rec[part][at, 32:64] = 0
+    return f
+
+
+def key_of(value):
+    def f(rec, at):
+        codes, metas = oa.kv4_quantize(np.full((1, rec[0].shape[1]), value))
+        rec[0][at], rec[1][at] = codes[0], metas[0]
+    return f
+
+
+@pytest.mark.parametrize("part", [0, 2])
+@pytest.mark.parametrize("max_len", [None, 1 << 20])   # one split and several
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("D", [64, 128])
+def test_marks_count_however_small_their_weight(D, new, max_len, part):
+    """A marked entry among tokens whose weights come to 0 beside those of one
+    key, some 600 powers of two above, that another wave or split has."""
+    bt = Batch([new, 1], [100, 40], 4, 2, D, 16, seed=21).fill(0.3)
+    change(bt, 0, 40, 0, key_of(30.0))
+    change(bt, 0, 5, 0, mark(part))
+    q = np.random.default_rng(3).standard_normal((bt.tokens, 4, D)) + 2
+    for dtype in ("f32", "bf16"):
+        o, want = check_attention(bt, dtype, q=q, max_len=max_len)
+        assert np.isnan(o[:new, :2]).any((1, 2)).all()
