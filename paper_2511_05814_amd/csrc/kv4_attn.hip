@@ -79,6 +79,8 @@ __device__ __forceinline__ RowScale row_scale(float amax, float scale) {
   const int exponent = min(max((int)(__float_as_uint(amax) >> 23) - 127, -60), 127);
   RowScale r;
   r.up = copysignf(ldexpf(1.0f, 9 - exponent), scale);
+  // a scale that is not finite makes every score that a row sees a NaN
+  if (!(fabsf(scale) < __builtin_inff())) r.up = __builtin_nanf("");
   r.down = exponent_factor(scale) * ldexpf(1.0f, exponent - 9);
   return r;
 }

@@ -11,7 +11,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from tests._attention_rig import Batch  # noqa: E402
-from tests.test_gpu_attention import check_attention  # noqa: E402
+from tests.test_gpu_attention import check_attention, host, ops  # noqa: E402
 
 
 def change(bt, seq, pos, head, f):
@@ -51,3 +51,13 @@ def test_marks_count_however_small_their_weight(D, new, max_len, part):
     for dtype in ("f32", "bf16"):
         o, want = check_attention(bt, dtype, q=q, max_len=max_len)
         assert np.isnan(o[:new, :2]).any((1, 2)).all()
+
+
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("scale", [np.nan, np.inf, -np.inf])
+def test_scales_that_are_not_finite_give_nan(scale, new):
+    """But zeros to a row that sees nothing."""
+    bt = Batch([new, 1], [300, 0], 4, 2, 64, 16, seed=22, short=1).fill(0.3)
+    for dtype in (torch.float32, torch.bfloat16):
+        o = host(ops().kv4_attention(torch.randn((bt.tokens, 4, 64), device="cuda").to(dtype), *bt.args(), scale))
+        assert np.isnan(o[:new]).all() and (o[new] == 0).all()
