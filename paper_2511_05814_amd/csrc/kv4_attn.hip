@@ -69,19 +69,23 @@ __device__ __forceinline__ void add_pair(float v0, float v1, int i, half8 (&p)[P
 
 // A row of q goes to fp16 times a power of two that brings its largest element
 // to 2^9 .. 2^10 (and the sign of the scale).  Its dot products times unit(),
-// exactly, are those of q and k, and times `down` the exponents of 2.
+// exactly, are those of q and k (unless `down` stops at an end), and times `down`
+// the exponents of 2.
 struct RowScale {
   float up, down;
 };
 // |scale| log2(e), kept off zero so that a masked score is minus infinity in any scale
-__device__ __forceinline__ float exponent_factor(float scale) { return fmaxf(fabsf(scale) * kLog2e, 0x1p-50f); }
+__device__ __forceinline__ float exponent_factor(float scale) { return fminf(fmaxf(fabsf(scale) * kLog2e, 0x1p-126f), 0x1p127f); }
+// Scales below fp32's normal range count as zero: every score is 0.  Scores are
+// below 2^32 (values below 2^15, up to 128 of them), so that `down` may stop at
+// 2^-100: less makes every difference of exponents nothing all the same.
 __device__ __forceinline__ RowScale row_scale(float amax, float scale) {
-  const int exponent = min(max((int)(__float_as_uint(amax) >> 23) - 127, -60), 127);
+  const int exponent = min(max((int)(__float_as_uint(amax) >> 23) - 127, -116), 127);
   RowScale r;
-  r.up = copysignf(ldexpf(1.0f, 9 - exponent), scale);
+  r.up = fabsf(scale) < 0x1p-126f ? 0.0f : copysignf(ldexpf(1.0f, 9 - exponent), scale);
   // a scale that is not finite makes every score that a row sees a NaN
   if (!(fabsf(scale) < __builtin_inff())) r.up = __builtin_nanf("");
-  r.down = exponent_factor(scale) * ldexpf(1.0f, exponent - 9);
+  r.down = fminf(fmaxf(exponent_factor(scale) * ldexpf(1.0f, exponent - 9), 0x1p-100f), 0x1p126f);
   return r;
 }
 // The power of two in `down`, from the exponents alone (a register less in loops).

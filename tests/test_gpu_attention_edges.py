@@ -61,3 +61,16 @@ def test_scales_that_are_not_finite_give_nan(scale, new):
     for dtype in (torch.float32, torch.bfloat16):
         o = host(ops().kv4_attention(torch.randn((bt.tokens, 4, 64), device="cuda").to(dtype), *bt.args(), scale))
         assert np.isnan(o[:new]).all() and (o[new] == 0).all()
+
+
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("scale,size", [(1e-20, 1e20), (-1e-30, 1e30), (1e-36, 1e36), (0.0, 1e25), (1e-36, 1e-10), (1e25, 1e-25),
+                                        (1e30, 1e-34)])
+@pytest.mark.parametrize("max_len", [None, 1 << 20])
+def test_scales_and_queries_of_any_size(scale, size, new, max_len):
+    """Scores are what counts, not how they divide between q and its scale; with
+    scale 0 every token weighs the same."""
+    bt = Batch([new, 1], [300, 20], 4, 2, 64, 16, seed=23).fill(0.3)
+    q = np.random.default_rng(4).standard_normal((bt.tokens, 4, 64)) * size
+    for dtype in ("f32", "bf16"):
+        check_attention(bt, dtype, q=q, scale=scale, max_len=max_len)
