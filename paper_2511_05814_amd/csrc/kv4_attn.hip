@@ -83,8 +83,10 @@ __device__ __forceinline__ RowScale row_scale(float amax, float scale) {
   const int exponent = min(max((int)(__float_as_uint(amax) >> 23) - 127, -116), 127);
   RowScale r;
   r.up = fabsf(scale) < 0x1p-126f ? 0.0f : copysignf(ldexpf(1.0f, 9 - exponent), scale);
-  // a scale that is not finite makes every score that a row sees a NaN
-  if (!(fabsf(scale) < __builtin_inff())) r.up = __builtin_nanf("");
+  // A scale that is not finite makes every score that a row sees a NaN, and so
+  // does an infinity in q: its scores are infinities or NaN, and where all of
+  // them are minus infinity the row would pass for one that sees nothing.
+  if (!(fabsf(scale) < __builtin_inff()) || amax == __builtin_inff()) r.up = __builtin_nanf("");
   r.down = fminf(fmaxf(exponent_factor(scale) * ldexpf(1.0f, exponent - 9), 0x1p-100f), 0x1p126f);
   return r;
 }

@@ -10,7 +10,7 @@ from oracle import attention as oa
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests._attention_rig import Batch  # noqa: E402
+from tests._attention_rig import Batch, device  # noqa: E402
 from tests.test_gpu_attention import check_attention, host, ops  # noqa: E402
 
 
@@ -74,3 +74,22 @@ def test_scales_and_queries_of_any_size(scale, size, new, max_len):
     q = np.random.default_rng(4).standard_normal((bt.tokens, 4, 64)) * size
     for dtype in ("f32", "bf16"):
         check_attention(bt, dtype, q=q, scale=scale, max_len=max_len)
+
+
+def alike(new, old, value, seed):
+    """A batch whose keys are all one value, and its values 1."""
+    bt = Batch(new, old, 4, 2, 64, 16, seed=seed)
+    bt.pool[:, :] = oa.record(*oa.kv4_quantize(np.full((16, 64), value)), *oa.kv4_quantize(np.ones((16, 64))))
+    return bt
+
+
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("value", [np.inf, -np.inf])
+def test_a_row_with_an_infinity_is_nan(value, new):
+    """Also where all of its scores are minus infinity."""
+    bt = alike([new, 2], [40, 30], 3.0, 24)
+    q = np.random.default_rng(5).standard_normal((bt.tokens, 4, 64)).astype(np.float32)
+    q[0, 1, 9] = value
+    for dtype in ("f32", "bf16"):
+        o = host(ops().kv4_attention(device(q, dtype), *bt.args(), 0.125))
+        assert np.isnan(o[0, 1]).all() and np.isnan(o).sum() == 64
