@@ -479,6 +479,9 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
  * = h / (heads / kv_heads); heads a multiple of kv_heads, at most 2^30 tokens
  * times heads and sequences times kv_heads.  A row that sees no
  * token gets zeros.  What a row does not see does not reach it, NaN included.
+ * A row of q with an infinity or a NaN, or a scale that is not finite, gives NaN
+ * to what sees a token; a scale below fp32's normal range counts as 0.  Where q . K
+ * passes fp32's range a row may come out as NaN.
  * max_new (new tokens of a sequence) and max_len (tokens of a sequence) say how
  * the work is best cut; results are right whatever they are.  The workspace
  * (16-byte aligned; NULL if it is 0 bytes) must hold

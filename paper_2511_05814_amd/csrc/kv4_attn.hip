@@ -95,6 +95,14 @@ __device__ __forceinline__ float unit(float down, float factor) {
   return __uint_as_float((__float_as_uint(down) & 0x7F800000u) - (__float_as_uint(factor) & 0x7F800000u) + 0x3F800000u);
 }
 
+// A row's largest dot product as the joins compare it.  Past fp32's range there is
+// no telling parts of a row apart: the sum becomes a NaN.
+__device__ __forceinline__ float joined_max(float m, float unit, float &l) {
+  const float v = m * unit;
+  if (fabsf(v) == __builtin_inff() && fabsf(m) < __builtin_inff()) l = __builtin_nanf("");
+  return v;
+}
+
 // scale(k), which fp16 holds exactly; NaN for the mark of a group that could not be stored
 __device__ __forceinline__ float meta_scale(uint32_t meta) {
   const uint32_t k = meta >> 8;
@@ -495,7 +503,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void 
         *reinterpret_cast<float4 *>(&s_o[wave][r][dim + u]) = make_float4(o[u][i], o[u + 1][i], o[u + 2][i], o[u + 3][i]);
     }
     if (j == 0) {
-      s_ml[wave][r][0] = m * unit(down, factor);
+      s_ml[wave][r][0] = joined_max(m, unit(down, factor), l);
       s_ml[wave][r][1] = l;
     }
     __syncthreads();
@@ -817,7 +825,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
       }
     }
     if (a.splits > 1 && hi == 0) {
-      a.ml[2 * at] = m * unit(rs.down, exponent_factor(a.scale));
+      a.ml[2 * at] = joined_max(m, unit(rs.down, exponent_factor(a.scale)), l);
       a.ml[2 * at + 1] = l;
     }
   }

@@ -93,3 +93,23 @@ def test_a_row_with_an_infinity_is_nan(value, new):
     for dtype in ("f32", "bf16"):
         o = host(ops().kv4_attention(device(q, dtype), *bt.args(), 0.125))
         assert np.isnan(o[0, 1]).all() and np.isnan(o).sum() == 64
+
+
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("max_len", [None, 1 << 20])
+@pytest.mark.parametrize("size", [-1e37, 1e37])
+def test_dot_products_past_fp32(size, new, max_len):
+    """One key takes all the weight; where parts of the row are joined by their
+    largest dot products, which fp32 does not hold, NaN, and nothing else."""
+    bt = alike([new, 2], [400, 30], 300.0, 25)
+    change(bt, 0, 5, 0, key_of(100.0 if size < 0 else 900.0))
+    def seven(rec, at):
+        codes, metas = oa.kv4_quantize(np.full((1, 64), 7.0))
+        rec[2][at], rec[3][at] = codes[0], metas[0]
+    change(bt, 0, 5, 0, seven)
+    q = np.random.default_rng(5).standard_normal((bt.tokens, 4, 64)).astype(np.float32)
+    q[0, 1] = size
+    for dtype in ("f32", "bf16"):
+        o = host(ops().kv4_attention(device(q, dtype), *bt.args(), 0.125, max_len=max_len))
+        assert np.isnan(o[0, 1]).all() or (o[0, 1] == 7).all()
+        assert np.isnan(o).sum() == np.isnan(o[0, 1]).sum()
