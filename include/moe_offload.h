@@ -408,8 +408,9 @@ int moe_probe_mfma_bf16(int shape, int iters, void *stream, double *tflops);
  * fp32 operands take part whole (no rounding to bf16).  Strides are in
  * elements between rows (tokens); a row itself is contiguous.  Pointers and
  * strides must be multiples of 16 bytes unless said otherwise.  With no rows
- * (tokens) a call checks its arguments and does nothing.  MOE_ERR_ARG: a bad
- * argument (moe_last_error says which); MOE_ERR_HIP: a launch failed. */
+ * (tokens) a call checks its arguments and does nothing; operands that have no
+ * elements then may be NULL.  MOE_ERR_ARG: a bad argument (moe_last_error says
+ * which); MOE_ERR_HIP: a launch failed. */
 
 /* Bytes of one 4-bit matrix [n x k]; 0 unless n >= 1 and k is a positive
  * multiple of 64.  Three planes back to back: codes [n][k/2] bytes (column c in

@@ -20,9 +20,10 @@ int check_dtype(int dtype) {
   return MOE_OK;
 }
 
-// A row-strided operand: non-NULL, rows of `width` elements of `bytes` bytes, aligned to `align`.
-int check_rows(const char *name, const void *p, int64_t stride, int64_t width, int bytes, int align) {
-  if (!p || misaligned(p, align)) return fail(MOE_ERR_ARG, "%s must be a non-NULL device pointer aligned to %d bytes", name, align);
+// A row-strided operand: rows of `width` elements of `bytes` bytes, aligned to
+// `align`, and non-NULL (a tensor without elements has no address) if there are rows.
+int check_rows(const char *name, const void *p, int64_t stride, int64_t width, int bytes, int align, int rows) {
+  if ((!p && rows) || misaligned(p, align)) return fail(MOE_ERR_ARG, "%s must be a non-NULL device pointer aligned to %d bytes", name, align);
   if (stride < width || stride > (int64_t)1 << 40) return fail(MOE_ERR_ARG, "%s: a stride of %lld for rows of %lld", name, (long long)stride, (long long)width);
   if (stride * bytes % align) return fail(MOE_ERR_ARG, "%s: its stride must be a multiple of %d bytes", name, align);
   return MOE_OK;
@@ -96,8 +97,8 @@ int moe_q4_matmul(const void *x, int64_t x_stride, const void *w, void *y, int64
   if (n < 1 || n > 1 << 24) return fail(MOE_ERR_ARG, "n must be in [1, 2^24]");
   if (k < 64 || k % 64 || k > 1 << 20) return fail(MOE_ERR_ARG, "k must be a multiple of 64 in [64, 2^20]");
   if (!w || misaligned(w, 16)) return fail(MOE_ERR_ARG, "w must be a non-NULL 16-byte aligned device pointer");
-  CHECK(check_rows("x", x, x_stride, k, element(dtype), 16));
-  CHECK(check_rows("y", y, y_stride, n, element(dtype), element(dtype)));
+  CHECK(check_rows("x", x, x_stride, k, element(dtype), 16, rows));
+  CHECK(check_rows("y", y, y_stride, n, element(dtype), element(dtype), rows));
   if (rows == 0) return MOE_OK;
   Q4Args a;
   a.x = x;
@@ -120,15 +121,15 @@ int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, cons
   CHECK(check_dtype(dtype));
   CHECK(check_heads(b, heads));
   const int bytes = element(dtype), d = b->head_dim;
-  CHECK(check_rows("q", q, q_stride, (int64_t)heads * d, bytes, 16));
-  CHECK(check_rows("k", k, k_stride, (int64_t)b->kv_heads * d, bytes, 16));
-  CHECK(check_rows("v", v, v_stride, (int64_t)b->kv_heads * d, bytes, 16));
-  CHECK(check_rows("q_out", q_out, q_out_stride, (int64_t)heads * d, bytes, 16));
+  CHECK(check_rows("q", q, q_stride, (int64_t)heads * d, bytes, 16, b->tokens));
+  CHECK(check_rows("k", k, k_stride, (int64_t)b->kv_heads * d, bytes, 16, b->tokens));
+  CHECK(check_rows("v", v, v_stride, (int64_t)b->kv_heads * d, bytes, 16, b->tokens));
+  CHECK(check_rows("q_out", q_out, q_out_stride, (int64_t)heads * d, bytes, 16, b->tokens));
   if (rot_dim < 0 || rot_dim > d || rot_dim % 16) return fail(MOE_ERR_ARG, "rot_dim must be a multiple of 16 in [0, head_dim], not %d", rot_dim);
   if (max_pos < 1) return fail(MOE_ERR_ARG, "max_pos must be >= 1");
   if (rot_dim && (!cos || !sin || misaligned(cos, 16) || misaligned(sin, 16)))
     return fail(MOE_ERR_ARG, "cos and sin must be non-NULL 16-byte aligned device pointers");
-  if (rot_dim && q_out == q) return fail(MOE_ERR_ARG, "q_out may be q only without rotation");
+  if (rot_dim && b->tokens && q_out == q) return fail(MOE_ERR_ARG, "q_out may be q only without rotation");
   if (product(b->tokens, heads + 2 * b->kv_heads, d / 8) >= (int64_t)256 << 31) return fail(MOE_ERR_ARG, "too many tokens times heads");
   if (b->tokens == 0) return MOE_OK;
   KvAppendArgs a;
@@ -152,7 +153,7 @@ int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, cons
 int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stream) {
   CHECK(check_batch(b));
   CHECK(check_dtype(dtype));
-  if (!k || !v || misaligned(k, 16) || misaligned(v, 16)) return fail(MOE_ERR_ARG, "k and v must be non-NULL 16-byte aligned device pointers");
+  if ((b->tokens && (!k || !v)) || misaligned(k, 16) || misaligned(v, 16)) return fail(MOE_ERR_ARG, "k and v must be non-NULL 16-byte aligned device pointers");
   if (product(b->tokens, 2 * b->kv_heads, b->head_dim / 8) >= (int64_t)256 << 31) return fail(MOE_ERR_ARG, "too many tokens times heads");
   if (b->tokens == 0) return MOE_OK;
   KvReadArgs a;
@@ -175,8 +176,8 @@ int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, v
   CHECK(check_dtype(dtype));
   CHECK(check_heads(b, heads));
   const int bytes = element(dtype), d = b->head_dim;
-  CHECK(check_rows("q", q, q_stride, (int64_t)heads * d, bytes, 16));
-  CHECK(check_rows("o", o, o_stride, (int64_t)heads * d, bytes, 16));
+  CHECK(check_rows("q", q, q_stride, (int64_t)heads * d, bytes, 16, b->tokens));
+  CHECK(check_rows("o", o, o_stride, (int64_t)heads * d, bytes, 16, b->tokens));
   if (max_new < 1 || max_len < 1) return fail(MOE_ERR_ARG, "max_new and max_len must be >= 1");
   if (product(b->seqs, b->kv_heads) > (int64_t)1 << 30 || product(b->tokens, heads) > (int64_t)1 << 30)
     return fail(MOE_ERR_ARG, "sequences times kv_heads and tokens times heads must be at most 2^30");
@@ -209,15 +210,15 @@ int moe_norm_residual(const float *h, int64_t h_stride, const void *y, int64_t y
   if (rows < 0 || rows > 1 << 24) return fail(MOE_ERR_ARG, "rows must be in [0, 2^24]");
   if (d < 8 || d % 8 || d > 16384) return fail(MOE_ERR_ARG, "d must be a multiple of 8 in [8, 16384]");
   const int bytes = element(dtype);
-  CHECK(check_rows("h", h, h_stride, d, 4, 16));
-  if (y) CHECK(check_rows("y", y, y_stride, d, bytes, 16));
-  if (!y && (gate || post)) return fail(MOE_ERR_ARG, "gate and post need y");
-  if (gate && gate_stride) CHECK(check_rows("gate", gate, gate_stride, d, 4, 16));
+  CHECK(check_rows("h", h, h_stride, d, 4, 16, rows));
+  if (y) CHECK(check_rows("y", y, y_stride, d, bytes, 16, rows));
+  if (!y && rows && (gate || post)) return fail(MOE_ERR_ARG, "gate and post need y");
+  if (gate && gate_stride) CHECK(check_rows("gate", gate, gate_stride, d, 4, 16, rows));
   if (misaligned(gate, 16) || misaligned(post, 16) || misaligned(pre, 16)) return fail(MOE_ERR_ARG, "gate, post and pre must be 16-byte aligned");
-  if (!h_out && !x_out) return fail(MOE_ERR_ARG, "neither h_out nor x_out is wanted");
-  if (h_out) CHECK(check_rows("h_out", h_out, h_out_stride, d, 4, 16));
-  if (x_out) CHECK(check_rows("x_out", x_out, x_stride, d, bytes, 16));
-  if (h_out == h && h_out_stride != h_stride) return fail(MOE_ERR_ARG, "h_out on h needs the same stride");
+  if (!h_out && !x_out && rows) return fail(MOE_ERR_ARG, "neither h_out nor x_out is wanted");
+  if (h_out) CHECK(check_rows("h_out", h_out, h_out_stride, d, 4, 16, rows));
+  if (x_out) CHECK(check_rows("x_out", x_out, x_stride, d, bytes, 16, rows));
+  if (h_out && h_out == h && h_out_stride != h_stride) return fail(MOE_ERR_ARG, "h_out on h needs the same stride");
   if (x_out && x_out == y && x_stride != y_stride) return fail(MOE_ERR_ARG, "x_out on y needs the same stride");
   if (rows == 0) return MOE_OK;
   NormArgs a;

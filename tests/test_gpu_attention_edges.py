@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 
 from oracle import attention as oa
+from paper_2511_05814_amd import binding as b
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -113,3 +114,29 @@ def test_dot_products_past_fp32(size, new, max_len):
         o = host(ops().kv4_attention(device(q, dtype), *bt.args(), 0.125, max_len=max_len))
         assert np.isnan(o[0, 1]).all() or (o[0, 1] == 7).all()
         assert np.isnan(o).sum() == np.isnan(o[0, 1]).sum()
+
+
+def test_tensors_without_rows():
+    """Real empty tensors, which have no address."""
+    a = ops()
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.zeros((3, 64), dtype=dtype, device="cuda")
+        w = torch.zeros(b.moe_q4_matrix_bytes(8, 64), dtype=torch.uint8, device="cuda")
+        for empty in (x[:0], torch.empty((0, 64), dtype=dtype, device="cuda")):
+            y = a.q4_matmul(empty, w, 8)
+            assert y.shape == (0, 8) and y.dtype == dtype
+            h = torch.empty((0, 64), device="cuda")
+            v = torch.ones(64, device="cuda")
+            for gate in (None, v, h):
+                ho, xo = a.norm_residual(h, empty, gate=gate, post=v, pre=v)
+                assert ho.shape == xo.shape == (0, 64) and xo.dtype == dtype
+            assert a.norm_residual(h, pre=v, h_out=h, want_x=False)[0] is h
+        bt = Batch([0, 0], [3, 0], 4, 2, 64, 16)
+        args = bt.args()
+        q, k = (torch.empty((0, n, 64), dtype=dtype, device="cuda") for n in (4, 2))
+        cos = torch.ones((8, 32), device="cuda")
+        before = args[0].clone()
+        q = a.kv4_append(q, k, k, cos, cos, *args)
+        o = a.kv4_attention(q, *args, 0.125)
+        assert q.shape == o.shape == (0, 4, 64) and torch.equal(args[0], before)
+        assert [t.shape for t in a.kv4_read(*args, 0, 64, dtype)] == [(0, 2, 64)] * 2
