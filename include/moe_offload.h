@@ -409,8 +409,10 @@ int moe_probe_mfma_bf16(int shape, int iters, void *stream, double *tflops);
  * elements between rows (tokens); a row itself is contiguous.  Pointers and
  * strides must be multiples of 16 bytes unless said otherwise.  With no rows
  * (tokens) a call checks its arguments and does nothing; operands that have no
- * elements then may be NULL.  MOE_ERR_ARG: a bad argument (moe_last_error says
- * which); MOE_ERR_HIP: a launch failed. */
+ * elements then may be NULL.  What a call writes must not overlap what it reads
+ * or writes besides, to the element (slices of one buffer may alternate), but for
+ * the cases said below.  MOE_ERR_ARG: a bad argument (moe_last_error says which);
+ * MOE_ERR_HIP: a launch failed. */
 
 /* Bytes of one 4-bit matrix [n x k]; 0 unless n >= 1 and k is a positive
  * multiple of 64.  Three planes back to back: codes [n][k/2] bytes (column c in
@@ -465,7 +467,7 @@ typedef struct {
  * [max_pos][rot_dim/2], contiguous; rot_dim a multiple of 16, 0 for no
  * rotation (cos and sin may then be NULL; max_pos still counts).  A token at a
  * position past max_pos - 1 is not stored and its query is zeros.  q_out may be
- * q itself only without rotation.  Other bytes of the cache stay as they are. */
+ * q itself (at its stride) only without rotation.  Other bytes of the cache stay as they are. */
 int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                    const void *v, int64_t v_stride, const float *cos, const float *sin, int max_pos, int rot_dim,
                    void *q_out, int64_t q_out_stride, int heads, int dtype, void *stream);
@@ -482,7 +484,7 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
  * token gets zeros.  What a row does not see does not reach it, NaN included.
  * A row of q with an infinity or a NaN, or a scale that is not finite, gives NaN
  * to what sees a token; a scale below fp32's normal range counts as 0.  Where q . K
- * passes fp32's range a row may come out as NaN.
+ * passes fp32's range a row may come out as NaN.  o may be q itself, at its stride.
  * max_new (new tokens of a sequence) and max_len (tokens of a sequence) say how
  * the work is best cut; results are right whatever they are.  The workspace
  * (16-byte aligned; NULL if it is 0 bytes) must hold
@@ -501,7 +503,8 @@ int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, v
  * next block's input (dtype), h_out fp32.  post and pre are fp32 [d], gate fp32
  * [d] (gate_stride 0) or [rows][d].  May be NULL: y (h_out = residual_scale *
  * h), post (y' = y), gate (1), pre (1), h_out or x_out (not wanted; not both).
- * h_out may be h, and x_out y, at the same stride. */
+ * h_out may be h, and x_out y, at the same stride (or any other operand of their
+ * element size, row by row; h_out not pre). */
 int moe_norm_residual(const float *h, int64_t h_stride, const void *y, int64_t y_stride, const float *gate,
                       int64_t gate_stride, const float *post, const float *pre, float residual_scale, float eps,
                       float *h_out, int64_t h_out_stride, void *x_out, int64_t x_stride, int rows, int d, int dtype,

@@ -35,6 +35,50 @@ int launched(hipError_t e, const char *what) {
   return e == hipSuccess ? MOE_OK : fail(MOE_ERR_HIP, "%s failed: %s", what, hipGetErrorString(e));
 }
 
+// `rows` stretches of memory of `width` bytes each, `stride` bytes apart.
+struct Span {
+  const void *at;
+  int64_t stride, width, rows;
+};
+Span rows_of(const void *p, int64_t stride, int64_t width, int bytes, int64_t rows) { return Span{p, stride * bytes, width * bytes, rows}; }
+Span block_of(const void *p, int64_t bytes) { return Span{p, bytes, bytes, 1}; }
+Span pool_of(const moe_kv4_batch *b) {
+  return rows_of(b->pool, (int64_t)b->kv_heads * b->page_size * b->head_dim * 9 / 8, (int64_t)b->kv_heads * b->page_size * b->head_dim * 9 / 8, 1, b->pages);
+}
+
+// Whether two spans share a byte: row i of a begins at i a.stride, row j of b at
+// d + j b.stride.
+bool share(const Span &a, const Span &b) {
+  typedef __int128 Wide;
+  if (!a.at || !b.at || a.rows < 1 || b.rows < 1) return false;
+  const Wide d = (Wide)(uintptr_t)b.at - (Wide)(uintptr_t)a.at;
+  if (d >= (Wide)a.stride * (a.rows - 1) + a.width || d + (Wide)b.stride * (b.rows - 1) + b.width <= 0) return false;
+  if (a.rows > b.rows) return share(b, a);
+  auto floor_div = [](Wide x, Wide y) { return x / y - (x % y < 0 ? 1 : 0); };
+  if (a.stride == b.stride) {
+    // rows are no wider than the stride: row j of b can meet rows j + k and j + k + 1 of a
+    const Wide k = floor_div(d, a.stride), rest = d - k * a.stride;
+    return (rest < a.width && k < a.rows && -k < b.rows) || (rest + b.width > a.stride && k + 1 < a.rows && -k - 1 < b.rows);
+  }
+  for (int64_t i = 0; i < a.rows; ++i) {
+    // the first row of b that ends after row i's start, the last that begins before its end
+    const Wide start = (Wide)a.stride * i - d;
+    const Wide first = floor_div(start - b.width, b.stride) + 1, last = floor_div(start + a.width - 1, b.stride);
+    if ((first < 0 ? 0 : first) <= (last < b.rows ? last : b.rows - 1)) return true;
+  }
+  return false;
+}
+bool exactly(const Span &a, const Span &b) {
+  return a.at == b.at && a.width == b.width && a.rows == b.rows && (a.rows == 1 || a.stride == b.stride);
+}
+
+// What is written may not overlap what other threads of the launch read, unless
+// `in_place`: each element is then read before its own thread writes it.
+int check_apart(const char *out, const Span &o, const char *in, const Span &i, bool in_place = false) {
+  if (!share(o, i) || (in_place && exactly(o, i))) return MOE_OK;
+  return fail(MOE_ERR_ARG, "%s overlaps %s", out, in);
+}
+
 int check_batch(const moe_kv4_batch *b) {
   if (!b) return fail(MOE_ERR_ARG, "NULL batch");
   if (b->head_dim != 64 && b->head_dim != 128) return fail(MOE_ERR_ARG, "head_dim must be 64 or 128, not %d", b->head_dim);
@@ -100,6 +144,9 @@ int moe_q4_matmul(const void *x, int64_t x_stride, const void *w, void *y, int64
   CHECK(check_rows("x", x, x_stride, k, element(dtype), 16, rows));
   CHECK(check_rows("y", y, y_stride, n, element(dtype), element(dtype), rows));
   if (rows == 0) return MOE_OK;
+  const Span to = rows_of(y, y_stride, n, element(dtype), rows);
+  CHECK(check_apart("y", to, "x", rows_of(x, x_stride, k, element(dtype), rows)));
+  CHECK(check_apart("y", to, "w", block_of(w, (int64_t)moe_q4_matrix_bytes(n, k))));
   Q4Args a;
   a.x = x;
   a.y = y;
@@ -129,9 +176,25 @@ int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, cons
   if (max_pos < 1) return fail(MOE_ERR_ARG, "max_pos must be >= 1");
   if (rot_dim && (!cos || !sin || misaligned(cos, 16) || misaligned(sin, 16)))
     return fail(MOE_ERR_ARG, "cos and sin must be non-NULL 16-byte aligned device pointers");
-  if (rot_dim && b->tokens && q_out == q) return fail(MOE_ERR_ARG, "q_out may be q only without rotation");
   if (product(b->tokens, heads + 2 * b->kv_heads, d / 8) >= (int64_t)256 << 31) return fail(MOE_ERR_ARG, "too many tokens times heads");
   if (b->tokens == 0) return MOE_OK;
+  const Span to = rows_of(q_out, q_out_stride, (int64_t)heads * d, bytes, b->tokens), pool = pool_of(b);
+  const Span qs = rows_of(q, q_stride, (int64_t)heads * d, bytes, b->tokens);
+  const Span ks = rows_of(k, k_stride, (int64_t)b->kv_heads * d, bytes, b->tokens), vs = rows_of(v, v_stride, (int64_t)b->kv_heads * d, bytes, b->tokens);
+  CHECK(check_apart("q_out", to, "q (it may be q itself without rotation)", qs, rot_dim == 0));
+  CHECK(check_apart("q_out", to, "k", ks));
+  CHECK(check_apart("q_out", to, "v", vs));
+  CHECK(check_apart("q_out", to, "the cache", pool));
+  CHECK(check_apart("the cache", pool, "q", qs));
+  CHECK(check_apart("the cache", pool, "k", ks));
+  CHECK(check_apart("the cache", pool, "v", vs));
+  if (rot_dim) {
+    const Span c = block_of(cos, (int64_t)max_pos * rot_dim * 2), n = block_of(sin, (int64_t)max_pos * rot_dim * 2);
+    CHECK(check_apart("q_out", to, "cos", c));
+    CHECK(check_apart("q_out", to, "sin", n));
+    CHECK(check_apart("the cache", pool, "cos", c));
+    CHECK(check_apart("the cache", pool, "sin", n));
+  }
   KvAppendArgs a;
   a.kv = kv_of(b);
   a.q = q;
@@ -156,6 +219,10 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
   if ((b->tokens && (!k || !v)) || misaligned(k, 16) || misaligned(v, 16)) return fail(MOE_ERR_ARG, "k and v must be non-NULL 16-byte aligned device pointers");
   if (product(b->tokens, 2 * b->kv_heads, b->head_dim / 8) >= (int64_t)256 << 31) return fail(MOE_ERR_ARG, "too many tokens times heads");
   if (b->tokens == 0) return MOE_OK;
+  const int64_t size = (int64_t)b->tokens * b->kv_heads * b->head_dim * element(dtype);
+  CHECK(check_apart("k", block_of(k, size), "v", block_of(v, size)));
+  CHECK(check_apart("k", block_of(k, size), "the cache", pool_of(b)));
+  CHECK(check_apart("v", block_of(v, size), "the cache", pool_of(b)));
   KvReadArgs a;
   a.kv = kv_of(b);
   a.k = k;
@@ -197,6 +264,14 @@ int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, v
   if (workspace_bytes < need || (need && (!workspace || misaligned(workspace, 16))))
     return fail(MOE_ERR_ARG, "workspace must be 16-byte aligned and hold %zu bytes (got %zu)", need, workspace_bytes);
   if (b->tokens == 0) return MOE_OK;
+  const Span to = rows_of(o, o_stride, (int64_t)heads * d, bytes, b->tokens), qs = rows_of(q, q_stride, (int64_t)heads * d, bytes, b->tokens);
+  CHECK(check_apart("o", to, "q", qs, true));
+  CHECK(check_apart("o", to, "the cache", pool_of(b)));
+  if (need) {
+    CHECK(check_apart("the workspace", block_of(workspace, (int64_t)need), "q", qs));
+    CHECK(check_apart("the workspace", block_of(workspace, (int64_t)need), "o", to));
+    CHECK(check_apart("the workspace", block_of(workspace, (int64_t)need), "the cache", pool_of(b)));
+  }
   a.part = static_cast<float *>(workspace);
   a.ml = a.part ? a.part + (size_t)a.splits * rows * d : nullptr;
   return launched(launch_kv4_attention(a, d, dtype == MOE_DTYPE_F32, static_cast<hipStream_t>(stream)), "cache attention");
@@ -218,9 +293,23 @@ int moe_norm_residual(const float *h, int64_t h_stride, const void *y, int64_t y
   if (!h_out && !x_out && rows) return fail(MOE_ERR_ARG, "neither h_out nor x_out is wanted");
   if (h_out) CHECK(check_rows("h_out", h_out, h_out_stride, d, 4, 16, rows));
   if (x_out) CHECK(check_rows("x_out", x_out, x_stride, d, bytes, 16, rows));
-  if (h_out && h_out == h && h_out_stride != h_stride) return fail(MOE_ERR_ARG, "h_out on h needs the same stride");
-  if (x_out && x_out == y && x_stride != y_stride) return fail(MOE_ERR_ARG, "x_out on y needs the same stride");
   if (rows == 0) return MOE_OK;
+  // A thread reads its channels of h, y, gate and post, writes h_out, reads pre and writes x_out.
+  const Span to_h = rows_of(h_out, h_out_stride, d, 4, rows), to_x = rows_of(x_out, x_stride, d, bytes, rows);
+  const Span hs = rows_of(h, h_stride, d, 4, rows), ys = rows_of(y, y_stride, d, bytes, rows);
+  const Span gs = rows_of(gate, gate_stride ? gate_stride : d, d, 4, gate_stride ? rows : 1);
+  const Span posts = rows_of(post, d, d, 4, 1), pres = rows_of(pre, d, d, 4, 1);
+  CHECK(check_apart("h_out", to_h, "h (it may be h itself)", hs, true));
+  CHECK(check_apart("h_out", to_h, "y", ys, true));
+  CHECK(check_apart("h_out", to_h, "gate", gs, true));
+  CHECK(check_apart("h_out", to_h, "post", posts, true));
+  CHECK(check_apart("h_out", to_h, "pre", pres));
+  CHECK(check_apart("h_out", to_h, "x_out", to_x));
+  CHECK(check_apart("x_out", to_x, "h", hs, true));
+  CHECK(check_apart("x_out", to_x, "y (it may be y itself)", ys, true));
+  CHECK(check_apart("x_out", to_x, "gate", gs, true));
+  CHECK(check_apart("x_out", to_x, "post", posts, true));
+  CHECK(check_apart("x_out", to_x, "pre", pres, true));
   NormArgs a;
   a.h = h;
   a.gate = gate;

@@ -1,6 +1,9 @@
 """Calls of the attention entry points at the edges of what they take, decided on
 the host: no rows, operands that overlap, sizes past a launch's."""
-from tests.test_attention_args import F32, P, append, attend, b, batch, norm, q4
+import numpy as np
+import pytest
+
+from tests.test_attention_args import BF16, F32, P, append, attend, b, batch, norm, q4, refused
 
 
 def test_operands_without_elements_may_be_null():
@@ -11,3 +14,104 @@ def test_operands_without_elements_may_be_null():
     b.moe_kv4_attention(*attend(none, q=None, o=None))
     b.moe_norm_residual(*norm(rows=0, h=None, y=None, ho=None, x=None))
     b.moe_norm_residual(*norm(rows=0, h=None, y=None, gate=None, gs=64, ho=None, x=None))
+
+
+def overlap(f, *args):
+    refused(f, *args)
+    assert "overlaps" in b.moe_last_error()
+
+
+# places that no operand below reaches from another; nothing is dereferenced
+A, B, C, D, E = (P + (i << 30) for i in range(1, 6))
+
+
+def apart(f, *args):
+    """The call gets past the checks, to a launch that fails without a GPU."""
+    if pytest.importorskip("torch").cuda.is_available():
+        pytest.skip("the operands are not device memory")
+    with pytest.raises(b.MoeError) as e:
+        f(*args)
+    assert e.value.code == b.MOE_ERR_HIP, e.value
+
+
+def test_products_refuse_overlap():
+    base = dict(x=A, w=B, y=C, rows=3, n=128, k=128, x_stride=128, y_stride=128)
+    overlap(b.moe_q4_matmul, *q4(**{**base, "y": A}))
+    overlap(b.moe_q4_matmul, *q4(**{**base, "y": A + 3 * 256 - 2}))
+    overlap(b.moe_q4_matmul, *q4(**{**base, "y": A - 3 * 256 + 2}))
+    overlap(b.moe_q4_matmul, *q4(**{**base, "y": B}))
+    overlap(b.moe_q4_matmul, *q4(**{**base, "y": B + 128 * 64 + 128 * 2 * 3 - 2}))
+    apart(b.moe_q4_matmul, *q4(**base))
+    apart(b.moe_q4_matmul, *q4(**{**base, "y": A + 3 * 256}))
+    apart(b.moe_q4_matmul, *q4(**{**base, "y": A - 3 * 256}))
+    # columns 0 .. 127 and 128 .. 255 of one buffer
+    wide = {**base, "x_stride": 256, "y_stride": 256}
+    apart(b.moe_q4_matmul, *q4(**{**wide, "y": A + 256}))
+    overlap(b.moe_q4_matmul, *q4(**{**wide, "y": A + 254}))
+    overlap(b.moe_q4_matmul, *q4(**{**wide, "y": A - 254}))
+    apart(b.moe_q4_matmul, *q4(**{**wide, "y": A - 256}))
+
+
+def test_append_refuses_overlap():
+    base = dict(q=A, k=B, v=C, out=D, cos=E, sin=E + 80 * 32 * 4)
+    far = batch(pool=P + (9 << 30))
+    apart(b.moe_kv4_append, *append(far, **base))
+    overlap(b.moe_kv4_append, *append(far, **{**base, "out": A}))
+    apart(b.moe_kv4_append, *append(far, **{**base, "out": A, "rot": 0}))
+    overlap(b.moe_kv4_append, *append(far, **{**base, "out": A, "rot": 0, "os": 264}))
+    overlap(b.moe_kv4_append, *append(far, **{**base, "out": A + 16, "rot": 0}))
+    for at in (B, C, E, E + 80 * 32 * 4, P + (9 << 30)):
+        overlap(b.moe_kv4_append, *append(far, **{**base, "out": at}))
+    for pool in (A, B, C, E):
+        overlap(b.moe_kv4_append, *append(batch(pool=pool), **base))
+    # queries, keys and values of a joined projection, the rotated ones beside them
+    joined = dict(q=A, k=A + 512, v=A + 768, out=A + 1024, qs=768, ks=768, vs=768, os=768)
+    apart(b.moe_kv4_append, *append(far, **{**base, **joined}))
+    overlap(b.moe_kv4_append, *append(far, **{**base, **joined, "out": A + 1040}))
+
+
+def test_read_and_attention_refuse_overlap():
+    far = batch(pool=P + (9 << 30))
+    size = 4 * 2 * 64 * 4
+    apart(b.moe_kv4_read, far, A, A + size, F32, 0)
+    overlap(b.moe_kv4_read, far, A, A + size - 16, F32, 0)
+    overlap(b.moe_kv4_read, far, A, P + (9 << 30), F32, 0)
+    base = dict(q=A, o=B)
+    apart(b.moe_kv4_attention, *attend(far, **base))
+    apart(b.moe_kv4_attention, *attend(far, **{**base, "o": A}))
+    overlap(b.moe_kv4_attention, *attend(far, **{**base, "o": A + 16}))
+    overlap(b.moe_kv4_attention, *attend(far, **{**base, "o": P + (9 << 30) + 16}))
+    need = b.moe_kv4_attention_workspace_bytes(far, 4, 1, 4096)
+    for at, bad in ((C, False), (A - need, False), (A - need + 16, True), (B, True), (P + (9 << 30), True)):
+        (overlap if bad else apart)(b.moe_kv4_attention, *attend(far, **base, max_len=4096, ws=at, wsb=need))
+
+
+def test_norm_refuses_overlap():
+    base = dict(h=A, y=B, gate=C, gs=64, post=D, pre=D + 256, ho=E, x=E + (1 << 20), dtype=F32)
+    apart(b.moe_norm_residual, *norm(**base))
+    for ho, ok in ((A, True), (B, True), (C, True), (D, False), (D + 256, False), (A + 16, False), (base["x"], False)):
+        (apart if ok else overlap)(b.moe_norm_residual, *norm(**{**base, "ho": ho}))
+    for x, ok in ((A, True), (B, True), (C, True), (D, False), (D + 256, False), (B - 16, False)):
+        (apart if ok else overlap)(b.moe_norm_residual, *norm(**{**base, "x": x}))
+    overlap(b.moe_norm_residual, *norm(**{**base, "ho": A, "hos": 128}))
+    overlap(b.moe_norm_residual, *norm(**{**base, "x": A, "dtype": BF16}))   # other elements
+    apart(b.moe_norm_residual, *norm(**{**base, "x": D + 256, "rows": 1}))
+    overlap(b.moe_norm_residual, *norm(**{**base, "ho": D + 256, "rows": 1}))
+
+
+def test_overlap_of_rows_by_hand():
+    """Against bytes marked one by one: equal and different strides."""
+    rng = np.random.default_rng(1)
+    seen = [0, 0]
+    for _ in range(400):
+        rows, k, n = int(rng.integers(1, 6)), 64 * int(rng.integers(1, 3)), int(rng.integers(1, 90))
+        xs = k + 8 * int(rng.integers(0, 12))
+        ys = n + int(rng.integers(0, 60)) if rng.random() < 0.6 else max(xs, n)
+        y = A + 2 * int(rng.integers(-500, 500))
+        taken = set()
+        for t in range(rows):
+            taken.update(range(A + t * xs * 2, A + t * xs * 2 + k * 2))
+        bad = any(not taken.isdisjoint(range(y + t * ys * 2, y + t * ys * 2 + n * 2)) for t in range(rows))
+        (overlap if bad else apart)(b.moe_q4_matmul, *q4(x=A, w=B, y=y, rows=rows, n=n, k=k, x_stride=xs, y_stride=ys))
+        seen[bad] += 1
+    assert min(seen) > 50

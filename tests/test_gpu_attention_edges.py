@@ -140,3 +140,29 @@ def test_tensors_without_rows():
         o = a.kv4_attention(q, *args, 0.125)
         assert q.shape == o.shape == (0, 4, 64) and torch.equal(args[0], before)
         assert [t.shape for t in a.kv4_read(*args, 0, 64, dtype)] == [(0, 2, 64)] * 2
+
+
+def test_overlapping_tensors_are_refused():
+    a = ops()
+    x = torch.randn((40, 64), device="cuda")
+    w = torch.zeros(b.moe_q4_matrix_bytes(64, 64), dtype=torch.uint8, device="cuda")
+    wide = torch.zeros((40, 160), device="cuda")
+    for call in (lambda: a.q4_matmul(x, w, 64, out=x), lambda: a.q4_matmul(x[1:], w, 64, out=x[:-1]),
+                 lambda: a.q4_matmul(wide[:, :64], w, 64, out=wide[:, 60:124]),
+                 lambda: a.norm_residual(x[1:], h_out=x[:-1])):
+        with pytest.raises(b.MoeError, match="overlaps"):
+            call()
+    wide[:, 64:] = 5
+    a.q4_matmul(wide[:, :64], w, 64, out=wide[:, 64:128])
+    assert (wide[:, 128:] == 5).all() and (wide[:, :128] == 0).all()
+
+
+@pytest.mark.parametrize("new", [[3, 1], [90, 2]])
+def test_attention_over_its_queries(new):
+    """o in q's place, with one split and with several."""
+    bt = Batch(new, [300, 20], 4, 2, 64, 16, seed=26).fill(0.3)
+    for max_len in (1, 1 << 20):
+        for dtype in (torch.float32, torch.bfloat16):
+            q = torch.randn((bt.tokens, 4, 64), device="cuda").to(dtype)
+            want = ops().kv4_attention(q, *bt.args(), 0.125, max_len=max_len)
+            assert torch.equal(ops().kv4_attention(q, *bt.args(), 0.125, max_len=max_len, out=q), want)
