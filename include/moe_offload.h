@@ -421,7 +421,8 @@ int moe_probe_mfma_bf16(int shape, int iters, void *stream, double *tflops);
  * 4.375 bits a weight. */
 size_t moe_q4_matrix_bytes(size_t n, size_t k);
 
-/* y[t][i] = sum_c x[t][c] W[i][c] for rows 0 <= t < rows (at most 2^20), W a
+/* y[t][i] = sum_c x[t][c] W[i][c] for rows 0 <= t < rows (at most 2^20, and fewer
+ * than 2^24 blocks of 64 rows by 128 of n), W a
  * 4-bit matrix [n x k] at w.  y's pointer and stride need only be aligned to
  * their type.  A row of x with an infinity or a NaN gives a row of NaN, and
  * a sum past fp32's range is a NaN. */
@@ -465,7 +466,8 @@ typedef struct {
  * from rot_dim on stay.  Queries [tokens][heads][head_dim] go to q_out, keys
  * and values [tokens][kv_heads][head_dim] into the cache.  cos and sin are fp32
  * [max_pos][rot_dim/2], contiguous; rot_dim a multiple of 16, 0 for no
- * rotation (cos and sin may then be NULL; max_pos still counts).  A token at a
+ * rotation (cos and sin may then be NULL; max_pos still counts).  At most 2^35 -
+ * 2^11 elements of q, k and v together (and of k and v that moe_kv4_read gives).  A token at a
  * position past max_pos - 1 is not stored and its query is zeros.  q_out may be
  * q itself (at its stride) only without rotation.  Other bytes of the cache stay as they are. */
 int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
@@ -480,7 +482,7 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
 /* Attention of every new token over its sequence's cache, itself and what is
  * before it: o[t][h] = sum_j softmax_j(scale q[t][h] . K[j][h']) V[j][h'], h'
  * = h / (heads / kv_heads); heads a multiple of kv_heads, at most 2^30 tokens
- * times heads and sequences times kv_heads.  A row that sees no
+ * times heads, fewer than 2^24 sequences times kv_heads.  A row that sees no
  * token gets zeros.  What a row does not see does not reach it, NaN included.
  * A row of q with an infinity or a NaN, or a scale that is not finite, gives NaN
  * to what sees a token; a scale below fp32's normal range counts as 0.  Where q . K
@@ -495,8 +497,8 @@ int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, v
                       float scale, int dtype, int max_new, int max_len, void *workspace, size_t workspace_bytes,
                       void *stream);
 
-/* Norms before and after a block with its gate and residual scale, for rows of
- * d (a multiple of 8 in [8, 16384]) channels:
+/* Norms before and after a block with its gate and residual scale, for rows (at
+ * most 2^24; fewer for d past 1024) of d (a multiple of 8 in [8, 16384]) channels:
  *   h_out = residual_scale * h + gate * y',   y' = y * post / rms(y)
  *   x_out = h_out * pre / rms(h_out),         rms(v) = sqrt(mean(v^2) + eps)
  * y is what the block gave (dtype), h the residual stream (fp32), x_out the

@@ -273,6 +273,9 @@ hipError_t launch_prefill_unpermute(float *H, const float *Y, const float *g, co
 int fail(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 
 // ---- the attention half of a layer ---------------------------------------
+// Workgroups of 256 threads that one dimension of a launch can have: its threads
+// are counted in 32 bits.
+constexpr int64_t kMaxGroups = (((int64_t)1 << 32) - 1) / 256;
 // Cache entries in 4 bits (moe_kv4_batch in moe_offload.h): positions of a
 // page's record.  P tokens a page, D dimensions a head.
 constexpr int kKvGroup = 32;  // dimensions that share a scale and a zero
@@ -323,6 +326,8 @@ struct Q4Args {
   int64_t x_stride, y_stride;
   int rows, n, k;
 };
+// Workgroups of the finest cut into tiles.
+inline int64_t q4_groups(int64_t rows, int64_t n) { return ((rows + 63) / 64) * ((n + 127) / 128); }
 hipError_t launch_q4_matmul(const Q4Args &a, bool f32, hipStream_t s);
 
 struct NormArgs {
@@ -334,6 +339,9 @@ struct NormArgs {
   float residual_scale, eps;
   int rows, d;
 };
+// Rows of up to this many columns go to single waves, four a workgroup.
+constexpr int kNormNarrow = 1024;
+inline int64_t norm_groups(int64_t rows, int d) { return d <= kNormNarrow ? (rows + 3) / 4 : rows; }
 hipError_t launch_norm_residual(const NormArgs &a, bool f32, hipStream_t s);
 
 // ---------------------------------------------------------------------------

@@ -936,7 +936,7 @@ KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int tokens, i
   const int per = s.prompt ? kPromptRows : 16, tile = s.prompt ? 4 * kPromptTile : kWaves * kTile;
   const int64_t full = (int64_t)tokens * (heads / kv_heads);   // rows, were they all of one sequence
   const int64_t blocks = ((rows < full ? rows : full) + per - 1) / per;
-  const int64_t pairs = (int64_t)seqs * kv_heads, room = ((int64_t)1 << 30) / pairs;  // of a launch's workgroups
+  const int64_t pairs = (int64_t)seqs * kv_heads, room = kMaxGroups / pairs;  // of a launch's workgroups
   s.row_blocks = (int)(blocks < 1 || room < 1 ? 1 : blocks > room ? room : blocks);
   // blocks with rows: no more than the batch's tokens fill, and one more a sequence
   const int64_t filled = full / per + seqs, all = (int64_t)seqs * s.row_blocks;
@@ -949,6 +949,7 @@ KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int tokens, i
   }
   n = n > most ? most : n;
   if (!s.prompt && max_len <= 512) n = 1;
+  if ((int64_t)tokens * heads > 8 * kMaxGroups) n = 1;   // rows past a launch of the join (of hints far too small)
   s.splits = (int)(n < 1 ? 1 : n);
   return s;
 }

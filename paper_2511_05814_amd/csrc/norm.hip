@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(NormArgs a) {
 
 template <int WAVES, int NV>
 void launch(const NormArgs &a, bool f32, hipStream_t s) {
-  const unsigned grid = WAVES == 1 ? ((unsigned)a.rows + 3) / 4 : (unsigned)a.rows;
+  const unsigned grid = (unsigned)norm_groups(a.rows, a.d);
   if (f32) hipLaunchKernelGGL((norm_residual_kernel<WAVES, NV, float>), dim3(grid), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((norm_residual_kernel<WAVES, NV, uint16_t>), dim3(grid), dim3(256), 0, s, a);
 }
@@ -100,7 +100,7 @@ void launch(const NormArgs &a, bool f32, hipStream_t s) {
 
 hipError_t launch_norm_residual(const NormArgs &a, bool f32, hipStream_t s) {
   if (a.d <= 512) launch<1, 1>(a, f32, s);
-  else if (a.d <= 1024) launch<1, 2>(a, f32, s);
+  else if (a.d <= kNormNarrow) launch<1, 2>(a, f32, s);
   else if (a.d <= 2048) launch<4, 1>(a, f32, s);
   else if (a.d <= 4096) launch<4, 2>(a, f32, s);
   else if (a.d <= 8192) launch<4, 4>(a, f32, s);

@@ -140,6 +140,7 @@ int moe_q4_matmul(const void *x, int64_t x_stride, const void *w, void *y, int64
   if (rows < 0 || rows > 1 << 20) return fail(MOE_ERR_ARG, "rows must be in [0, 2^20]");
   if (n < 1 || n > 1 << 24) return fail(MOE_ERR_ARG, "n must be in [1, 2^24]");
   if (k < 64 || k % 64 || k > 1 << 20) return fail(MOE_ERR_ARG, "k must be a multiple of 64 in [64, 2^20]");
+  if (q4_groups(rows, n) > kMaxGroups) return fail(MOE_ERR_ARG, "too many rows times n");
   if (!w || misaligned(w, 16)) return fail(MOE_ERR_ARG, "w must be a non-NULL 16-byte aligned device pointer");
   CHECK(check_rows("x", x, x_stride, k, element(dtype), 16, rows));
   CHECK(check_rows("y", y, y_stride, n, element(dtype), element(dtype), rows));
@@ -176,7 +177,7 @@ int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, cons
   if (max_pos < 1) return fail(MOE_ERR_ARG, "max_pos must be >= 1");
   if (rot_dim && (!cos || !sin || misaligned(cos, 16) || misaligned(sin, 16)))
     return fail(MOE_ERR_ARG, "cos and sin must be non-NULL 16-byte aligned device pointers");
-  if (product(b->tokens, heads + 2 * b->kv_heads, d / 8) >= (int64_t)256 << 31) return fail(MOE_ERR_ARG, "too many tokens times heads");
+  if (product(b->tokens, heads + 2 * b->kv_heads, d / 8) > kMaxGroups * 256) return fail(MOE_ERR_ARG, "too many tokens times heads");
   if (b->tokens == 0) return MOE_OK;
   const Span to = rows_of(q_out, q_out_stride, (int64_t)heads * d, bytes, b->tokens), pool = pool_of(b);
   const Span qs = rows_of(q, q_stride, (int64_t)heads * d, bytes, b->tokens);
@@ -217,7 +218,7 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
   CHECK(check_batch(b));
   CHECK(check_dtype(dtype));
   if ((b->tokens && (!k || !v)) || misaligned(k, 16) || misaligned(v, 16)) return fail(MOE_ERR_ARG, "k and v must be non-NULL 16-byte aligned device pointers");
-  if (product(b->tokens, 2 * b->kv_heads, b->head_dim / 8) >= (int64_t)256 << 31) return fail(MOE_ERR_ARG, "too many tokens times heads");
+  if (product(b->tokens, 2 * b->kv_heads, b->head_dim / 8) > kMaxGroups * 256) return fail(MOE_ERR_ARG, "too many tokens times heads");
   if (b->tokens == 0) return MOE_OK;
   const int64_t size = (int64_t)b->tokens * b->kv_heads * b->head_dim * element(dtype);
   CHECK(check_apart("k", block_of(k, size), "v", block_of(v, size)));
@@ -232,6 +233,7 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
 
 size_t moe_kv4_attention_workspace_bytes(const moe_kv4_batch *b, int heads, int max_new, int max_len) {
   if (check_batch(b) != MOE_OK || check_heads(b, heads) != MOE_OK || max_new < 1 || max_len < 1) return 0;
+  if (product(b->seqs, b->kv_heads) > kMaxGroups || product(b->tokens, heads) > (int64_t)1 << 30) return 0;
   const int splits = kv4_attention_shape(b->seqs, b->kv_heads, heads, b->tokens, max_new, max_len).splits;
   return splits == 1 ? 0 : (size_t)splits * b->tokens * heads * (b->head_dim + 2) * sizeof(float);
 }
@@ -246,8 +248,8 @@ int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, v
   CHECK(check_rows("q", q, q_stride, (int64_t)heads * d, bytes, 16, b->tokens));
   CHECK(check_rows("o", o, o_stride, (int64_t)heads * d, bytes, 16, b->tokens));
   if (max_new < 1 || max_len < 1) return fail(MOE_ERR_ARG, "max_new and max_len must be >= 1");
-  if (product(b->seqs, b->kv_heads) > (int64_t)1 << 30 || product(b->tokens, heads) > (int64_t)1 << 30)
-    return fail(MOE_ERR_ARG, "sequences times kv_heads and tokens times heads must be at most 2^30");
+  if (product(b->seqs, b->kv_heads) > kMaxGroups || product(b->tokens, heads) > (int64_t)1 << 30)
+    return fail(MOE_ERR_ARG, "sequences times kv_heads must be below 2^24 and tokens times heads at most 2^30");
   KvAttnArgs a;
   a.kv = kv_of(b);
   a.q = q;
@@ -284,6 +286,7 @@ int moe_norm_residual(const float *h, int64_t h_stride, const void *y, int64_t y
   CHECK(check_dtype(dtype));
   if (rows < 0 || rows > 1 << 24) return fail(MOE_ERR_ARG, "rows must be in [0, 2^24]");
   if (d < 8 || d % 8 || d > 16384) return fail(MOE_ERR_ARG, "d must be a multiple of 8 in [8, 16384]");
+  if (norm_groups(rows, d) > kMaxGroups) return fail(MOE_ERR_ARG, "rows of more than %d channels must be fewer than 2^24", kNormNarrow);
   const int bytes = element(dtype);
   CHECK(check_rows("h", h, h_stride, d, 4, 16, rows));
   if (y) CHECK(check_rows("y", y, y_stride, d, bytes, 16, rows));

@@ -1,5 +1,7 @@
 """Calls of the attention entry points at the edges of what they take, decided on
 the host: no rows, operands that overlap, sizes past a launch's."""
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -115,3 +117,52 @@ def test_overlap_of_rows_by_hand():
         (overlap if bad else apart)(b.moe_q4_matmul, *q4(x=A, w=B, y=y, rows=rows, n=n, k=k, x_stride=xs, y_stride=ys))
         seen[bad] += 1
     assert min(seen) > 50
+
+
+class Shape(ctypes.Structure):
+    _fields_ = [("splits", ctypes.c_int), ("row_blocks", ctypes.c_int), ("prompt", ctypes.c_int)]
+
+
+def cut(seqs, kv_heads, heads, tokens, max_new, max_len):
+    """moe::kv4_attention_shape, the cut of an attention's launch."""
+    f = getattr(b.lib(), "_ZN3moe19kv4_attention_shapeEiiiiii")
+    f.argtypes, f.restype = [ctypes.c_int] * 6, Shape
+    return f(seqs, kv_heads, heads, tokens, max_new, max_len)
+
+
+MOST = ((1 << 32) - 1) // 256     # workgroups of 256 threads in a launch's dimension
+
+
+def test_attention_launches_fit():
+    """Workgroups of the attention and of its join, whatever the batch and hints."""
+    rng = np.random.default_rng(2)
+
+    def power(most):
+        return int(min(most, 2 ** (rng.random() * np.log2(most + 1))))
+
+    cases = [(1024, 8, 64, 1023 + 32768, 32768, 40000), (1 << 20, 15, 15, 1 << 20, 1, 1), (1 << 20, 15, 15, 1 << 24, 1 << 24, 1 << 30),
+             (1, 1, 4096, 1 << 18, 1 << 18, 1 << 30), (4, 1, 4096, 1 << 18, 1, 1 << 30)]
+    for _ in range(3000):
+        kv = power(1024)
+        heads = kv * power(4096 // kv)
+        cases.append((power(min(1 << 20, MOST // kv)), kv, heads, power(min(1 << 24, (1 << 30) // heads)), power((1 << 31) - 1), power((1 << 31) - 1)))
+    for seqs, kv, heads, tokens, max_new, max_len in cases:
+        s = cut(seqs, kv, heads, tokens, max_new, max_len)
+        assert s.splits >= 1 and s.row_blocks >= 1
+        assert seqs * kv * s.row_blocks * s.splits <= MOST, (seqs, kv, heads, tokens, max_new, max_len, s.splits, s.row_blocks)
+        if s.splits > 1:   # 8 rows a workgroup at least, or a few rows by 4 workgroups each
+            assert -(-tokens * heads // 8) <= MOST
+
+
+def test_sizes_past_a_launch_are_refused():
+    refused(b.moe_kv4_attention, *attend(batch(seqs=1 << 20, kv_heads=16), heads=16, qs=1024, os=1024))
+    assert b.moe_kv4_attention_workspace_bytes(batch(seqs=1 << 20, kv_heads=16), 16, 1, 4096) == 0
+    most = dict(qs=1024 * 64, ks=1024 * 64, vs=1024 * 64, os=1024 * 64, heads=1024, q=A, k=A, v=A, out=C + (1 << 50), cos=B, sin=B)
+    refused(b.moe_kv4_append, *append(batch(pool=D, kv_heads=1024, tokens=1 << 18), **most))
+    refused(b.moe_kv4_read, batch(pool=D, kv_heads=1024, tokens=1 << 18), A, C + (1 << 50), F32, 0)
+    refused(b.moe_q4_matmul, *q4(rows=1 << 20, n=1 << 24, y_stride=1 << 24))
+    wide = dict(d=1032, hs=1032, ys=1032, hos=1032, xs=1032, h=A, y=A, gate=None, post=None, pre=None, ho=None, x=C + (1 << 50))
+    refused(b.moe_norm_residual, *norm(**wide, rows=1 << 24))
+    apart(b.moe_norm_residual, *norm(**wide, rows=(1 << 24) - 1))
+    narrow = {**wide, "d": 1024}
+    apart(b.moe_norm_residual, *norm(**narrow, rows=1 << 24))

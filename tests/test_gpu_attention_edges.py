@@ -12,7 +12,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from tests._attention_rig import Batch, device  # noqa: E402
-from tests.test_gpu_attention import check_attention, host, ops  # noqa: E402
+from tests.test_gpu_attention import U, check_attention, host, ops  # noqa: E402
 
 
 def change(bt, seq, pos, head, f):
@@ -166,3 +166,25 @@ def test_attention_over_its_queries(new):
             q = torch.randn((bt.tokens, 4, 64), device="cuda").to(dtype)
             want = ops().kv4_attention(q, *bt.args(), 0.125, max_len=max_len)
             assert torch.equal(ops().kv4_attention(q, *bt.args(), 0.125, max_len=max_len, out=q), want)
+
+
+def test_more_workgroups_than_a_launch_takes():
+    """One long run of new tokens among many sequences: the largest runs'
+    blocks for all of them would pass 2^32 threads, so workgroups take several."""
+    seqs, new, heads, kv, D, P = 1 << 16, 4096, 64, 8, 64, 16
+    pool = torch.zeros((new // P, kv, P * D * 9 // 8), dtype=torch.uint8, device="cuda")
+    table = torch.full((seqs, new // P), -1, dtype=torch.int32, device="cuda")
+    table[7] = torch.arange(new // P, device="cuda")
+    count = torch.zeros(seqs, dtype=torch.int32, device="cuda")
+    count[7] = new
+    start = torch.zeros(seqs + 1, dtype=torch.int32, device="cuda")
+    start[8:] = new
+    k = torch.zeros((new, kv, D), device="cuda")
+    v = torch.arange(new, device="cuda").float()[:, None, None].expand(new, kv, D) % 8
+    none = torch.empty((new, 0), device="cuda")
+    q = torch.randn((new, heads, D), device="cuda")
+    ops().kv4_append(q, k, v.contiguous(), none, none, pool, table, start, count)
+    o = ops().kv4_attention(q, pool, table, start, count, 0.125, max_new=new, max_len=new)
+    _, stored = ops().kv4_read(pool, table, start, count, new, D)
+    want = stored[:, 0, 0].double().cumsum(0) / torch.arange(1, new + 1, device="cuda")   # alike keys: the mean of the values so far
+    assert (o.double() - want[:, None, None]).abs().max() <= 8 * (2.0 ** -21 + 200 * U)
