@@ -468,7 +468,8 @@ typedef struct {
  * [max_pos][rot_dim/2], contiguous; rot_dim a multiple of 16, 0 for no
  * rotation (cos and sin may then be NULL; max_pos still counts).  At most 2^35 -
  * 2^11 elements of q, k and v together (and of k and v that moe_kv4_read gives).  A token at a
- * position past max_pos - 1 is not stored and its query is zeros.  q_out may be
+ * position past max_pos - 1 is not stored and its query is zeros; it still counts
+ * in kv_len, and moe_kv4_attention attends to whatever its place holds.  q_out may be
  * q itself (at its stride) only without rotation.  Other bytes of the cache stay as they are. */
 int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                    const void *v, int64_t v_stride, const float *cos, const float *sin, int max_pos, int rot_dim,

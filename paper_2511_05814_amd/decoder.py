@@ -27,18 +27,23 @@ from . import workload as wl
 
 class Sequences:
     """Pages and lengths of a set of sequences that share one page table in
-    every layer, kept on the host; `extend` plans a call's new tokens."""
+    every layer, kept on the host; `extend` plans a call's new tokens.  max_pos:
+    the longest that a sequence may get (the stack's)."""
 
-    def __init__(self, count: int, pages: int, page_size: int):
-        self.page_size, self.free = page_size, list(range(pages))[::-1]
+    def __init__(self, count: int, pages: int, page_size: int, max_pos: Optional[int] = None):
+        self.page_size, self.max_pos, self.free = page_size, max_pos, list(range(pages))[::-1]
         self.length = [0] * count
         self.pages: List[List[int]] = [[] for _ in range(count)]
 
     def extend(self, new: List[int]) -> dict:
         """The batch of new[b] more tokens for each sequence b: the page_table,
-        q_start and kv_len of the calls, on the device, and the longest runs."""
+        q_start and kv_len of the calls, on the device, and the longest runs.
+        Nothing changes where one is refused."""
         if len(new) != len(self.length) or min(new) < 0:
             raise ValueError(f"new tokens for {len(self.length)} sequences wanted, got {new}")
+        longest = max(n + l for n, l in zip(new, self.length))
+        if self.max_pos is not None and longest > self.max_pos:
+            raise ValueError(f"a sequence of {longest} tokens, but positions end at {self.max_pos}")
         need = [max(0, -(-(n + l) // self.page_size) - len(p)) for n, l, p in zip(new, self.length, self.pages)]
         if sum(need) > len(self.free):
             raise RuntimeError(f"{sum(need)} pages needed, {len(self.free)} free")
@@ -51,7 +56,7 @@ class Sequences:
         start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
         arrays = table, start, np.array(self.length, dtype=np.int32)
         table, start, length = (torch.from_numpy(a).to("cuda") for a in arrays)
-        return dict(page_table=table, q_start=start, kv_len=length, max_new=max(1, max(new)), max_len=max(1, max(self.length)))
+        return dict(page_table=table, q_start=start, kv_len=length, max_new=max(1, max(new)), max_len=max(1, longest), longest=longest)
 
     def release(self, b: int) -> None:
         """Sequence b is done: its pages are free again."""
@@ -67,6 +72,7 @@ class DecoderStack:
     def __init__(self, moe: offload.OffloadedMoE, heads: int, kv_heads: int, head_dim: int, pages: int,
                  page_size: int = 16, max_pos: int = 4096, dtype=torch.bfloat16, eps: float = 1e-5):
         cfg = moe.cfg
+        self.max_pos = max_pos
         self.moe, self.heads, self.kv_heads, self.head_dim, self.dtype, self.eps = moe, heads, kv_heads, head_dim, dtype, eps
         self.width = (heads + 2 * kv_heads) * head_dim
         rng = np.random.default_rng(np.random.SeedSequence(cfg.seed, spawn_key=(len("attention"),)))
@@ -82,6 +88,12 @@ class DecoderStack:
                             pool=at.kv4_pool(pages, kv_heads, page_size, head_dim)) for _ in range(cfg.layers)]
         angle = np.arange(max_pos)[:, None] * 10000.0 ** (-np.arange(0, head_dim, 2) / head_dim)
         self.cos, self.sin = (torch.from_numpy(f(angle).astype(np.float32)).to("cuda") for f in (np.cos, np.sin))
+
+    def _check(self, H: torch.Tensor, batch: dict) -> None:
+        """What a plan of `Sequences.extend` says of itself must fit the stack;
+        found on the host, before anything is enqueued."""
+        if batch.get("longest", 0) > self.max_pos:
+            raise ValueError(f"a sequence of {batch['longest']} tokens, but positions end at {self.max_pos}")
 
     def attention_block(self, layer: int, h: torch.Tensor, batch: dict) -> None:
         """h [tokens][d_model] (fp32, device), in place, on the current stream."""
@@ -100,6 +112,7 @@ class DecoderStack:
         receives h entering and leaving every attention block.  The work is only
         enqueued, on moe.compute: moe.sync() waits for it."""
         moe = self.moe
+        self._check(H, batch)
         for t in (H, batch["page_table"], batch["q_start"], batch["kv_len"]):
             t.record_stream(moe.compute)   # the caller may let go of them before it is done
         moe.compute.wait_stream(torch.cuda.current_stream())
@@ -135,7 +148,7 @@ def main(argv=None) -> None:
     moe = offload.OffloadedMoE(cfg, offload.HostStore(cfg), offload.DeviceGates(cfg), slots=cfg.slots[0],
                                policy=cfg.policies[-1], max_prefill_tokens=batched)
     stack = DecoderStack(moe, heads, max(1, heads // 4), head_dim, pages=a.sequences * -(-total // 16), max_pos=total)
-    seqs = Sequences(a.sequences, a.sequences * -(-total // 16), 16)
+    seqs = Sequences(a.sequences, a.sequences * -(-total // 16), 16, max_pos=total)
     states = torch.from_numpy(wl.hidden_states(cfg, a.sequences * total)).to("cuda").view(a.sequences, total, -1)
 
     def take(first, count):

@@ -1,0 +1,44 @@
+"""DecoderStack at its limits on an MI355X."""
+import numpy as np
+import pytest
+
+from paper_2511_05814_amd import workload as wl
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from tests._gpu_rig import Rig  # noqa: E402
+
+
+@pytest.fixture()
+def rig():
+    r = Rig(wl.CONFIGS["tiny-stack"].with_(dtype="bf16", tokens=40))
+    yield r
+    r.store.close()
+
+
+def hidden(rig, first, n):
+    return torch.from_numpy(np.ascontiguousarray(wl.hidden_states(rig.cfg, 40)[first:first + n])).cuda()
+
+
+def test_up_to_max_pos_and_no_further(rig):
+    from paper_2511_05814_amd import decoder
+    moe = rig.cache(8, "lfu", max_prefill_tokens=40)
+    dec = decoder.DecoderStack(moe, 4, 2, 64, pages=4, max_pos=20)
+    free, bound = decoder.Sequences(1, 4, 16), decoder.Sequences(1, 4, 16, max_pos=20)
+    for n in (19, 1):
+        H = hidden(rig, 0, n)
+        dec.step(H, bound.extend([n]))
+        moe.sync()
+        assert torch.isfinite(H).all()
+        free.extend([n])
+    with pytest.raises(ValueError, match="positions end at 20"):
+        bound.extend([1])
+    assert bound.length == [20]
+    H = hidden(rig, 0, 1)
+    before, pools = H.clone(), [l["pool"].clone() for l in dec.layers]
+    with pytest.raises(ValueError, match="positions end at 20"):
+        dec.step(H, free.extend([1]))
+    moe.sync()
+    assert torch.equal(H, before) and all(torch.equal(p, l["pool"]) for p, l in zip(pools, dec.layers))
+    moe.close()
