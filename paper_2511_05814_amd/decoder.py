@@ -107,8 +107,8 @@ class DecoderStack:
         at.norm_residual(h, y, gate=w["gate"], post=w["post"], eps=self.eps, h_out=h, want_x=False)
 
     def step(self, H: torch.Tensor, batch: dict, snapshots: Optional[torch.Tensor] = None) -> None:
-        """The batch's new tokens H [tokens][d_model] (fp32, device) through all
-        layers, in place.  snapshots (optional, [layers][2][tokens][d_model])
+        """The batch's new tokens H [tokens][d_model] (fp32, device; rows may lie
+        apart) through all layers, in place.  snapshots (optional, [layers][2][tokens][d_model])
         receives h entering and leaving every attention block.  The work is only
         enqueued, on moe.compute: moe.sync() waits for it."""
         moe = self.moe
@@ -124,7 +124,10 @@ class DecoderStack:
                 if snapshots is not None:
                     snapshots[l, 1].copy_(H)
                 if H.shape[0] > 1 and moe.desc.max_prefill_tokens >= H.shape[0]:
-                    offload.b.moe_prefill_layer(moe.handle, l, H.data_ptr(), H.shape[0])
+                    dense = H.contiguous()   # moe_prefill_layer takes rows one behind the other
+                    offload.b.moe_prefill_layer(moe.handle, l, dense.data_ptr(), H.shape[0])
+                    if dense is not H:
+                        H.copy_(dense)
                 else:
                     for t in range(H.shape[0]):
                         moe.decode_layer(l, H[t])

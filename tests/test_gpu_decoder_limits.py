@@ -42,3 +42,29 @@ def test_up_to_max_pos_and_no_further(rig):
     moe.sync()
     assert torch.equal(H, before) and all(torch.equal(p, l["pool"]) for p, l in zip(pools, dec.layers))
     moe.close()
+
+
+def test_rows_of_a_wider_tensor(rig):
+    """H may have a stride between rows: the same results in place, nothing beside them."""
+    from paper_2511_05814_amd import decoder
+    moe = rig.cache(8, "lfu", max_prefill_tokens=40)
+    dec = decoder.DecoderStack(moe, 4, 2, 64, pages=4, max_pos=40)
+    out = []
+    for strided in (False, True):
+        seqs = decoder.Sequences(2, 4, 16, max_pos=40)
+        moe.reset()
+        got = []
+        for at, new in ((0, [9, 4]), (13, [1, 1]), (15, [1, 0])):
+            H = hidden(rig, at, sum(new))
+            wide = torch.full((len(H), 2 * H.shape[1]), 3.0, device="cuda")
+            if strided:
+                wide[:, :H.shape[1]] = H
+                H = wide[:, :H.shape[1]]
+            snaps = torch.empty((rig.cfg.layers, 2, *H.shape), device="cuda")
+            dec.step(H, seqs.extend(new), snapshots=snaps)
+            moe.sync()
+            got += [H.clone(), snaps]
+            assert (wide[:, -H.shape[1]:] == 3).all()
+        out.append(got)
+    assert all(torch.equal(a, c) for a, c in zip(*out))
+    moe.close()
