@@ -27,18 +27,20 @@ from . import workload as wl
 
 class Sequences:
     """Pages and lengths of a set of sequences that share one page table in
-    every layer, kept on the host; `extend` plans a call's new tokens.  max_pos:
-    the longest that a sequence may get (the stack's)."""
+    every layer, kept on the host; `extend` plans a call's new tokens.  pages,
+    page_size and max_pos (the longest that a sequence may get) are those of the
+    stack; `DecoderStack.sequences` fills them in."""
 
     def __init__(self, count: int, pages: int, page_size: int, max_pos: Optional[int] = None):
-        self.page_size, self.max_pos, self.free = page_size, max_pos, list(range(pages))[::-1]
+        self.page_size, self.max_pos, self.count, self.free = page_size, max_pos, pages, list(range(pages))[::-1]
         self.length = [0] * count
         self.pages: List[List[int]] = [[] for _ in range(count)]
 
     def extend(self, new: List[int]) -> dict:
         """The batch of new[b] more tokens for each sequence b: the page_table,
-        q_start and kv_len of the calls, on the device, and the longest runs.
-        Nothing changes where one is refused."""
+        q_start and kv_len of the calls, on the device, the longest runs, and
+        what the plan was made for (tokens, longest, pages, page_size).  Nothing
+        changes where one is refused."""
         if len(new) != len(self.length) or min(new) < 0:
             raise ValueError(f"new tokens for {len(self.length)} sequences wanted, got {new}")
         longest = max(n + l for n, l in zip(new, self.length))
@@ -56,7 +58,8 @@ class Sequences:
         start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
         arrays = table, start, np.array(self.length, dtype=np.int32)
         table, start, length = (torch.from_numpy(a).to("cuda") for a in arrays)
-        return dict(page_table=table, q_start=start, kv_len=length, max_new=max(1, max(new)), max_len=max(1, longest), longest=longest)
+        return dict(page_table=table, q_start=start, kv_len=length, max_new=max(1, max(new)), max_len=max(1, longest),
+                    tokens=sum(new), longest=longest, pages=self.count, page_size=self.page_size)
 
     def release(self, b: int) -> None:
         """Sequence b is done: its pages are free again."""
@@ -72,7 +75,7 @@ class DecoderStack:
     def __init__(self, moe: offload.OffloadedMoE, heads: int, kv_heads: int, head_dim: int, pages: int,
                  page_size: int = 16, max_pos: int = 4096, dtype=torch.bfloat16, eps: float = 1e-5):
         cfg = moe.cfg
-        self.max_pos = max_pos
+        self.pages, self.page_size, self.max_pos = pages, page_size, max_pos
         self.moe, self.heads, self.kv_heads, self.head_dim, self.dtype, self.eps = moe, heads, kv_heads, head_dim, dtype, eps
         self.width = (heads + 2 * kv_heads) * head_dim
         rng = np.random.default_rng(np.random.SeedSequence(cfg.seed, spawn_key=(len("attention"),)))
@@ -89,11 +92,22 @@ class DecoderStack:
         angle = np.arange(max_pos)[:, None] * 10000.0 ** (-np.arange(0, head_dim, 2) / head_dim)
         self.cos, self.sin = (torch.from_numpy(f(angle).astype(np.float32)).to("cuda") for f in (np.cos, np.sin))
 
+    def sequences(self, count: int) -> Sequences:
+        """A set of sequences over this stack's pages (one set at a time)."""
+        return Sequences(count, self.pages, self.page_size, self.max_pos)
+
     def _check(self, H: torch.Tensor, batch: dict) -> None:
-        """What a plan of `Sequences.extend` says of itself must fit the stack;
-        found on the host, before anything is enqueued."""
+        """H and what a plan of `Sequences.extend` says of itself must fit the
+        stack; found on the host, before anything is enqueued."""
+        if H.dim() != 2 or H.shape[1] != self.moe.cfg.d_model or H.dtype != torch.float32:
+            raise ValueError(f"H must be float32 [tokens, {self.moe.cfg.d_model}], not {H.dtype} {list(H.shape)}")
+        if batch.get("tokens", H.shape[0]) != H.shape[0]:
+            raise ValueError(f"{H.shape[0]} rows of H for a plan of {batch['tokens']} tokens")
         if batch.get("longest", 0) > self.max_pos:
             raise ValueError(f"a sequence of {batch['longest']} tokens, but positions end at {self.max_pos}")
+        if batch.get("page_size", self.page_size) != self.page_size or batch.get("pages", 0) > self.pages:
+            raise ValueError(f"a plan for {batch['pages']} pages of {batch['page_size']} tokens, but the stack has "
+                             f"{self.pages} of {self.page_size}")
 
     def attention_block(self, layer: int, h: torch.Tensor, batch: dict) -> None:
         """h [tokens][d_model] (fp32, device), in place, on the current stream."""
@@ -151,7 +165,7 @@ def main(argv=None) -> None:
     moe = offload.OffloadedMoE(cfg, offload.HostStore(cfg), offload.DeviceGates(cfg), slots=cfg.slots[0],
                                policy=cfg.policies[-1], max_prefill_tokens=batched)
     stack = DecoderStack(moe, heads, max(1, heads // 4), head_dim, pages=a.sequences * -(-total // 16), max_pos=total)
-    seqs = Sequences(a.sequences, a.sequences * -(-total // 16), 16, max_pos=total)
+    seqs = stack.sequences(a.sequences)
     states = torch.from_numpy(wl.hidden_states(cfg, a.sequences * total)).to("cuda").view(a.sequences, total, -1)
 
     def take(first, count):

@@ -12,7 +12,7 @@ def stack(**kw):
     """A stack's sizes alone: no GPU, no weights."""
     s = decoder.DecoderStack.__new__(decoder.DecoderStack)
     s.moe = types.SimpleNamespace(L=1, cfg=types.SimpleNamespace(d_model=64))
-    s.max_pos = 40
+    s.pages, s.page_size, s.max_pos = 3, 16, 40
     for name, value in kw.items():
         setattr(s, name, value)
     return s
@@ -20,7 +20,7 @@ def stack(**kw):
 
 def plan(**kw):
     table, start, length = (torch.zeros(n, dtype=torch.int32) for n in ((1, 3), 2, 1))
-    return {**dict(page_table=table, q_start=start, kv_len=length, max_new=2, max_len=40, longest=40), **kw}
+    return {**dict(page_table=table, q_start=start, kv_len=length, max_new=2, max_len=40, tokens=2, longest=40, pages=3, page_size=16), **kw}
 
 
 def test_positions_past_the_tables():
@@ -33,3 +33,23 @@ def test_positions_past_the_tables():
     assert s.length == [39, 3] and s.free == [0, 1, 2, 3] and s.pages == [[7, 6, 5], [4]]
     with pytest.raises(ValueError, match="positions end at 40"):
         stack().step(torch.zeros((2, 64)), plan(longest=41))
+
+
+@pytest.mark.parametrize("wrong,says", [(dict(page_size=32), "pages of 32"), (dict(pages=4), "4 pages"), (dict(tokens=3), "plan of 3 tokens"),
+                                        (dict(tokens=1), "plan of 1 tokens")])
+def test_plans_for_another_stack(wrong, says):
+    """Other pages or page sizes name places that this cache does not have; rows
+    without a plan would be results of nothing."""
+    with pytest.raises(ValueError, match=says):
+        stack().step(torch.zeros((2, 64)), plan(**wrong))
+
+
+@pytest.mark.parametrize("H", [torch.zeros((2, 32)), torch.zeros((2, 64), dtype=torch.bfloat16), torch.zeros(64)])
+def test_hidden_states_of_another_shape(H):
+    with pytest.raises(ValueError, match="H must be"):
+        stack().step(H, plan())
+
+
+def test_a_stack_makes_its_sequences():
+    s = stack().sequences(5)
+    assert (len(s.length), sorted(s.free), s.page_size, s.max_pos) == (5, [0, 1, 2], 16, 40)

@@ -68,3 +68,25 @@ def test_rows_of_a_wider_tensor(rig):
         out.append(got)
     assert all(torch.equal(a, c) for a, c in zip(*out))
     moe.close()
+
+
+def test_sequences_of_the_stack(rig):
+    """A plan of its own sequences runs; one for more or other pages does not. A step of no tokens is no work."""
+    from paper_2511_05814_amd import decoder
+    moe = rig.cache(8, "lfu", max_prefill_tokens=40)
+    dec = decoder.DecoderStack(moe, 4, 2, 64, pages=4, page_size=16, max_pos=40)
+    H = hidden(rig, 0, 3)
+    before = H.clone()
+    for other in (decoder.Sequences(1, 5, 16), decoder.Sequences(1, 4, 32)):
+        with pytest.raises(ValueError, match="the stack has 4 of 16"):
+            dec.step(H, other.extend([3]))
+    seqs = dec.sequences(2)
+    dec.step(H[:0], seqs.extend([0, 0]))
+    with pytest.raises(ValueError, match="3 rows of H for a plan of 2"):
+        dec.step(H, seqs.extend([2, 0]))
+    moe.sync()
+    assert torch.equal(H, before)
+    dec.step(H, seqs.extend([0, 3]))
+    moe.sync()
+    assert torch.isfinite(H).all() and not torch.equal(H, before)
+    moe.close()
