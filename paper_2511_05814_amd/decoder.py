@@ -91,6 +91,8 @@ class DecoderStack:
                             pool=at.kv4_pool(pages, kv_heads, page_size, head_dim)) for _ in range(cfg.layers)]
         angle = np.arange(max_pos)[:, None] * 10000.0 ** (-np.arange(0, head_dim, 2) / head_dim)
         self.cos, self.sin = (torch.from_numpy(f(angle).astype(np.float32)).to("cuda") for f in (np.cos, np.sin))
+        for t in (self.cos, self.sin, *(t for l in self.layers for t in l.values())):
+            t.record_stream(moe.compute)   # a stack may be dropped before its steps are done
 
     def sequences(self, count: int) -> Sequences:
         """A set of sequences over this stack's pages (one set at a time)."""
@@ -127,8 +129,9 @@ class DecoderStack:
         enqueued, on moe.compute: moe.sync() waits for it."""
         moe = self.moe
         self._check(H, batch)
-        for t in (H, batch["page_table"], batch["q_start"], batch["kv_len"]):
-            t.record_stream(moe.compute)   # the caller may let go of them before it is done
+        for t in (H, batch["page_table"], batch["q_start"], batch["kv_len"], snapshots):
+            if t is not None:
+                t.record_stream(moe.compute)   # the caller may let go of them before it is done
         moe.compute.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(moe.compute):
             for l in range(moe.L):

@@ -53,3 +53,31 @@ def test_hidden_states_of_another_shape(H):
 def test_a_stack_makes_its_sequences():
     s = stack().sequences(5)
     assert (len(s.length), sorted(s.free), s.page_size, s.max_pos) == (5, [0, 1, 2], 16, 40)
+
+
+def test_tensors_of_a_step_are_known_to_its_stream(monkeypatch):
+    """Weights, pages, tables, H, plan and snapshots belong to the caller's
+    stream and are used on the experts': torch's allocator must know."""
+    known = []
+
+    class Stop(Exception):
+        pass
+
+    def stop(*a):
+        raise Stop
+
+    to, zeros = torch.Tensor.to, torch.zeros
+    monkeypatch.setattr(torch.Tensor, "to", lambda t, *a, **k: t if a == ("cuda",) else to(t, *a, **k))
+    monkeypatch.setattr(torch, "zeros", lambda *a, device=None, **k: zeros(*a, **k))
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: known.append((t.data_ptr(), s)))
+    monkeypatch.setattr(torch.cuda, "current_stream", stop)
+    cfg = types.SimpleNamespace(seed=1, d_model=64, layers=2)
+    moe = types.SimpleNamespace(cfg=cfg, L=2, compute=types.SimpleNamespace(wait_stream=stop))
+    s = decoder.DecoderStack(moe, 2, 1, 64, pages=3, max_pos=40)
+    H, snaps, batch = torch.zeros((2, 64)), torch.zeros((2, 2, 2, 64)), plan()
+    with pytest.raises(Stop):
+        s.step(H, batch, snapshots=snaps)
+    with pytest.raises(Stop):
+        s.step(H, batch)
+    used = [s.cos, s.sin, H, snaps, *(batch[k] for k in ("page_table", "q_start", "kv_len")), *(t for l in s.layers for t in l.values())]
+    assert len(used) == 7 + 2 * 6 and all((t.data_ptr(), moe.compute) in known for t in used)

@@ -90,3 +90,32 @@ def test_sequences_of_the_stack(rig):
     moe.sync()
     assert torch.isfinite(H).all() and not torch.equal(H, before)
     moe.close()
+
+
+def test_a_stack_dropped_before_its_steps_are_done(rig):
+    """What it held is not given to tensors of the caller's stream while the steps still read it."""
+    from paper_2511_05814_amd import decoder
+    results = []
+    for drop in (False, True):
+        moe = rig.cache(8, "lfu", max_prefill_tokens=40)
+        dec = decoder.DecoderStack(moe, 4, 2, 64, pages=4, max_pos=40)
+        seqs, H = dec.sequences(1), hidden(rig, 0, 20)
+        snaps = torch.zeros((rig.cfg.layers, 2, *H.shape), device="cuda")
+        work = torch.randn((4096, 4096), device="cuda")
+        work.record_stream(moe.compute)
+        sizes = [t.numel() for l in dec.layers for t in l.values() if t.dtype == torch.uint8]
+        torch.cuda.synchronize()
+        moe.compute.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(moe.compute):
+            for _ in range(30):      # some milliseconds ahead of the step
+                work = (work @ work).clamp(-1, 1)
+        dec.step(H, seqs.extend([20]), snapshots=snaps)
+        if drop:
+            del dec, snaps
+            held = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(2)]
+            assert len(held) == 2 * len(sizes)
+        moe.sync()
+        torch.cuda.synchronize()
+        results.append(H.clone())
+        moe.close()
+    assert torch.equal(*results)
