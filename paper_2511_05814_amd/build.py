@@ -3,8 +3,8 @@
 Compiles every HIP source under csrc/ for gfx950 with hipcc into one shared
 library exporting the C ABI of include/moe_offload.h, and csrc/attention_ops.cpp
 (host code: the torch calls of `attention`) into a CPython module beside it that
-links to it.  Run as a module (`python -m paper_2511_05814_amd.build`) or through
-__graft_entry__.build().
+links to it (with torch only: the C library builds without).  Run as a module
+(`python -m paper_2511_05814_amd.build`) or through __graft_entry__.build().
 """
 from __future__ import annotations
 
@@ -12,6 +12,7 @@ import glob
 import os
 import subprocess
 import sys
+from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -36,24 +37,29 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found")
 
 
-def build_ops(verbose: bool = False) -> str:
-    """The CPython module, against this interpreter's and torch's headers."""
+def build_ops(verbose: bool = False) -> Optional[str]:
+    """The CPython module, against this interpreter's and torch's headers; None
+    without torch, for which it is: the C library needs none."""
     import sysconfig
 
-    import torch
-    from torch.utils import cpp_extension
+    try:
+        import torch
+        from torch.utils import cpp_extension
+    except ImportError:
+        print("torch is not installed: the C library is built without the module of torch calls", file=sys.stderr)
+        return None
     tmp = OPS + ".tmp"
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+    cmd = [hipcc(), "-x", "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
            "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"],
            *[f for d in cpp_extension.include_paths() for f in ("-isystem", d)],
-           os.path.join(CSRC, "attention_ops.cpp"), "-o", tmp, OUT, "-Wl,-rpath,$ORIGIN",
+           os.path.join(CSRC, "attention_ops.cpp"), "-x", "none", "-o", tmp, OUT, "-Wl,-rpath,$ORIGIN",
            *["-L" + d for d in cpp_extension.library_paths()], "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError("g++ failed:\n" + "\n".join(res.stderr.splitlines()[-60:]))
+        raise RuntimeError("hipcc failed:\n" + "\n".join(res.stderr.splitlines()[-60:]))
     os.replace(tmp, OPS)
     return OPS
 
