@@ -70,7 +70,9 @@ def build(verbose: bool = False) -> str:
     tmp = OUT + ".tmp"
     # MOE_HIPCC_EXTRA: extra compiler flags for tuning builds (e.g. -DMOE_FETCH_BLOCKS=32)
     extra = os.environ.get("MOE_HIPCC_EXTRA", "").split()
-    cmd = [hipcc(), *FLAGS, *extra, "-I", os.path.join(ROOT, "include"), "-I", CSRC, *sources, "-o", tmp]
+    # a name of its own, so that what links to it finds the library beside itself, wherever that is
+    name = "-Wl,-soname," + os.path.basename(OUT)
+    cmd = [hipcc(), *FLAGS, name, *extra, "-I", os.path.join(ROOT, "include"), "-I", CSRC, *sources, "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
