@@ -8,7 +8,8 @@ formulas and layouts) on torch's current stream of the tensors' device, so
 Nothing synchronises.  Tensors are fp32 or bf16 as a whole call; a tensor used
 on another stream than its own has to be made known to torch's allocator
 (`record_stream`) as with any torch operator.  ValueError: tensors that do not
-fit together; binding.MoeError: what the library refuses (alignment, limits).
+fit together; binding.MoeError: what the library refuses (alignment, overlap,
+limits); torch.OutOfMemoryError: no memory for a result or a workspace.
 
 A cache's pool is uint8 [pages][kv heads][page_size * head_dim * 9 / 8]
 (`kv4_pool`).  A batch of B sequences is three int32 tensors on the device:
@@ -46,7 +47,7 @@ def _ops():
         loader = importlib.machinery.ExtensionFileLoader("_attention_ops", OPS_PATH)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_attention_ops", loader))
         loader.exec_module(module)
-        module.set_error(b.MoeError)
+        module.set_errors(b.MoeError, torch.OutOfMemoryError)
         _module = module
     return _module
 

@@ -5,7 +5,8 @@
 // the host some 3 us; through ctypes the checks and the marshalling took more
 // than that.  Every function takes its positional arguments in attention.py's
 // order and the stream as an integer last.  ValueError: tensors that do not fit
-// together; the class given to set_error: what the library refuses.
+// together; the classes given to set_errors: what the library refuses, and no
+// memory for a result or a workspace.
 #include <Python.h>
 
 #include <ATen/ATen.h>
@@ -15,7 +16,8 @@
 
 namespace {
 
-PyObject *g_error = nullptr;   // binding.MoeError
+PyObject *g_error = nullptr;     // binding.MoeError
+PyObject *g_memory = nullptr;    // torch.OutOfMemoryError
 
 // Thrown with the Python error set.
 struct Raised {};
@@ -147,6 +149,8 @@ PyObject *call(Py_ssize_t got, Py_ssize_t n, F f) {
   try {
     return f();
   } catch (const Raised &) {
+  } catch (const c10::OutOfMemoryError &e) {
+    PyErr_SetString(g_memory ? g_memory : PyExc_RuntimeError, e.what_without_backtrace());
   } catch (const std::exception &e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
   }
@@ -291,16 +295,22 @@ PyObject *norm_residual(PyObject *, PyObject *const *a, Py_ssize_t got) {
   });
 }
 
-PyObject *set_error(PyObject *, PyObject *cls) {
+void set_class(PyObject **to, PyObject *cls) {
   Py_INCREF(cls);
-  Py_XDECREF(g_error);
-  g_error = cls;
+  Py_XDECREF(*to);
+  *to = cls;
+}
+PyObject *set_errors(PyObject *, PyObject *args) {
+  PyObject *error, *memory;
+  if (!PyArg_ParseTuple(args, "OO", &error, &memory)) return nullptr;
+  set_class(&g_error, error);
+  set_class(&g_memory, memory);
   Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(q4_matmul), FAST(kv4_append), FAST(kv4_read), FAST(kv4_attention), FAST(norm_residual),
-                         {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         {"set_errors", set_errors, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_attention_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -188,3 +188,14 @@ def test_more_workgroups_than_a_launch_takes():
     _, stored = ops().kv4_read(pool, table, start, count, new, D)
     want = stored[:, 0, 0].double().cumsum(0) / torch.arange(1, new + 1, device="cuda")   # alike keys: the mean of the values so far
     assert (o.double() - want[:, None, None]).abs().max() <= 8 * (2.0 ** -21 + 200 * U)
+
+
+def test_no_memory_is_torchs_error():
+    """More than the card has: torch's own class, and the next call works."""
+    bt = Batch([1], [1], 4, 2, 64, 16)
+    args = bt.args()
+    pool = torch.zeros((4, 1024, 16 * 64 * 9 // 8), dtype=torch.uint8, device="cuda")
+    assert (1 << 22) * 1024 * 64 * 4 > 2 * torch.cuda.get_device_properties(0).total_memory
+    with pytest.raises(torch.OutOfMemoryError):
+        ops().kv4_read(pool, *args[1:], 1 << 22, 64)
+    assert ops().kv4_read(*args, 1, 64)[0].shape == (1, 2, 64)
