@@ -5,11 +5,12 @@ Each function checks its tensors, allocates what it returns (unless it is given
 `out`) and enqueues one call of the C ABI (include/moe_offload.h, which has the
 formulas and layouts) on torch's current stream of the tensors' device, so
 `with torch.cuda.stream(moe.compute)` puts it in line with an `OffloadedMoE`.
-Nothing synchronises.  Tensors are fp32 or bf16 as a whole call; a tensor used
-on another stream than its own has to be made known to torch's allocator
-(`record_stream`) as with any torch operator.  ValueError: tensors that do not
-fit together; binding.MoeError: what the library refuses (alignment, overlap,
-limits); torch.OutOfMemoryError: no memory for a result or a workspace.
+Nothing synchronises.  None has a gradient: a tensor that requires one is
+refused unless gradients are off.  Tensors are fp32 or bf16 as a whole call; a
+tensor used on another stream than its own has to be made known to torch's
+allocator (`record_stream`) as with any torch operator.  ValueError: tensors
+that do not fit together; binding.MoeError: what the library refuses (alignment,
+overlap, limits); torch.OutOfMemoryError: no memory for a result or a workspace.
 
 A cache's pool is uint8 [pages][kv heads][page_size * head_dim * 9 / 8]
 (`kv4_pool`).  A batch of B sequences is three int32 tensors on the device:

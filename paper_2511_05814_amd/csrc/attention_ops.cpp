@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "moe_offload.h"
@@ -41,7 +42,11 @@ void check_rc(int rc, const char *where) {
 
 const at::Tensor &tensor(PyObject *o, const char *name) {
   if (!THPVariable_Check(o)) value_error(std::string(name) + " must be a tensor");
-  return THPVariable_Unpack(o);
+  const at::Tensor &t = THPVariable_Unpack(o);
+  // the result would come back detached
+  if (t.requires_grad() && c10::GradMode::is_enabled())
+    value_error(std::string(name) + " requires grad, and these operators have no gradient: detach it or use torch.no_grad()");
+  return t;
 }
 bool given(PyObject *o) { return o != Py_None; }
 

@@ -199,3 +199,24 @@ def test_no_memory_is_torchs_error():
     with pytest.raises(torch.OutOfMemoryError):
         ops().kv4_read(pool, *args[1:], 1 << 22, 64)
     assert ops().kv4_read(*args, 1, 64)[0].shape == (1, 2, 64)
+
+
+def test_tensors_that_require_grad():
+    """Refused while gradients are on, rather than answered without one."""
+    a = ops()
+    x, h = (torch.randn((3, 64), device="cuda", requires_grad=True) for _ in range(2))
+    plain, v = torch.randn((3, 64), device="cuda"), torch.ones(64, device="cuda", requires_grad=True)
+    w = torch.zeros(b.moe_q4_matrix_bytes(8, 64), dtype=torch.uint8, device="cuda")
+    bt = Batch([3], [1], 1, 1, 64, 16).fill(0.3)
+    args, cos = bt.args(), torch.ones((8, 32), device="cuda")
+    q = x.unflatten(1, (1, 64))
+    calls = [lambda: a.q4_matmul(x, w, 8), lambda: a.q4_matmul(plain, w, 64 // 8, out=torch.empty((3, 8), device="cuda", requires_grad=True)),
+             lambda: a.norm_residual(h), lambda: a.norm_residual(plain, x), lambda: a.norm_residual(plain, plain, gate=v),
+             lambda: a.norm_residual(plain, plain, post=v), lambda: a.norm_residual(plain, pre=v),
+             lambda: a.kv4_append(plain[:, None], q, plain[:, None], cos, cos, *args), lambda: a.kv4_attention(q, *args, 0.125)]
+    for call in calls:
+        with pytest.raises(ValueError, match="requires grad"):
+            call()
+        with torch.no_grad():
+            call()
+    assert not a.q4_matmul(x.detach(), w, 8).requires_grad
