@@ -11,8 +11,9 @@ from paper_2511_05814_amd import binding as b
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests._attention_rig import Batch, device  # noqa: E402
-from tests.test_gpu_attention import U, check_attention, host, ops  # noqa: E402
+from tests._attention_rig import Batch, bf16, device  # noqa: E402
+from tests.test_attention_limits import cut  # noqa: E402
+from tests.test_gpu_attention import U, check_attention, check_product, host, matrix, ops  # noqa: E402
 
 
 def change(bt, seq, pos, head, f):
@@ -220,3 +221,55 @@ def test_tensors_that_require_grad():
         with torch.no_grad():
             call()
     assert not a.q4_matmul(x.detach(), w, 8).requires_grad
+
+
+# -- splits over a long cache and their joins ----------------------------------------
+
+def splits(bt, max_new, max_len):
+    return cut(len(bt.new), bt.kv_heads, bt.heads, bt.tokens, max_new, max_len)
+
+
+@pytest.mark.parametrize("what", ["plain", "marked", "holes", "empty"])
+@pytest.mark.parametrize("new", [[1], [3], [100], [150]])   # a block of 16 rows, of 128; the last goes to the other join
+@pytest.mark.parametrize("D", [64, 128])
+def test_splits_of_a_long_sequence(D, new, what):
+    """One sequence cut into many parts: with few rows they are joined by a
+    workgroup for 32 dimensions of a row, with many by a few lanes."""
+    bt = Batch(new, [3100], 4, 2, D, 16, seed=31).fill(0.3)
+    if what == "marked":      # both in parts of their own, of a head each
+        change(bt, 0, 700, 0, mark(0))
+        change(bt, 0, 2050, 1, mark(2))
+    if what == "holes":       # more than a part without a page, and single pages
+        bt.table[0, 40:80] = -1
+        bt.table[0, [3, 100, 101, 190]] = 1 << 20
+    if what == "empty":       # parts behind the end
+        bt.table = np.concatenate([bt.table, np.full((1, 800), -1, np.int32)], 1)
+    assert splits(bt, new[0], bt.table.shape[1] * bt.P).splits >= 8
+    for dtype in ("f32", "bf16"):
+        o, want = check_attention(bt, dtype)
+        if what == "marked":
+            assert np.isnan(o[:, :2]).all() and np.isnan(o[:, 2:, 32:64]).all() and not np.isnan(o[:, 2:, :32]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prompts_of_many_sequences(dtype):
+    """From eight sequences on splits are finer: 16, one of them long, short
+    ones and ones without new tokens."""
+    new = [16, 2, 0, 16, 1, 5, 16, 0, 9, 3, 16, 1, 16, 7, 16, 2]
+    old = [30, 3900, 0, 100, 17, 40, 0, 90, 260, 3, 10, 800, 5, 64, 31, 0]
+    bt = Batch(new, old, 32, 8, 64, 16, seed=32).fill(0.3)
+    s = splits(bt, 16, 3902)
+    assert (s.prompt, s.splits) == (1, 5) and splits(bt, 16, 3071).splits < 5
+    check_attention(bt, dtype, max_new=16, max_len=3902)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n,k", [(9, 100, 8192), (1, 33, 16384), (31, 64, 4096)])
+def test_products_of_long_rows(rows, n, k, dtype):
+    """Few rows over many groups: the waves' runs of groups, whole and ragged."""
+    rng = np.random.default_rng(k + n)
+    for kk in (k, k + 64, k + 192):
+        buf = matrix(rng, n, kk)
+        x = rng.standard_normal((rows, kk)).astype(np.float32)
+        x = bf16(x) if dtype == "bf16" else x
+        check_product(x.astype(np.float64), buf, n, kk, ops().q4_matmul(device(x, dtype), torch.from_numpy(buf).cuda(), n), dtype)
