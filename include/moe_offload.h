@@ -405,7 +405,8 @@ int moe_probe_mfma_bf16(int shape, int iters, void *stream, double *tflops);
  * device memory of that device and must stay valid until the work is done.
  * `dtype` is MOE_DTYPE_F32 or MOE_DTYPE_BF16, the type of all inputs and
  * outputs not said to be something else; sums and softmax statistics are fp32,
- * fp32 operands take part whole (no rounding to bf16).  Strides are in
+ * and fp32 operands are not rounded to bf16 (what is rounded is said at each call).
+ * Strides are in
  * elements between rows (tokens); a row itself is contiguous.  Pointers and
  * strides must be multiples of 16 bytes unless said otherwise.  With no rows
  * (tokens) a call checks its arguments and does nothing; operands that have no
@@ -424,8 +425,10 @@ size_t moe_q4_matrix_bytes(size_t n, size_t k);
 /* y[t][i] = sum_c x[t][c] W[i][c] for rows 0 <= t < rows (at most 2^20, and fewer
  * than 2^24 blocks of 64 rows by 128 of n), W a
  * 4-bit matrix [n x k] at w.  y's pointer and stride need only be aligned to
- * their type.  A row of x with an infinity or a NaN gives a row of NaN, and
- * a sum past fp32's range is a NaN. */
+ * their type.  fp32 x takes part whole.  A row of x with an infinity (also where
+ * the product would be one of known sign) or a NaN gives a row of NaN, and a sum
+ * past fp32's range is a NaN; partial sums are up to 255 times those of |x| over 64
+ * columns, so |x| should stay below 2^113. */
 int moe_q4_matmul(const void *x, int64_t x_stride, const void *w, void *y, int64_t y_stride, int rows, int n, int k,
                   int dtype, void *stream);
 
@@ -487,7 +490,10 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
  * token gets zeros.  What a row does not see does not reach it, NaN included.
  * A row of q with an infinity or a NaN, or a scale that is not finite, gives NaN
  * to what sees a token; a scale below fp32's normal range counts as 0.  Where q . K
- * passes fp32's range a row may come out as NaN.  o may be q itself, at its stride.
+ * passes fp32's range a row may come out as NaN.  Roundings: bf16 calls hold a
+ * probability in one fp16 number (2^-11 of itself, and the sum that divides counts
+ * the rounded ones), fp32 calls hold q and the probabilities in 22 bits; keys and
+ * values are exact.  o may be q itself, at its stride.
  * max_new (new tokens of a sequence) and max_len (tokens of a sequence) say how
  * the work is best cut; results are right whatever they are.  The workspace
  * (16-byte aligned; NULL if it is 0 bytes) must hold

@@ -228,9 +228,10 @@ __device__ __forceinline__ float sum_over_j(float v) {
 // sequence is spread over all of them.  Prompts: blocks last and the later rows,
 // which see most, first, so that the longest work starts first; the sequences of
 // a block rotate with it, or one in four, long, would put all of its work on one
-// engine of each XCD (prompts of 2048 tokens over 2048 and three shorter ones:
-// 682 us so, 188 with the blocks of a sequence one after another, 183 as it is,
-// all three before the products were reordered, since when it takes 166).
+// engine of each XCD (2048 new tokens of one sequence over 2048 and single tokens
+// of three others: 682 us so, 188 with the blocks of a sequence one after
+// another, 183 as it is, all three before the products were reordered, since when
+// it takes 166).
 struct Place {
   int split, block, seq, kv_head;
 };
@@ -286,10 +287,18 @@ __device__ __forceinline__ Seq sequence(const KvAttnArgs &a, int b, int group) {
 // lanes, and the rows' maxima and sums rescale lane-locally.  Keys and values
 // are exact in fp16; q (and p, in fp32 calls) is one fp16 number or, for fp32
 // calls, the sum of two.
-// It reads the cache once; the vector instructions that expand it (about 360 a
-// wave and block) and the latency of its loads bound it before HBM does: 32
-// sequences of up to 4096 tokens, 91 MB, in 29 us (3.1 TB/s), one of 131072, 151
-// MB, in 40 us with the join (3.7 TB/s).
+// It reads the cache once.  Below HBM's rate it is held by the vector instructions
+// that expand the cache (about 360 a wave and block) and by the latency of its
+// loads, of which one block a wave is in flight: 32 sequences of up to 4096
+// tokens, 91 MB, in 29 us (3.1 TB/s), vector lanes busy 61% of the kernel's time,
+// and the splits, as many for every sequence, leave the shorter ones' waves idle;
+// one of 131072, 151 MB, in 41 us with the join (3.7 TB/s), vector lanes busy 79%.
+//
+// A probability is rounded to fp16 in bf16 calls, 2^-11 of itself toward zero,
+// where fp32 would need a second product: the row's sum counts the rounded ones,
+// so only their differences reach the result, which then takes 2^-9 in bf16.  fp32
+// calls hold q and the probabilities in 22 bits, two numbers each; a third would
+// be half as many products again for bits that sums of fp32 lose.
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void kv4_attention_kernel(KvAttnArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
@@ -556,9 +565,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void 
 // which is the operand of O^T = V^T P^T when its sum takes the tokens in that
 // order.  Two tiles of LDS, one barrier a tile; the bytes of the tile after
 // next are on their way to registers.
-// Vector instructions bound it (an exponential a score, the expansion), which
-// little of the matrix work runs beside: four prompts of up to 2048 tokens over
-// 2048, 32 heads to 8, 103 GFLOP, in 166 us, 620 TFLOP/s.
+// Vector instructions (an exponential a score, the expansion) and matrix
+// instructions run mostly one after another, busy 48% and 26% of the time: 2048
+// new tokens of one sequence over 2048, and single ones of three others, 32 heads
+// to 8, 103 GFLOP, in 166 us, 620 TFLOP/s.
 constexpr int kPromptTile = 64, kPromptRows = 128;
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_kernel(KvAttnArgs a) {
@@ -918,10 +928,16 @@ void launch(const KvAttnArgs &a, hipStream_t s) {
 // Rows in blocks of 16, or of 128 from 64 rows a sequence and kv head on.  Enough
 // workgroups for four on each of the 256 compute units, two with large blocks,
 // or again four from eight sequences on, whose lengths differ, as long as a split
-// keeps 768 tokens (us with two / with four: a third of 11 sequences with 32 new
-// tokens over up to 23050, 32 heads to 4, 154 / 115; of 4096, 32 heads to 8, half
-// of 24 with 256 new ones 243 / 237 and all of 24 with 24 97 / 93, but all of 8
-// with 24 44 / 57; below eight, 3 with up to 100 over 6000: 55 / 60).  What counts are
+// keeps 768 tokens.  us with two / with four, over 4096 tokens, 32 heads to 8:
+//   new tokens of some sequences, single ones of the rest
+//     256 of every second of 8, 24, 64    130 / 109   243 / 237   536 / 537
+//     256 of every eighth of 8, 16, 24     48 / 50     87 / 78    135 / 103
+//     32 of every eighth of 8, 16, 24      27 / 27     42 / 49     64 / 52
+//   24 of every one of 8, 16, 24, 32, 64   44 / 44    61 / 76     96 / 93   101 / 112   176 / 196
+//   a third of 11 with 32 over up to 23050, 32 heads to 4    154 / 115
+// so that equal sequences can lose (640 workgroups take two rounds of 512) what
+// unequal ones gain; without the 768 all of 8 with 24 take 56.  Below eight, 3 with
+// up to 100 over 6000: 55 / 60.  What counts are
 // blocks that can have rows: 215 tokens of one sequence of 28854 and single ones
 // of seven others, 20 heads to 4, take 1145 us cut as 288 blocks and 171 as 68.
 // No split has less than one block of 32 tokens a wave, or four tiles (512 tokens
