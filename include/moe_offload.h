@@ -491,7 +491,7 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
  * A row of q with an infinity or a NaN, or a scale that is not finite, gives NaN
  * to what sees a token; a scale below fp32's normal range counts as 0.  Where q . K
  * passes fp32's range a row may come out as NaN.  Roundings: bf16 calls hold a
- * probability in one fp16 number (2^-11 of itself, and the sum that divides counts
+ * probability in one fp16 number (2^-10 of itself, and the sum that divides counts
  * the rounded ones), fp32 calls hold q and the probabilities in 22 bits; keys and
  * values are exact.  o may be q itself, at its stride.
  * max_new (new tokens of a sequence) and max_len (tokens of a sequence) say how

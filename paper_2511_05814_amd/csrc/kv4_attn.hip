@@ -294,9 +294,9 @@ __device__ __forceinline__ Seq sequence(const KvAttnArgs &a, int b, int group) {
 // and the splits, as many for every sequence, leave the shorter ones' waves idle;
 // one of 131072, 151 MB, in 41 us with the join (3.7 TB/s), vector lanes busy 79%.
 //
-// A probability is rounded to fp16 in bf16 calls, 2^-11 of itself toward zero,
+// A probability is rounded to fp16 in bf16 calls, up to 2^-10 of itself toward zero,
 // where fp32 would need a second product: the row's sum counts the rounded ones,
-// so only their differences reach the result, which then takes 2^-9 in bf16.  fp32
+// so only their differences reach the result, which then takes 2^-8 in bf16.  fp32
 // calls hold q and the probabilities in 22 bits, two numbers each; a third would
 // be half as many products again for bits that sums of fp32 lose.
 template <int D, typename T>
