@@ -504,6 +504,79 @@ int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, v
                       float scale, int dtype, int max_new, int max_len, void *workspace, size_t workspace_bytes,
                       void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Steps with drafted tokens.  A sequence's new tokens are a tree: the first is
+ * its pending token, each other follows another one of them (its parent), as
+ * one of several guesses.  Token i keeps place kv_len[b] - n + i of the cache,
+ * but its position, for which it is rotated, is that of its depth.  Because the
+ * experts that a layer copies serve all tokens of a call (Sec. 2.2), a few
+ * guesses cost little more than the pending token alone.  The calls in order:
+ * moe_draft_tree once a step; moe_kv4_append_at and moe_kv4_tree_attention in
+ * every layer; moe_verify_drafts; moe_kv4_keep once for all layers. */
+
+/* pos[t] = kv_len[b] - n + depth of t, and bit j % 32 of word j / 32 of
+ * seen[t][words]: whether new token j of the sequence is t or one of its
+ * ancestors.  parent[t] counts within the sequence; one that is not an earlier
+ * token of it (-1) is none.  words is in [1, 32]; a token past the first 32 words
+ * of its sequence gets position -1 and sees no new token. */
+int moe_draft_tree(const int32_t *parent, const int32_t *q_start, const int32_t *kv_len, int seqs, int tokens, int words,
+                   int32_t *pos, uint32_t *seen, void *stream);
+
+/* moe_kv4_append with the positions pos [tokens] (NULL: the places) in the
+ * rotation.  A token at a position outside 0 .. max_pos - 1 is not stored and its
+ * query is zeros; places may lie past max_pos. */
+int moe_kv4_append_at(const moe_kv4_batch *b, const int32_t *pos, const void *q, int64_t q_stride, const void *k,
+                      int64_t k_stride, const void *v, int64_t v_stride, const float *cos, const float *sin, int max_pos,
+                      int rot_dim, void *q_out, int64_t q_out_stride, int heads, int dtype, void *stream);
+
+/* moe_kv4_attention in which a new token sees the tokens that were cached and,
+ * of its sequence's new ones, those whose bits are set in its words of seen
+ * [tokens][words], 1 <= words <= 32: any pattern, itself only if its own bit is
+ * set; bits of tokens that the sequence does not have mean nothing.  The
+ * workspace is moe_kv4_attention_workspace_bytes; roundings, NaN and limits are
+ * those of moe_kv4_attention. */
+int moe_kv4_tree_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, const uint32_t *seen, int words, void *o,
+                           int64_t o_stride, int heads, float scale, int dtype, int max_new, int max_len, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/* Which drafted tokens become the sequence's, such that its tokens are
+ * distributed as the target's own.  Row t of p [tokens][vocab] is the target's
+ * distribution of the token behind t, taken as it is (entries >= 0 that sum to
+ * 1; a negative one counts as 0), row t of q that which t's children were drawn
+ * from, independently and in their order; without q (NULL) they were chosen
+ * otherwise, as the draft's likeliest for one.  Rows of p and q need only be
+ * aligned to their type.  ids [tokens] are the tokens, u [tokens] random numbers
+ * in [0, 1) (less counts as 0).  From a sequence's first token, which
+ * is certain, the walk tries the children c of where it stands, in their order:
+ *   with q     S = 0, T = 1; c is accepted if u[c] T q(c) < max(p(c) - S q(c), 0),
+ *              else S becomes S + T and then T the sum of max(p - S q, 0);
+ *   without q  T = 1; c is accepted if u[c] T < p(c) (0 if its id was tried), else
+ *              T becomes T - p(c);
+ * and goes on from the accepted one.  Where none is, the next token is drawn from
+ * the weights that are left (max(p - S q, 0); without q p without the tried ids;
+ * p itself where they are all 0): the least id with a weight at which the sum of weights up
+ * to it passes u[first] times their sum, or the last with one.  All of this is
+ * computed in fp64, so that it does not depend on the order of a sum.
+ * path [tokens]: at q_start[b] + k the k-th accepted token's number within the
+ * sequence (0 first, ascending), -1 after the last.  count [seqs]: how many; next
+ * [seqs]: the next token.  A sequence without new tokens has count 0 and next -1;
+ * next is also -1 where the weights' sum is 0, infinite or NaN.  An id outside
+ * 0 .. vocab - 1 is refused with weight 0.  Of a sequence's tokens the first 1024
+ * take part; vocab is in [1, 2^24]. */
+int moe_verify_drafts(const void *p, int64_t p_stride, const void *q, int64_t q_stride, const int32_t *ids,
+                      const int32_t *parent, const float *u, const int32_t *q_start, int seqs, int tokens, int vocab,
+                      int dtype, int32_t *path, int32_t *count, int32_t *next, void *stream);
+
+/* The entry in place base + path[q_start[b] + k] of each sequence goes to place
+ * base + k, for k < count[b] (at most the new tokens), base = kv_len[b] - n, in
+ * each of n_pools (1 .. 1024) caches of b's sizes at pools, a host array (b->pool
+ * is not looked at); sequences then have base + count[b] tokens.  A path[..] that
+ * is not one of k .. n - 1 leaves place k as it is, and so does a place without a page.
+ * Other bytes stay.  The caches must not overlap, and no page of a new token
+ * belong to two sequences. */
+int moe_kv4_keep(const moe_kv4_batch *b, void *const *pools, int n_pools, const int32_t *path, const int32_t *count,
+                 void *stream);
+
 /* Norms before and after a block with its gate and residual scale, for rows (at
  * most 2^24; fewer for d past 1024) of d (a multiple of 8 in [8, 16384]) channels:
  *   h_out = residual_scale * h + gate * y',   y' = y * post / rms(y)

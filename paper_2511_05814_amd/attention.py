@@ -83,12 +83,15 @@ def kv4_pool(pages: int, kv_heads: int, page_size: int, head_dim: int, device="c
     return torch.zeros((pages, kv_heads, kv4_record_bytes(page_size, head_dim)), dtype=torch.uint8, device=device)
 
 
-def kv4_append(q, k, v, cos, sin, pool, page_table, q_start, kv_len, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+def kv4_append(q, k, v, cos, sin, pool, page_table, q_start, kv_len, out: Optional[torch.Tensor] = None,
+               pos: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotate the new tokens' q [tokens, heads, head_dim] and k by their
     positions, store k and v [tokens, kv_heads, head_dim] in the cache and
     return the rotated q.  cos and sin: fp32 [positions, rot_dim / 2]; with
-    rot_dim 0 nothing is rotated.  Rows may be slices of a joined projection."""
-    return _ops().kv4_append(q, k, v, cos, sin, pool, page_table, q_start, kv_len, out, _stream(q))
+    rot_dim 0 nothing is rotated.  Rows may be slices of a joined projection.
+    pos (int32 [tokens], `drafts.draft_tree` gives it) has the positions of
+    tokens that are not where their places in the cache are."""
+    return _ops().kv4_append(q, k, v, cos, sin, pool, page_table, q_start, kv_len, out, pos, _stream(q))
 
 
 def kv4_read(pool, page_table, q_start, kv_len, tokens: int, head_dim: int, dtype=torch.float32):
@@ -106,7 +109,27 @@ def kv4_attention(q, pool, page_table, q_start, kv_len, scale: float, max_new: O
     max_len (the longest run of new tokens, the longest sequence) say how to cut
     the work; without them they are taken from the tensors' shapes.  A workspace
     is allocated unless one (uint8) is given."""
-    return _ops().kv4_attention(q, pool, page_table, q_start, kv_len, scale, max_new, max_len, out, workspace, _stream(q))
+    return _ops().kv4_attention(q, pool, page_table, q_start, kv_len, scale, max_new, max_len, out, workspace, None, _stream(q))
+
+
+def kv4_tree_attention(q, pool, page_table, q_start, kv_len, seen, scale: float, max_new: Optional[int] = None,
+                       max_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """`kv4_attention` of a tree of new tokens: each sees what was cached and the
+    new tokens of its sequence that its bits in seen (int32 [tokens, words],
+    `drafts.draft_tree` gives them) name."""
+    return _ops().kv4_attention(q, pool, page_table, q_start, kv_len, scale, max_new, max_len, out, workspace, seen, _stream(q))
+
+
+def kv4_keep(pools, page_table, q_start, kv_len, path, count, head_dim: int) -> None:
+    """Of each sequence's new tokens keep path's first count[b] (as
+    `drafts.verify_drafts` gives them): their entries move to the places right
+    behind the cached tokens, in every one of pools (a cache or a sequence of
+    them, one a layer).  A sequence then has kv_len[b] - n + count[b] tokens."""
+    pools = (pools,) if isinstance(pools, torch.Tensor) else tuple(pools)
+    if not pools:
+        raise ValueError("pools must be one cache or several")
+    _ops().kv4_keep(pools, page_table, q_start, kv_len, path, count, head_dim, _stream(pools[0]))
 
 
 def norm_residual(h, y=None, gate=None, post=None, pre=None, residual_scale: float = 1.0, eps: float = 1e-5,

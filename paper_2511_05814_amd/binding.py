@@ -136,10 +136,18 @@ _SIGNATURES = [
     ("moe_q4_matmul", _I, [_P, _I64, _P, _P, _I64, _I, _I, _I, _I, _P]),
     ("moe_kv4_append", _I,
      [ctypes.POINTER(moe_kv4_batch), _P, _I64, _P, _I64, _P, _I64, _P, _P, _I, _I, _P, _I64, _I, _I, _P]),
+    ("moe_kv4_append_at", _I,
+     [ctypes.POINTER(moe_kv4_batch), _P, _P, _I64, _P, _I64, _P, _I64, _P, _P, _I, _I, _P, _I64, _I, _I, _P]),
     ("moe_kv4_read", _I, [ctypes.POINTER(moe_kv4_batch), _P, _P, _I, _P]),
     ("moe_kv4_attention_workspace_bytes", ctypes.c_size_t, [ctypes.POINTER(moe_kv4_batch), _I, _I, _I]),
     ("moe_kv4_attention", _I,
      [ctypes.POINTER(moe_kv4_batch), _P, _I64, _P, _I64, _I, _F, _I, _I, _I, _P, ctypes.c_size_t, _P]),
+    ("moe_kv4_tree_attention", _I,
+     [ctypes.POINTER(moe_kv4_batch), _P, _I64, _P, _I, _P, _I64, _I, _F, _I, _I, _I, _P, ctypes.c_size_t, _P]),
+    ("moe_kv4_keep", _I, [ctypes.POINTER(moe_kv4_batch), ctypes.POINTER(ctypes.c_void_p), _I, _P, _P, _P]),
+    ("moe_draft_tree", _I, [_P, _P, _P, _I, _I, _I, _P, _P, _P]),
+    ("moe_verify_drafts", _I,
+     [_P, _I64, _P, _I64, _P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P]),
     ("moe_norm_residual", _I,
      [_P, _I64, _P, _I64, _P, _I64, _P, _P, _F, _F, _P, _I64, _P, _I64, _I, _I, _I, _P]),
     ("moe_last_error", ctypes.c_char_p, []),
@@ -328,6 +336,13 @@ def moe_kv4_append(batch: moe_kv4_batch, q: int, q_stride: int, k: int, k_stride
                                 q_out_stride, heads, dtype, stream), "moe_kv4_append")
 
 
+def moe_kv4_append_at(batch: moe_kv4_batch, pos: int, q: int, q_stride: int, k: int, k_stride: int, v: int, v_stride: int,
+                      cos: int, sin: int, max_pos: int, rot_dim: int, q_out: int, q_out_stride: int, heads: int,
+                      dtype: int, stream: int) -> None:
+    _check(lib().moe_kv4_append_at(batch, pos, q, q_stride, k, k_stride, v, v_stride, cos, sin, max_pos, rot_dim, q_out,
+                                   q_out_stride, heads, dtype, stream), "moe_kv4_append_at")
+
+
 def moe_kv4_read(batch: moe_kv4_batch, k: int, v: int, dtype: int, stream: int) -> None:
     _check(lib().moe_kv4_read(batch, k, v, dtype, stream), "moe_kv4_read")
 
@@ -341,6 +356,31 @@ def moe_kv4_attention(batch: moe_kv4_batch, q: int, q_stride: int, o: int, o_str
                       stream: int) -> None:
     _check(lib().moe_kv4_attention(batch, q, q_stride, o, o_stride, heads, scale, dtype, max_new, max_len, workspace,
                                    workspace_bytes, stream), "moe_kv4_attention")
+
+
+def moe_kv4_tree_attention(batch: moe_kv4_batch, q: int, q_stride: int, seen: int, words: int, o: int, o_stride: int,
+                           heads: int, scale: float, dtype: int, max_new: int, max_len: int, workspace: int,
+                           workspace_bytes: int, stream: int) -> None:
+    _check(lib().moe_kv4_tree_attention(batch, q, q_stride, seen, words, o, o_stride, heads, scale, dtype, max_new,
+                                        max_len, workspace, workspace_bytes, stream), "moe_kv4_tree_attention")
+
+
+def moe_kv4_keep(batch: moe_kv4_batch, pools, path: int, count: int, stream: int) -> None:
+    """pools: the caches' device addresses."""
+    array = (ctypes.c_void_p * len(pools))(*pools)
+    _check(lib().moe_kv4_keep(batch, array, len(pools), path, count, stream), "moe_kv4_keep")
+
+
+def moe_draft_tree(parent: int, q_start: int, kv_len: int, seqs: int, tokens: int, words: int, pos: int, seen: int,
+                   stream: int) -> None:
+    _check(lib().moe_draft_tree(parent, q_start, kv_len, seqs, tokens, words, pos, seen, stream), "moe_draft_tree")
+
+
+def moe_verify_drafts(p: int, p_stride: int, q: int, q_stride: int, ids: int, parent: int, u: int, q_start: int,
+                      seqs: int, tokens: int, vocab: int, dtype: int, path: int, count: int, next_: int,
+                      stream: int) -> None:
+    _check(lib().moe_verify_drafts(p, p_stride, q, q_stride, ids, parent, u, q_start, seqs, tokens, vocab, dtype, path,
+                                   count, next_, stream), "moe_verify_drafts")
 
 
 def moe_norm_residual(h: int, h_stride: int, y: int, y_stride: int, gate: int, gate_stride: int, post: int, pre: int,

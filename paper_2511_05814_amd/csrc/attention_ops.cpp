@@ -1,4 +1,4 @@
-// CPython module behind paper_2511_05814_amd.attention: checks of tensors,
+// CPython module behind paper_2511_05814_amd.attention and .drafts: checks of tensors,
 // allocation of results and the calls of the C ABI (include/moe_offload.h).
 //
 // A decode step makes a dozen of these calls a layer, and a kernel launch takes
@@ -12,6 +12,8 @@
 #include <ATen/ATen.h>
 #include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <vector>
 
 #include "moe_offload.h"
 
@@ -182,7 +184,7 @@ PyObject *q4_matmul(PyObject *, PyObject *const *a, Py_ssize_t got) {
 }
 
 PyObject *kv4_append(PyObject *, PyObject *const *a, Py_ssize_t got) {
-  return call(got, 11, [&] {
+  return call(got, 12, [&] {
     const at::Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &cos = tensor(a[3], "cos"), &sin = tensor(a[4], "sin");
     dims("q", q, 3, "[tokens, heads, head_dim]");
     dims("cos", cos, 2, "[positions, rot_dim / 2]");
@@ -197,9 +199,10 @@ PyObject *kv4_append(PyObject *, PyObject *const *a, Py_ssize_t got) {
     const int64_t vs = rows("v", v, at_.device, at_.type, {t, (int64_t)b.kv_heads, d});
     at::Tensor o = given(a[9]) ? tensor(a[9], "out") : at::empty({t, heads, d}, q.options());
     const int64_t os = given(a[9]) ? rows("out", o, at_.device, at_.type, {t, heads, d}) : heads * d;
-    check_rc(moe_kv4_append(&b, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, static_cast<const float *>(cos.data_ptr()),
+    const void *pos = given(a[10]) ? vector("pos", tensor(a[10], "pos"), at_.device, at::kInt, t) : nullptr;
+    check_rc(moe_kv4_append_at(&b, static_cast<const int32_t *>(pos), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, static_cast<const float *>(cos.data_ptr()),
                             static_cast<const float *>(sin.data_ptr()), small(positions), small(2 * half), o.data_ptr(), os, small(heads),
-                            at_.code, stream_of(a[10])), "moe_kv4_append");
+                            at_.code, stream_of(a[11])), "moe_kv4_append");
     return THPVariable_Wrap(std::move(o));
   });
 }
@@ -218,7 +221,7 @@ PyObject *kv4_read(PyObject *, PyObject *const *a, Py_ssize_t got) {
 }
 
 PyObject *kv4_attention(PyObject *, PyObject *const *a, Py_ssize_t got) {
-  return call(got, 11, [&] {
+  return call(got, 12, [&] {
     const at::Tensor &q = tensor(a[0], "q");
     dims("q", q, 3, "[tokens, heads, head_dim]");
     const int64_t t = q.size(0), heads = q.size(1), d = q.size(2);
@@ -240,9 +243,89 @@ PyObject *kv4_attention(PyObject *, PyObject *const *a, Py_ssize_t got) {
       bytes = moe_kv4_attention_workspace_bytes(&b, small(heads), max_new, max_len);
       if (bytes) workspace = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
     }
-    check_rc(moe_kv4_attention(&b, q.data_ptr(), qs, o.data_ptr(), os, small(heads), (float)real(a[5]), at_.code, max_new, max_len,
-                               bytes ? workspace.data_ptr() : nullptr, bytes, stream_of(a[10])), "moe_kv4_attention");
+    void *const ws = bytes ? workspace.data_ptr() : nullptr, *const stream = stream_of(a[11]);
+    const float scale = (float)real(a[5]);
+    if (given(a[10])) {
+      const at::Tensor &seen = tensor(a[10], "seen");
+      dims("seen", seen, 2, "[tokens, words]");
+      rows("seen", seen, at_.device, at::kInt, {t, seen.size(1)});
+      if (!seen.is_contiguous()) value_error("seen must be contiguous");
+      check_rc(moe_kv4_tree_attention(&b, q.data_ptr(), qs, static_cast<const uint32_t *>(seen.data_ptr()), small(seen.size(1)), o.data_ptr(),
+                                      os, small(heads), scale, at_.code, max_new, max_len, ws, bytes, stream), "moe_kv4_tree_attention");
+    } else {
+      check_rc(moe_kv4_attention(&b, q.data_ptr(), qs, o.data_ptr(), os, small(heads), scale, at_.code, max_new, max_len, ws, bytes, stream),
+               "moe_kv4_attention");
+    }
     return THPVariable_Wrap(std::move(o));
+  });
+}
+
+PyObject *draft_tree(PyObject *, PyObject *const *a, Py_ssize_t got) {
+  return call(got, 5, [&] {
+    const at::Tensor &parent = tensor(a[0], "parent"), &start = tensor(a[1], "q_start"), &length = tensor(a[2], "kv_len");
+    const int64_t most = integer(a[3]);
+    dims("parent", parent, 1, "[tokens]");
+    dims("kv_len", length, 1, "[sequences]");
+    if (!parent.is_cuda()) value_error("tensors must be on the GPU, not on " + parent.device().str());
+    const int device = parent.get_device();
+    const int64_t t = parent.size(0), seqs = length.size(0), words = most < 1 ? 0 : small((most - 1) / 32 + 1);
+    const void *p = vector("parent", parent, device, at::kInt, t), *s = vector("q_start", start, device, at::kInt, seqs + 1);
+    const void *l = vector("kv_len", length, device, at::kInt, seqs);
+    if (words < 1 || words > 32) value_error("max_new must be in [1, 1024], not " + std::to_string(most));
+    at::Tensor pos = at::empty({t}, parent.options()), seen = at::empty({t, words}, parent.options());
+    check_rc(moe_draft_tree(static_cast<const int32_t *>(p), static_cast<const int32_t *>(s), static_cast<const int32_t *>(l), small(seqs),
+                            small(t), (int)words, static_cast<int32_t *>(pos.data_ptr()), static_cast<uint32_t *>(seen.data_ptr()),
+                            stream_of(a[4])), "moe_draft_tree");
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(pos)), THPVariable_Wrap(std::move(seen)));
+  });
+}
+
+PyObject *verify_drafts(PyObject *, PyObject *const *a, Py_ssize_t got) {
+  return call(got, 7, [&] {
+    const at::Tensor &p = tensor(a[0], "p"), &ids = tensor(a[1], "tokens"), &parent = tensor(a[2], "parent"), &u = tensor(a[3], "u"), &start = tensor(a[4], "q_start");
+    dims("p", p, 2, "[tokens, vocabulary]");
+    dims("q_start", start, 1, "[sequences + 1]");
+    const int64_t t = p.size(0), vocab = p.size(1), seqs = start.size(0) - 1;
+    const Where at_ = where(p, p.scalar_type());
+    const int64_t ps = rows("p", p, at_.device, at_.type, {t, vocab});
+    const void *q = nullptr;
+    int64_t qs = vocab;
+    if (given(a[5])) {
+      qs = rows("q", tensor(a[5], "q"), at_.device, at_.type, {t, vocab});
+      q = tensor(a[5], "q").data_ptr();
+    }
+    const void *i = vector("tokens", ids, at_.device, at::kInt, t), *c = vector("parent", parent, at_.device, at::kInt, t);
+    const void *r = vector("u", u, at_.device, at::kFloat, t), *s = vector("q_start", start, at_.device, at::kInt, seqs + 1);
+    at::Tensor path = at::empty({t}, ids.options()), count = at::empty({std::max<int64_t>(0, seqs)}, ids.options()), next = at::empty_like(count);
+    check_rc(moe_verify_drafts(p.data_ptr(), ps, q, qs, static_cast<const int32_t *>(i), static_cast<const int32_t *>(c),
+                               static_cast<const float *>(r), static_cast<const int32_t *>(s), small(seqs), small(t), small(vocab), at_.code,
+                               static_cast<int32_t *>(path.data_ptr()), static_cast<int32_t *>(count.data_ptr()),
+                               static_cast<int32_t *>(next.data_ptr()), stream_of(a[6])), "moe_verify_drafts");
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(path)), THPVariable_Wrap(std::move(count)), THPVariable_Wrap(std::move(next)));
+  });
+}
+
+PyObject *kv4_keep(PyObject *, PyObject *const *a, Py_ssize_t got) {
+  return call(got, 8, [&] {
+    if (!PyTuple_Check(a[0]) || !PyTuple_GET_SIZE(a[0])) value_error("pools must be one cache or several");
+    const Py_ssize_t n = PyTuple_GET_SIZE(a[0]);
+    const at::Tensor &first = tensor(PyTuple_GET_ITEM(a[0], 0), "pools"), &path = tensor(a[4], "path"), &count = tensor(a[5], "count");
+    if (!first.is_cuda()) value_error("tensors must be on the GPU, not on " + first.device().str());
+    dims("path", path, 1, "[tokens]");
+    const int device = first.get_device();
+    const int64_t t = path.size(0);
+    const moe_kv4_batch b = batch_of(device, first, tensor(a[1], "page_table"), tensor(a[2], "q_start"), tensor(a[3], "kv_len"), t, integer(a[6]));
+    std::vector<void *> pools;
+    for (Py_ssize_t i = 0; i < n; ++i) {
+      const at::Tensor &pool = tensor(PyTuple_GET_ITEM(a[0], i), "pools");
+      if (pool.sizes() != first.sizes() || pool.scalar_type() != at::kByte || !pool.is_contiguous() || !pool.is_cuda() || pool.get_device() != device)
+        bad("pools", pool, at::kByte, first.sizes(), device);
+      pools.push_back(pool.data_ptr());
+    }
+    const void *p = vector("path", path, device, at::kInt, t), *c = vector("count", count, device, at::kInt, b.seqs);
+    check_rc(moe_kv4_keep(&b, pools.data(), small(n), static_cast<const int32_t *>(p), static_cast<const int32_t *>(c), stream_of(a[7])),
+             "moe_kv4_keep");
+    Py_RETURN_NONE;
   });
 }
 
@@ -314,7 +397,8 @@ PyObject *set_errors(PyObject *, PyObject *args) {
 }
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FAST(q4_matmul), FAST(kv4_append), FAST(kv4_read), FAST(kv4_attention), FAST(norm_residual),
+PyMethodDef methods[] = {FAST(q4_matmul), FAST(kv4_append), FAST(kv4_read), FAST(kv4_attention), FAST(norm_residual), FAST(kv4_keep),
+                         FAST(draft_tree), FAST(verify_drafts),
                          {"set_errors", set_errors, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_attention_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -293,6 +293,7 @@ struct KvAppendArgs {
   void *q_out;
   int64_t q_stride, k_stride, v_stride, q_out_stride;  // elements between tokens
   const float *cos, *sin;      // [max_pos][rot / 2]
+  const int32_t *pos;          // [tokens], positions of the rotation; NULL: the places
   int max_pos, rot, heads;
 };
 struct KvReadArgs {
@@ -308,9 +309,20 @@ struct KvAttnArgs {
   float *ml;                   // [splits][tokens * heads][2]
   float scale;
   int heads, splits, row_blocks, prompt;
+  const uint32_t *seen;        // [tokens][words], which new tokens a token sees; NULL: those before it
+  int words;
+};
+// Moves entries of new tokens to the places right behind the cached ones.
+constexpr int kKeepPools = 64;   // caches of a launch
+struct KvKeepArgs {
+  Kv4 kv;                      // kv.pool unused
+  uint8_t *pools[kKeepPools];
+  const int32_t *path;         // [tokens]
+  const int32_t *count;        // [seqs]
 };
 hipError_t launch_kv4_append(const KvAppendArgs &a, int head_dim, bool f32, hipStream_t s);
 hipError_t launch_kv4_read(const KvReadArgs &a, int head_dim, bool f32, hipStream_t s);
+hipError_t launch_kv4_keep(const KvKeepArgs &a, int pools, int head_dim, hipStream_t s);
 // How a launch of kv4_attention is cut: splits of the keys, workgroups along the
 // rows, and whether rows go in the large blocks of the prompt kernel.
 struct KvAttnShape {
@@ -318,6 +330,28 @@ struct KvAttnShape {
 };
 KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len);
 hipError_t launch_kv4_attention(const KvAttnArgs &a, int head_dim, bool f32, hipStream_t s);
+
+// Trees of drafted tokens.
+constexpr int kMaxTree = 1024;   // tokens of a sequence that can be in its tree
+struct DraftTreeArgs {
+  const int32_t *parent;       // [tokens], within the sequence
+  const int32_t *q_start, *kv_len;
+  int32_t *pos;                // [tokens]
+  uint32_t *seen;              // [tokens][words]
+  int seqs, tokens, words;
+};
+hipError_t launch_draft_tree(const DraftTreeArgs &a, hipStream_t s);
+struct VerifyArgs {
+  const void *p, *q;           // [tokens][vocab]; q may be NULL
+  int64_t p_stride, q_stride;
+  const int32_t *ids, *parent; // [tokens]
+  const float *u;              // [tokens]
+  const int32_t *q_start;
+  int32_t *path;               // [tokens]
+  int32_t *count, *next;       // [seqs]
+  int seqs, tokens, vocab;
+};
+hipError_t launch_verify_drafts(const VerifyArgs &a, bool f32, hipStream_t s);
 
 struct Q4Args {
   const void *x;

@@ -96,13 +96,14 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(KvAppendArgs a) {
   src += head * D;
   float x[8];
   load8(src + 8 * o, x);
-  const bool placed = pos >= 0 && pos < a.max_pos;
+  const int turn = a.pos ? a.pos[t] : pos;   // the position that it is rotated for
+  const bool placed = pos >= 0 && turn >= 0 && turn < a.max_pos;
   if (!value && 8 * o < a.rot && placed) {
     const int half = a.rot / 2, i = 8 * o < half ? 8 * o : 8 * o - half;
     float other[8], c[8], s[8];
     load8(src + (8 * o < half ? 8 * o + half : 8 * o - half), other);
-    load8(a.cos + (size_t)pos * half + i, c);
-    load8(a.sin + (size_t)pos * half + i, s);
+    load8(a.cos + (size_t)turn * half + i, c);
+    load8(a.sin + (size_t)turn * half + i, s);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float p = x[e] * c[e], r = other[e] * s[e];
@@ -180,6 +181,55 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(KvReadArgs a) {
   store8(out + ((int64_t)t * a.kv.kv_heads + head) * D + 8 * o, x);
 }
 
+// Entry base + path[k] of a sequence to base + k, k below count, base its first
+// new place; one workgroup a cache and sequence, D / 8 lanes an entry.  A path
+// that does not go back (path[k] >= k; others are left alone) lets groups of
+// entries go in order, each read whole before it is written: what a group reads
+// lies at or past its own first place, and earlier groups wrote below that.
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv4_keep_kernel(KvKeepArgs a) {
+  constexpr int kLanes = D / 8, kItems = kThreads / kLanes;
+  const int seq = blockIdx.x, o = threadIdx.x % kLanes, item = threadIdx.x / kLanes;
+  Kv4 kv = a.kv;
+  kv.pool = a.pools[blockIdx.y];
+  const int start = min(max(kv.q_start[seq], 0), kv.tokens), end = min(max(kv.q_start[seq + 1], start), kv.tokens);
+  const int n = end - start, kept = min(a.count[seq], n), base = kv.kv_len[seq] - n;
+  for (int head = 0; head < kv.kv_heads; ++head) {
+    for (int k0 = 0; k0 < kept; k0 += kItems) {
+      const int k = k0 + item;
+      uint8_t *from = nullptr, *to = nullptr;
+      uint32_t codes[2];
+      uint16_t metas[2];
+      int in_to = 0;
+      if (k < kept) {
+        const int source = a.path[start + k];
+        if (source > k && source < n) {
+          from = record_of<D>(kv, seq, base + source, head);
+          to = record_of<D>(kv, seq, base + k, head);
+          const int mask = (1 << kv.page_log2) - 1, in = (base + source) & mask;
+          in_to = (base + k) & mask;
+          if (from && to) {
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              codes[v] = *reinterpret_cast<const uint32_t *>(from + code_at<D>(kv, v, in, o));
+              metas[v] = *reinterpret_cast<const uint16_t *>(from + meta_at<D>(kv, v, in, o / 4));
+            }
+          }
+        }
+      }
+      __syncthreads();
+      if (from && to) {
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          *reinterpret_cast<uint32_t *>(to + code_at<D>(kv, v, in_to, o)) = codes[v];
+          if (o % 4 == 0) *reinterpret_cast<uint16_t *>(to + meta_at<D>(kv, v, in_to, o / 4)) = metas[v];
+        }
+      }
+      __syncthreads();
+    }
+  }
+}
+
 template <int D>
 unsigned blocks(int64_t items) {
   return (unsigned)((items * (D / 8) + kThreads - 1) / kThreads);
@@ -196,6 +246,13 @@ hipError_t launch_kv4_append(const KvAppendArgs &a, int head_dim, bool f32, hipS
     if (f32) hipLaunchKernelGGL((kv4_append_kernel<128, float>), dim3(blocks<128>(items)), dim3(kThreads), 0, s, a);
     else hipLaunchKernelGGL((kv4_append_kernel<128, uint16_t>), dim3(blocks<128>(items)), dim3(kThreads), 0, s, a);
   }
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_keep(const KvKeepArgs &a, int pools, int head_dim, hipStream_t s) {
+  const dim3 grid((unsigned)a.kv.seqs, (unsigned)pools);
+  if (head_dim == 64) hipLaunchKernelGGL((kv4_keep_kernel<64>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((kv4_keep_kernel<128>), grid, dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -1,6 +1,7 @@
 // Attention over the 4-bit paged cache (kv4.hip has its layout):
 //   o[t][h] = sum_j softmax_j(scale q[t][h] . k_j) v_j,
-// j over the positions 0 .. p of t's sequence, p the position of t; a row
+// j over the positions 0 .. p of t's sequence, p the position of t, or, of a tree
+// of tokens, over the cached tokens and the new ones that t's bits name; a row
 // without any gets zeros.
 #include "common.hpp"
 
@@ -260,6 +261,15 @@ __device__ __forceinline__ Place place(const KvAttnArgs &a) {
 typedef const int32_t __attribute__((address_space(4))) *ScalarInts;
 __device__ __forceinline__ ScalarInts scalar_ints(const int32_t *p) { return (ScalarInts)(uintptr_t)p; }
 
+// A row's view of the 32 tokens from `rel` places past the first new one on, as
+// bits: tokens that were cached are seen by all, new ones where the row of
+// `words` words says so.
+__device__ __forceinline__ uint32_t tree_bits(const uint32_t *row, int words, int rel) {
+  const int w = rel >> 5;
+  const uint32_t lo = w < 0 ? ~0u : w < words ? row[w] : 0u, hi = w + 1 < 0 ? ~0u : w + 1 < words ? row[w + 1] : 0u;
+  return __builtin_amdgcn_alignbit(hi, lo, rel & 31);
+}
+
 // What a workgroup needs to know of its sequence.
 struct Seq {
   int start, rows;   // first new token; rows = new tokens * heads a kv head
@@ -299,7 +309,9 @@ __device__ __forceinline__ Seq sequence(const KvAttnArgs &a, int b, int group) {
 // so only their differences reach the result, which then takes 2^-8 in bf16.  fp32
 // calls hold q and the probabilities in 22 bits, two numbers each; a third would
 // be half as many products again for bits that sums of fp32 lose.
-template <int D, typename T>
+//
+// TREE: rows see the cached tokens and what their words of `seen` name.
+template <int D, typename T, bool TREE>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void kv4_attention_kernel(KvAttnArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
   constexpr int KW = D / 32;   // words of codes of a lane's part of a key, steps of the dot product
@@ -324,8 +336,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void 
     const int row = min(row0 + r, seq.rows - 1);
     const int token = seq.start + row / group, head = g * group + row % group;
     const int last = min(seq.first + row / group, seq.held - 1);  // this row's last position
-    const int least = min(seq.first + row0 / group, seq.held - 1);  // the first row's
-    const int end = min(seq.first + (min(row0 + 15, seq.rows - 1)) / group, seq.held - 1) + 1;
+    const int least = TREE ? min(seq.first, seq.held) - 1 : min(seq.first + row0 / group, seq.held - 1);  // the last that all rows see
+    const int end = TREE ? min(seq.first + seq.rows / group, seq.held)
+                         : min(seq.first + (min(row0 + 15, seq.rows - 1)) / group, seq.held - 1) + 1;
+    const uint32_t *mine = TREE ? a.seen + (int64_t)token * a.words : nullptr;
 
     // the row of q, scaled by a power of two to a largest value of 2^9 .. 2^10
     half8 q[PARTS][KW];
@@ -433,12 +447,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void 
         for (int i = 0; i < 4; ++i) s[h][i] = acc[i];
       }
       const bool whole = held[0] && held[1] && t0 + kTile - 1 <= least;
+      uint32_t bits = ~0u;   // TREE: of this lane's tokens 4 j .. and 16 + 4 j .. of the block
       if (!whole) {
+        if constexpr (TREE) bits = tree_bits(mine, a.words, t0 - seq.first) >> (4 * j);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!held[h] || t0 + 16 * h + 4 * j + i > last) s[h][i] = -__builtin_inff();
+          for (int i = 0; i < 4; ++i) {
+            const int at = t0 + 16 * h + 4 * j + i;
+            if (!held[h] || (TREE ? at >= end || !(bits >> (16 * h + i) & 1) : at > last)) s[h][i] = -__builtin_inff();
+          }
       }
       fetch_keys(t0 + step);
       // softmax of the block
@@ -491,7 +509,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void 
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           mark[e] = (_Float16)((metas[e / 2] >> (16 * (e % 2) + 8) & 255) == 255 ? 1.0f : 0.0f);
-          seen[e] = (_Float16)(t0 + 16 * (e / 4) + 4 * j + e % 4 <= last ? 1.0f : 0.0f);
+          seen[e] = (_Float16)((TREE ? bits >> (16 * (e / 4) + e % 4) & 1 : t0 + 16 * (e / 4) + 4 * j + e % 4 <= last) ? 1.0f : 0.0f);
         }
         floatx4 count = {};
         count = __builtin_amdgcn_mfma_f32_16x16x32_f16(mark, seen, count, 0, 0, 0);
@@ -570,7 +588,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 3 : 4) void 
 // new tokens of one sequence over 2048, and single ones of three others, 32 heads
 // to 8, 103 GFLOP, in 166 us, 620 TFLOP/s.
 constexpr int kPromptTile = 64, kPromptRows = 128;
-template <int D, typename T>
+template <int D, typename T, bool TREE>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_kernel(KvAttnArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
   constexpr int KS = D / 16;           // steps of a score's dot product
@@ -607,9 +625,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
     const int row = min(wrow + r, seq.rows - 1);
     const int token = seq.start + row / group, head = g * group + row % group;
     const int last = min(seq.first + row / group, seq.held - 1);
-    const int wfirst = min(seq.first + min(wrow, seq.rows - 1) / group, seq.held - 1);
-    const int wend = wrow < seq.rows ? min(seq.first + min(wrow + 31, seq.rows - 1) / group, seq.held - 1) + 1 : 0;
-    const int end = min(seq.first + min(block * kPromptRows + kPromptRows - 1, seq.rows - 1) / group, seq.held - 1) + 1;
+    const int wfirst = TREE ? min(seq.first, seq.held) - 1 : min(seq.first + min(wrow, seq.rows - 1) / group, seq.held - 1);
+    const int all = min(seq.first + seq.rows / group, seq.held);   // TREE: where the sequence ends
+    const int wend = wrow >= seq.rows ? 0 : TREE ? all : min(seq.first + min(wrow + 31, seq.rows - 1) / group, seq.held - 1) + 1;
+    const int end = TREE ? all : min(seq.first + min(block * kPromptRows + kPromptRows - 1, seq.rows - 1) / group, seq.held - 1) + 1;
+    const uint32_t *mine = TREE ? a.seen + (int64_t)token * a.words : nullptr;
 
     half8 q[PARTS][KS];
     const T *qp = static_cast<const T *>(a.q) + token * a.q_stride + head * D + 8 * hi;
@@ -746,15 +766,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
       __builtin_amdgcn_sched_barrier(0);
       const u32x4 any4 = *reinterpret_cast<const u32x4 *>(s_any[buf]);
       const uint32_t any = __builtin_amdgcn_readfirstlane(any4[0] | any4[1] | any4[2] | any4[3]);
+      uint32_t bits[2] = {~0u, ~0u};   // TREE: of this lane's tokens of both blocks, shifted by 4 hi
       if (t0 + kPromptTile - 1 > wfirst || (any & 2)) {
+        if constexpr (TREE) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) bits[x] = tree_bits(mine, a.words, t0 + 32 * x - seq.first) >> (4 * hi);
+        }
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           bool held;
           page_of(t0 + 16 * x, held);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int at = t0 + 16 * x + 8 * (i / 4) + 4 * hi + i % 4;
-            if (at > last || !held) s[x / 2][8 * (x % 2) + i] = -__builtin_inff();
+            const int in = 8 * (i / 4) + i % 4, at = t0 + 16 * x + 4 * hi + in;
+            if ((TREE ? at >= end || !(bits[x / 2] >> (16 * (x % 2) + in) & 1) : at > last) || !held) s[x / 2][8 * (x % 2) + i] = -__builtin_inff();
           }
         }
       }
@@ -803,9 +828,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
           half8 mark, seen;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const int at = 16 * x + 8 * (e / 4) + 4 * hi + e % 4;
+            const int in = 8 * (e / 4) + e % 4, at = 16 * x + 4 * hi + in;
             mark[e] = (_Float16)(any4[x / 2 + 2 * (x % 2)] & 1 ? (float)marks[at] : 0.0f);
-            seen[e] = (_Float16)(t0 + at <= last ? 1.0f : 0.0f);
+            seen[e] = (_Float16)((TREE ? bits[x / 2] >> (16 * (x % 2) + in) & 1 : t0 + at <= last) ? 1.0f : 0.0f);
           }
           count = __builtin_amdgcn_mfma_f32_32x32x16_f16(mark, seen, count, 0, 0, 0);
         }
@@ -914,8 +939,10 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(KvAttnArgs a) {
 template <int D, typename T>
 void launch(const KvAttnArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)a.kv.seqs * a.kv.kv_heads * a.row_blocks * a.splits);
-  if (a.prompt) hipLaunchKernelGGL((kv4_prompt_kernel<D, T>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((kv4_attention_kernel<D, T>), grid, dim3(kThreads), 0, s, a);
+  if (a.prompt && a.seen) hipLaunchKernelGGL((kv4_prompt_kernel<D, T, true>), grid, dim3(kThreads), 0, s, a);
+  else if (a.prompt) hipLaunchKernelGGL((kv4_prompt_kernel<D, T, false>), grid, dim3(kThreads), 0, s, a);
+  else if (a.seen) hipLaunchKernelGGL((kv4_attention_kernel<D, T, true>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((kv4_attention_kernel<D, T, false>), grid, dim3(kThreads), 0, s, a);
   if (a.splits == 1) return;
   const int64_t rows = (int64_t)a.kv.tokens * a.heads;
   constexpr int kGroups = kThreads / (D / 4);

@@ -1,4 +1,7 @@
-// C entries of the attention half of a layer: argument checks and launches.
+// C entries of the attention half of a layer and of drafted tokens: argument
+// checks and launches.
+#include <algorithm>
+
 #include "common.hpp"
 #include "moe_offload.h"
 
@@ -119,6 +122,19 @@ Kv4 kv_of(const moe_kv4_batch *b) {
   return k;
 }
 
+int check_tree(const int32_t *q_start, int seqs, int tokens) {
+  if (seqs < 1 || seqs > 1 << 20) return fail(MOE_ERR_ARG, "seqs must be in [1, 2^20]");
+  if (tokens < 0 || tokens > 1 << 24) return fail(MOE_ERR_ARG, "tokens must be in [0, 2^24]");
+  if (!q_start || misaligned(q_start, 4)) return fail(MOE_ERR_ARG, "q_start must be a non-NULL device array of int32");
+  return MOE_OK;
+}
+
+// An array of 4-byte elements, non-NULL if it has any.
+int check_ints(const char *name, const void *p, int n) {
+  if ((!p && n) || misaligned(p, 4)) return fail(MOE_ERR_ARG, "%s must be a non-NULL device pointer aligned to 4 bytes", name);
+  return MOE_OK;
+}
+
 #define CHECK(expr)                    \
   do {                                 \
     const int rc_ = (expr);            \
@@ -165,7 +181,15 @@ int moe_q4_matmul(const void *x, int64_t x_stride, const void *w, void *y, int64
 int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                    const void *v, int64_t v_stride, const float *cos, const float *sin, int max_pos, int rot_dim,
                    void *q_out, int64_t q_out_stride, int heads, int dtype, void *stream) {
+  return moe_kv4_append_at(b, nullptr, q, q_stride, k, k_stride, v, v_stride, cos, sin, max_pos, rot_dim, q_out, q_out_stride, heads,
+                           dtype, stream);
+}
+
+int moe_kv4_append_at(const moe_kv4_batch *b, const int32_t *pos, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                      const void *v, int64_t v_stride, const float *cos, const float *sin, int max_pos, int rot_dim,
+                      void *q_out, int64_t q_out_stride, int heads, int dtype, void *stream) {
   CHECK(check_batch(b));
+  if (misaligned(pos, 4)) return fail(MOE_ERR_ARG, "pos must be a device array of int32");
   CHECK(check_dtype(dtype));
   CHECK(check_heads(b, heads));
   const int bytes = element(dtype), d = b->head_dim;
@@ -189,6 +213,10 @@ int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, cons
   CHECK(check_apart("the cache", pool, "q", qs));
   CHECK(check_apart("the cache", pool, "k", ks));
   CHECK(check_apart("the cache", pool, "v", vs));
+  if (pos) {
+    CHECK(check_apart("q_out", to, "pos", block_of(pos, (int64_t)b->tokens * 4)));
+    CHECK(check_apart("the cache", pool, "pos", block_of(pos, (int64_t)b->tokens * 4)));
+  }
   if (rot_dim) {
     const Span c = block_of(cos, (int64_t)max_pos * rot_dim * 2), n = block_of(sin, (int64_t)max_pos * rot_dim * 2);
     CHECK(check_apart("q_out", to, "cos", c));
@@ -208,6 +236,7 @@ int moe_kv4_append(const moe_kv4_batch *b, const void *q, int64_t q_stride, cons
   a.q_out_stride = q_out_stride;
   a.cos = cos;
   a.sin = sin;
+  a.pos = pos;
   a.max_pos = max_pos;
   a.rot = rot_dim;
   a.heads = heads;
@@ -238,9 +267,13 @@ size_t moe_kv4_attention_workspace_bytes(const moe_kv4_batch *b, int heads, int 
   return splits == 1 ? 0 : (size_t)splits * b->tokens * heads * (b->head_dim + 2) * sizeof(float);
 }
 
-int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, void *o, int64_t o_stride, int heads,
-                      float scale, int dtype, int max_new, int max_len, void *workspace, size_t workspace_bytes,
-                      void *stream) {
+}  // extern "C"
+
+namespace {
+
+// Both attentions; `seen` is NULL where tokens see what is before them.
+int attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, const uint32_t *seen, int words, void *o, int64_t o_stride,
+              int heads, float scale, int dtype, int max_new, int max_len, void *workspace, size_t workspace_bytes, void *stream) {
   CHECK(check_batch(b));
   CHECK(check_dtype(dtype));
   CHECK(check_heads(b, heads));
@@ -269,14 +302,143 @@ int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, v
   const Span to = rows_of(o, o_stride, (int64_t)heads * d, bytes, b->tokens), qs = rows_of(q, q_stride, (int64_t)heads * d, bytes, b->tokens);
   CHECK(check_apart("o", to, "q", qs, true));
   CHECK(check_apart("o", to, "the cache", pool_of(b)));
+  const Span bits = block_of(seen, (int64_t)b->tokens * words * 4);
+  CHECK(check_apart("o", to, "seen", bits));
   if (need) {
+    CHECK(check_apart("the workspace", block_of(workspace, (int64_t)need), "seen", bits));
     CHECK(check_apart("the workspace", block_of(workspace, (int64_t)need), "q", qs));
     CHECK(check_apart("the workspace", block_of(workspace, (int64_t)need), "o", to));
     CHECK(check_apart("the workspace", block_of(workspace, (int64_t)need), "the cache", pool_of(b)));
   }
   a.part = static_cast<float *>(workspace);
   a.ml = a.part ? a.part + (size_t)a.splits * rows * d : nullptr;
+  a.seen = seen;
+  a.words = words;
   return launched(launch_kv4_attention(a, d, dtype == MOE_DTYPE_F32, static_cast<hipStream_t>(stream)), "cache attention");
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, void *o, int64_t o_stride, int heads,
+                      float scale, int dtype, int max_new, int max_len, void *workspace, size_t workspace_bytes,
+                      void *stream) {
+  return attention(b, q, q_stride, nullptr, 0, o, o_stride, heads, scale, dtype, max_new, max_len, workspace, workspace_bytes, stream);
+}
+
+int moe_kv4_tree_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, const uint32_t *seen, int words, void *o,
+                           int64_t o_stride, int heads, float scale, int dtype, int max_new, int max_len, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+  if (words < 1 || words > kMaxTree / 32) return fail(MOE_ERR_ARG, "words must be in [1, %d], not %d", kMaxTree / 32, words);
+  if (!seen || misaligned(seen, 4)) return fail(MOE_ERR_ARG, "seen must be a non-NULL device array of uint32");
+  return attention(b, q, q_stride, seen, words, o, o_stride, heads, scale, dtype, max_new, max_len, workspace, workspace_bytes, stream);
+}
+
+int moe_kv4_keep(const moe_kv4_batch *b, void *const *pools, int n_pools, const int32_t *path, const int32_t *count, void *stream) {
+  constexpr int kMost = 1024;
+  if (!b || !pools || n_pools < 1 || n_pools > kMost) return fail(MOE_ERR_ARG, "NULL batch or pools, or not 1 .. %d of them", kMost);
+  uintptr_t at[kMost];
+  moe_kv4_batch each = *b;
+  for (int i = 0; i < n_pools; ++i) {
+    each.pool = pools[i];
+    CHECK(check_batch(&each));
+    CHECK(check_apart("a cache", pool_of(&each), "path", block_of(path, (int64_t)b->tokens * 4)));
+    CHECK(check_apart("a cache", pool_of(&each), "count", block_of(count, (int64_t)b->seqs * 4)));
+    at[i] = reinterpret_cast<uintptr_t>(pools[i]);
+  }
+  CHECK(check_ints("path", path, b->tokens));
+  CHECK(check_ints("count", count, b->tokens));
+  if (b->tokens == 0) return MOE_OK;
+  // one cache twice would move its entries twice at once
+  std::sort(at, at + n_pools);
+  const uintptr_t bytes = (uintptr_t)pool_of(&each).stride * (uintptr_t)b->pages;
+  for (int i = 1; i < n_pools; ++i)
+    if (at[i] - at[i - 1] < bytes) return fail(MOE_ERR_ARG, "two caches overlap");
+  KvKeepArgs a;
+  a.path = path;
+  a.count = count;
+  for (int i = 0; i < n_pools; i += kKeepPools) {
+    const int n = std::min(kKeepPools, n_pools - i);
+    a.kv = kv_of(&each);
+    for (int j = 0; j < kKeepPools; ++j) a.pools[j] = static_cast<uint8_t *>(pools[i + std::min(j, n - 1)]);
+    CHECK(launched(launch_kv4_keep(a, n, b->head_dim, static_cast<hipStream_t>(stream)), "keeping cache entries"));
+  }
+  return MOE_OK;
+}
+
+int moe_draft_tree(const int32_t *parent, const int32_t *q_start, const int32_t *kv_len, int seqs, int tokens, int words,
+                   int32_t *pos, uint32_t *seen, void *stream) {
+  CHECK(check_tree(q_start, seqs, tokens));
+  if (words < 1 || words > kMaxTree / 32) return fail(MOE_ERR_ARG, "words must be in [1, %d], not %d", kMaxTree / 32, words);
+  CHECK(check_ints("parent", parent, tokens));
+  CHECK(check_ints("kv_len", kv_len, 1));
+  CHECK(check_ints("pos", pos, tokens));
+  CHECK(check_ints("seen", seen, tokens));
+  if (tokens == 0) return MOE_OK;
+  const Span outs[2] = {block_of(pos, (int64_t)tokens * 4), block_of(seen, (int64_t)tokens * words * 4)};
+  CHECK(check_apart("pos", outs[0], "seen", outs[1]));
+  for (int i = 0; i < 2; ++i) {
+    CHECK(check_apart(i ? "seen" : "pos", outs[i], "parent", block_of(parent, (int64_t)tokens * 4)));
+    CHECK(check_apart(i ? "seen" : "pos", outs[i], "q_start", block_of(q_start, (int64_t)(seqs + 1) * 4)));
+    CHECK(check_apart(i ? "seen" : "pos", outs[i], "kv_len", block_of(kv_len, (int64_t)seqs * 4)));
+  }
+  DraftTreeArgs a;
+  a.parent = parent;
+  a.q_start = q_start;
+  a.kv_len = kv_len;
+  a.pos = pos;
+  a.seen = seen;
+  a.seqs = seqs;
+  a.tokens = tokens;
+  a.words = words;
+  return launched(launch_draft_tree(a, static_cast<hipStream_t>(stream)), "plan of a tree");
+}
+
+int moe_verify_drafts(const void *p, int64_t p_stride, const void *q, int64_t q_stride, const int32_t *ids, const int32_t *parent,
+                      const float *u, const int32_t *q_start, int seqs, int tokens, int vocab, int dtype, int32_t *path,
+                      int32_t *count, int32_t *next, void *stream) {
+  CHECK(check_dtype(dtype));
+  CHECK(check_tree(q_start, seqs, tokens));
+  if (vocab < 1 || vocab > 1 << 24) return fail(MOE_ERR_ARG, "vocab must be in [1, 2^24]");
+  const int bytes = element(dtype);
+  CHECK(check_rows("p", p, p_stride, vocab, bytes, bytes, tokens));
+  if (q) CHECK(check_rows("q", q, q_stride, vocab, bytes, bytes, tokens));
+  CHECK(check_ints("ids", ids, tokens));
+  CHECK(check_ints("parent", parent, tokens));
+  CHECK(check_ints("u", u, tokens));
+  CHECK(check_ints("path", path, tokens));
+  CHECK(check_ints("count", count, 1));
+  CHECK(check_ints("next", next, 1));
+  const Span outs[3] = {block_of(path, (int64_t)tokens * 4), block_of(count, (int64_t)seqs * 4), block_of(next, (int64_t)seqs * 4)};
+  const char *const names[3] = {"path", "count", "next"};
+  CHECK(check_apart("path", outs[0], "count", outs[1]));
+  CHECK(check_apart("path", outs[0], "next", outs[2]));
+  CHECK(check_apart("count", outs[1], "next", outs[2]));
+  for (int i = 0; i < 3; ++i) {
+    CHECK(check_apart(names[i], outs[i], "p", rows_of(p, p_stride, vocab, bytes, tokens)));
+    CHECK(check_apart(names[i], outs[i], "q", rows_of(q, q_stride, vocab, bytes, tokens)));
+    CHECK(check_apart(names[i], outs[i], "ids", block_of(ids, (int64_t)tokens * 4)));
+    CHECK(check_apart(names[i], outs[i], "parent", block_of(parent, (int64_t)tokens * 4)));
+    CHECK(check_apart(names[i], outs[i], "u", block_of(u, (int64_t)tokens * 4)));
+    CHECK(check_apart(names[i], outs[i], "q_start", block_of(q_start, (int64_t)(seqs + 1) * 4)));
+  }
+  VerifyArgs a;
+  a.p = p;
+  a.q = q;
+  a.p_stride = p_stride;
+  a.q_stride = q_stride;
+  a.ids = ids;
+  a.parent = parent;
+  a.u = u;
+  a.q_start = q_start;
+  a.path = path;
+  a.count = count;
+  a.next = next;
+  a.seqs = seqs;
+  a.tokens = tokens;
+  a.vocab = vocab;
+  return launched(launch_verify_drafts(a, dtype == MOE_DTYPE_F32, static_cast<hipStream_t>(stream)), "verification");
 }
 
 int moe_norm_residual(const float *h, int64_t h_stride, const void *y, int64_t y_stride, const float *gate,
