@@ -81,3 +81,42 @@ def test_tensors_of_a_step_are_known_to_its_stream(monkeypatch):
         s.step(H, batch)
     used = [s.cos, s.sin, H, snaps, *(batch[k] for k in ("page_table", "q_start", "kv_len")), *(t for l in s.layers for t in l.values())]
     assert len(used) == 7 + 2 * 6 and all((t.data_ptr(), moe.compute) in known for t in used)
+
+
+def test_trees_of_new_tokens(monkeypatch):
+    """Positions go by depth, places by number; what is kept stays, and a
+    sequence that is released has nothing left to keep."""
+    move = torch.Tensor.to
+    monkeypatch.setattr(torch.Tensor, "to", lambda t, where, *a: t if where == "cuda" else move(t, where, *a))
+    s = decoder.Sequences(2, 8, 16, max_pos=20)
+    s.extend([14, 0])
+    batch = s.extend([7, 1], [[-1, 0, 0, 1, 1, 2, 3], [-1]])   # 21 places, but 18 positions
+    assert batch["parent"].tolist() == [-1, 0, 0, 1, 1, 2, 3, -1] and batch["longest"] == 18 and batch["max_len"] == 21
+    assert s.length == [21, 1] and len(s.pages[0]) == 2
+    s.keep([3, 1])
+    assert s.length == [17, 1] and batch["kv_len"].tolist() == [21, 1]
+    with pytest.raises(ValueError, match="positions end at 20"):
+        s.extend([4, 0], [[-1, 0, 1, 2], []])
+    s.extend([2, 3], [[-1, 0], [-1, -1, 1]])
+    s.release(0)
+    s.keep([0, 2])
+    assert s.length == [0, 3]
+
+
+@pytest.mark.parametrize("parents", [[[-1, 0]], [[-1, 0], [-1]], [[-1, 1], []], [[-1, -2], []], [[0, 0], []]])
+def test_trees_that_are_none(parents):
+    s = decoder.Sequences(2, 8, 16, max_pos=40)
+    with pytest.raises(ValueError, match="parents of|cannot follow"):
+        s.extend([2, 0], parents)
+    assert s.length == [0, 0] and len(s.free) == 8
+
+
+@pytest.mark.parametrize("count", [[3, 0], [-1, 0], [1], [1, 1]])
+def test_more_kept_than_there_was(count, monkeypatch):
+    move = torch.Tensor.to
+    monkeypatch.setattr(torch.Tensor, "to", lambda t, where, *a: t if where == "cuda" else move(t, where, *a))
+    s = decoder.Sequences(2, 8, 16)
+    s.extend([2, 0])
+    with pytest.raises(ValueError, match="cannot be kept"):
+        s.keep(count)
+    assert s.length == [2, 0]
