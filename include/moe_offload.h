@@ -562,10 +562,14 @@ int moe_kv4_tree_attention(const moe_kv4_batch *b, const void *q, int64_t q_stri
  * [seqs]: the next token.  A sequence without new tokens has count 0 and next -1;
  * next is also -1 where the weights' sum is 0, infinite or NaN.  An id outside
  * 0 .. vocab - 1 is refused with weight 0.  Of a sequence's tokens the first 1024
- * take part; vocab is in [1, 2^24]. */
+ * take part; vocab is in [1, 2^24].  The workspace (16-byte aligned; NULL if it is 0
+ * bytes) must hold moe_verify_drafts_workspace_bytes (0 for invalid arguments as
+ * well); what it holds before does not matter. */
+size_t moe_verify_drafts_workspace_bytes(int seqs, int vocab);
 int moe_verify_drafts(const void *p, int64_t p_stride, const void *q, int64_t q_stride, const int32_t *ids,
                       const int32_t *parent, const float *u, const int32_t *q_start, int seqs, int tokens, int vocab,
-                      int dtype, int32_t *path, int32_t *count, int32_t *next, void *stream);
+                      int dtype, int32_t *path, int32_t *count, int32_t *next, void *workspace, size_t workspace_bytes,
+                      void *stream);
 
 /* The entry in place base + path[q_start[b] + k] of each sequence goes to place
  * base + k, for k < count[b] (at most the new tokens), base = kv_len[b] - n, in

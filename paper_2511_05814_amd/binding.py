@@ -146,8 +146,9 @@ _SIGNATURES = [
      [ctypes.POINTER(moe_kv4_batch), _P, _I64, _P, _I, _P, _I64, _I, _F, _I, _I, _I, _P, ctypes.c_size_t, _P]),
     ("moe_kv4_keep", _I, [ctypes.POINTER(moe_kv4_batch), ctypes.POINTER(ctypes.c_void_p), _I, _P, _P, _P]),
     ("moe_draft_tree", _I, [_P, _P, _P, _I, _I, _I, _P, _P, _P]),
+    ("moe_verify_drafts_workspace_bytes", ctypes.c_size_t, [_I, _I]),
     ("moe_verify_drafts", _I,
-     [_P, _I64, _P, _I64, _P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P]),
+     [_P, _I64, _P, _I64, _P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     ("moe_norm_residual", _I,
      [_P, _I64, _P, _I64, _P, _I64, _P, _P, _F, _F, _P, _I64, _P, _I64, _I, _I, _I, _P]),
     ("moe_last_error", ctypes.c_char_p, []),
@@ -376,11 +377,15 @@ def moe_draft_tree(parent: int, q_start: int, kv_len: int, seqs: int, tokens: in
     _check(lib().moe_draft_tree(parent, q_start, kv_len, seqs, tokens, words, pos, seen, stream), "moe_draft_tree")
 
 
+def moe_verify_drafts_workspace_bytes(seqs: int, vocab: int) -> int:
+    return lib().moe_verify_drafts_workspace_bytes(seqs, vocab)
+
+
 def moe_verify_drafts(p: int, p_stride: int, q: int, q_stride: int, ids: int, parent: int, u: int, q_start: int,
                       seqs: int, tokens: int, vocab: int, dtype: int, path: int, count: int, next_: int,
-                      stream: int) -> None:
+                      workspace: int, workspace_bytes: int, stream: int) -> None:
     _check(lib().moe_verify_drafts(p, p_stride, q, q_stride, ids, parent, u, q_start, seqs, tokens, vocab, dtype, path,
-                                   count, next_, stream), "moe_verify_drafts")
+                                   count, next_, workspace, workspace_bytes, stream), "moe_verify_drafts")
 
 
 def moe_norm_residual(h: int, h_stride: int, y: int, y_stride: int, gate: int, gate_stride: int, post: int, pre: int,

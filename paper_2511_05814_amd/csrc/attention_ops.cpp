@@ -297,10 +297,14 @@ PyObject *verify_drafts(PyObject *, PyObject *const *a, Py_ssize_t got) {
     const void *i = vector("tokens", ids, at_.device, at::kInt, t), *c = vector("parent", parent, at_.device, at::kInt, t);
     const void *r = vector("u", u, at_.device, at::kFloat, t), *s = vector("q_start", start, at_.device, at::kInt, seqs + 1);
     at::Tensor path = at::empty({t}, ids.options()), count = at::empty({std::max<int64_t>(0, seqs)}, ids.options()), next = at::empty_like(count);
+    const size_t bytes = moe_verify_drafts_workspace_bytes(small(seqs), small(vocab));
+    at::Tensor workspace;
+    if (bytes) workspace = at::empty({(int64_t)bytes}, ids.options().dtype(at::kByte));
     check_rc(moe_verify_drafts(p.data_ptr(), ps, q, qs, static_cast<const int32_t *>(i), static_cast<const int32_t *>(c),
                                static_cast<const float *>(r), static_cast<const int32_t *>(s), small(seqs), small(t), small(vocab), at_.code,
                                static_cast<int32_t *>(path.data_ptr()), static_cast<int32_t *>(count.data_ptr()),
-                               static_cast<int32_t *>(next.data_ptr()), stream_of(a[6])), "moe_verify_drafts");
+                               static_cast<int32_t *>(next.data_ptr()), bytes ? workspace.data_ptr() : nullptr, bytes, stream_of(a[6])),
+             "moe_verify_drafts");
     return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(path)), THPVariable_Wrap(std::move(count)), THPVariable_Wrap(std::move(next)));
   });
 }

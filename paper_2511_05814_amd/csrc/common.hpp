@@ -349,8 +349,12 @@ struct VerifyArgs {
   const int32_t *q_start;
   int32_t *path;               // [tokens]
   int32_t *count, *next;       // [seqs]
-  int seqs, tokens, vocab;
+  uint64_t *slots;             // [seqs][kVerifyPasses][clusters], not for one
+  int seqs, tokens, vocab, clusters;
 };
+constexpr int kMaxClusters = 64;    // workgroups of a sequence
+constexpr int kVerifyPasses = 16;   // over its rows, that they share
+int verify_clusters(int seqs, int vocab);
 hipError_t launch_verify_drafts(const VerifyArgs &a, bool f32, hipStream_t s);
 
 struct Q4Args {

@@ -395,9 +395,15 @@ int moe_draft_tree(const int32_t *parent, const int32_t *q_start, const int32_t 
   return launched(launch_draft_tree(a, static_cast<hipStream_t>(stream)), "plan of a tree");
 }
 
+size_t moe_verify_drafts_workspace_bytes(int seqs, int vocab) {
+  if (seqs < 1 || seqs > 1 << 20 || vocab < 1 || vocab > 1 << 24) return 0;
+  const int clusters = verify_clusters(seqs, vocab);
+  return clusters == 1 ? 0 : (size_t)seqs * kVerifyPasses * clusters * sizeof(uint64_t);
+}
+
 int moe_verify_drafts(const void *p, int64_t p_stride, const void *q, int64_t q_stride, const int32_t *ids, const int32_t *parent,
                       const float *u, const int32_t *q_start, int seqs, int tokens, int vocab, int dtype, int32_t *path,
-                      int32_t *count, int32_t *next, void *stream) {
+                      int32_t *count, int32_t *next, void *workspace, size_t workspace_bytes, void *stream) {
   CHECK(check_dtype(dtype));
   CHECK(check_tree(q_start, seqs, tokens));
   if (vocab < 1 || vocab > 1 << 24) return fail(MOE_ERR_ARG, "vocab must be in [1, 2^24]");
@@ -410,12 +416,14 @@ int moe_verify_drafts(const void *p, int64_t p_stride, const void *q, int64_t q_
   CHECK(check_ints("path", path, tokens));
   CHECK(check_ints("count", count, 1));
   CHECK(check_ints("next", next, 1));
-  const Span outs[3] = {block_of(path, (int64_t)tokens * 4), block_of(count, (int64_t)seqs * 4), block_of(next, (int64_t)seqs * 4)};
-  const char *const names[3] = {"path", "count", "next"};
-  CHECK(check_apart("path", outs[0], "count", outs[1]));
-  CHECK(check_apart("path", outs[0], "next", outs[2]));
-  CHECK(check_apart("count", outs[1], "next", outs[2]));
-  for (int i = 0; i < 3; ++i) {
+  const size_t need = moe_verify_drafts_workspace_bytes(seqs, vocab);
+  if (workspace_bytes < need || (need && (!workspace || misaligned(workspace, 16))))
+    return fail(MOE_ERR_ARG, "workspace must be 16-byte aligned and hold %zu bytes (got %zu)", need, workspace_bytes);
+  const Span outs[4] = {block_of(path, (int64_t)tokens * 4), block_of(count, (int64_t)seqs * 4), block_of(next, (int64_t)seqs * 4),
+                        block_of(workspace, (int64_t)need)};
+  const char *const names[4] = {"path", "count", "next", "the workspace"};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = i + 1; j < 4; ++j) CHECK(check_apart(names[i], outs[i], names[j], outs[j]));
     CHECK(check_apart(names[i], outs[i], "p", rows_of(p, p_stride, vocab, bytes, tokens)));
     CHECK(check_apart(names[i], outs[i], "q", rows_of(q, q_stride, vocab, bytes, tokens)));
     CHECK(check_apart(names[i], outs[i], "ids", block_of(ids, (int64_t)tokens * 4)));
@@ -438,6 +446,8 @@ int moe_verify_drafts(const void *p, int64_t p_stride, const void *q, int64_t q_
   a.seqs = seqs;
   a.tokens = tokens;
   a.vocab = vocab;
+  a.clusters = verify_clusters(seqs, vocab);
+  a.slots = static_cast<uint64_t *>(workspace);
   return launched(launch_verify_drafts(a, dtype == MOE_DTYPE_F32, static_cast<hipStream_t>(stream)), "verification");
 }
 

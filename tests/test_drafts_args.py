@@ -28,7 +28,7 @@ def plan(**kw):
 
 def verify(**kw):
     a = dict(p=A, ps=50, q=B, qs=50, ids=C, parent=C + 64, u=C + 128, q_start=C + 192, seqs=3, tokens=9, vocab=50, dtype=F32, path=D,
-             count=D + 64, next=D + 128, stream=0)
+             count=D + 64, next=D + 128, ws=None, wsb=0, stream=0)
     a.update(kw)
     return tuple(a.values())
 
@@ -81,7 +81,7 @@ def test_draft_tree_overlaps():
 @pytest.mark.parametrize("bad", [
     dict(p=None), dict(p=A + 2), dict(ps=49), dict(q=B + 1), dict(qs=40), dict(ids=None), dict(parent=None), dict(u=None), dict(u=C + 129),
     dict(q_start=None), dict(seqs=0), dict(tokens=-1), dict(vocab=0), dict(vocab=(1 << 24) + 1, ps=1 << 25, qs=1 << 25), dict(dtype=2),
-    dict(path=None), dict(count=None), dict(next=None), dict(next=D + 130)])
+    dict(path=None), dict(count=None), dict(next=None), dict(next=D + 130), dict(vocab=1 << 20, ps=1 << 20, qs=1 << 20)])
 def test_verify_refuses(bad):
     refused(b.moe_verify_drafts, *verify(**bad))
 
@@ -93,6 +93,11 @@ def test_verify_overlaps():
     for bad in (dict(path=A + 400), dict(path=B), dict(count=C), dict(next=C + 64 + 8), dict(count=C + 128), dict(next=C + 192), dict(next=D + 64),
                 dict(count=D + 32), dict(next=D)):
         overlap(b.moe_verify_drafts, *verify(**bad))
+    large = dict(p=A, q=None, ps=1 << 20, vocab=1 << 20, ws=E, wsb=b.moe_verify_drafts_workspace_bytes(3, 1 << 20))
+    assert large["wsb"] > 0
+    apart(b.moe_verify_drafts, *verify(**large))
+    for bad in (dict(ws=E + 8), dict(wsb=large["wsb"] - 1), dict(ws=None), dict(ws=A + 16), dict(ws=C), dict(next=E + 64), dict(path=E)):
+        refused(b.moe_verify_drafts, *verify(**{**large, **bad}))
 
 
 def test_keep_refuses():
