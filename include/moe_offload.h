@@ -533,8 +533,9 @@ int moe_kv4_append_at(const moe_kv4_batch *b, const int32_t *pos, const void *q,
  * of its sequence's new ones, those whose bits are set in its words of seen
  * [tokens][words], 1 <= words <= 32: any pattern, itself only if its own bit is
  * set; bits of tokens that the sequence does not have mean nothing.  The
- * workspace is moe_kv4_attention_workspace_bytes; roundings, NaN and limits are
- * those of moe_kv4_attention. */
+ * workspace must hold moe_kv4_tree_attention_workspace_bytes; all else is as it is
+ * for moe_kv4_attention. */
+size_t moe_kv4_tree_attention_workspace_bytes(const moe_kv4_batch *b, int heads, int dtype, int max_new, int max_len);
 int moe_kv4_tree_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, const uint32_t *seen, int words, void *o,
                            int64_t o_stride, int heads, float scale, int dtype, int max_new, int max_len, void *workspace,
                            size_t workspace_bytes, void *stream);

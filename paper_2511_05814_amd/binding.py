@@ -142,6 +142,7 @@ _SIGNATURES = [
     ("moe_kv4_attention_workspace_bytes", ctypes.c_size_t, [ctypes.POINTER(moe_kv4_batch), _I, _I, _I]),
     ("moe_kv4_attention", _I,
      [ctypes.POINTER(moe_kv4_batch), _P, _I64, _P, _I64, _I, _F, _I, _I, _I, _P, ctypes.c_size_t, _P]),
+    ("moe_kv4_tree_attention_workspace_bytes", ctypes.c_size_t, [ctypes.POINTER(moe_kv4_batch), _I, _I, _I, _I]),
     ("moe_kv4_tree_attention", _I,
      [ctypes.POINTER(moe_kv4_batch), _P, _I64, _P, _I, _P, _I64, _I, _F, _I, _I, _I, _P, ctypes.c_size_t, _P]),
     ("moe_kv4_keep", _I, [ctypes.POINTER(moe_kv4_batch), ctypes.POINTER(ctypes.c_void_p), _I, _P, _P, _P]),
@@ -357,6 +358,10 @@ def moe_kv4_attention(batch: moe_kv4_batch, q: int, q_stride: int, o: int, o_str
                       stream: int) -> None:
     _check(lib().moe_kv4_attention(batch, q, q_stride, o, o_stride, heads, scale, dtype, max_new, max_len, workspace,
                                    workspace_bytes, stream), "moe_kv4_attention")
+
+
+def moe_kv4_tree_attention_workspace_bytes(batch: moe_kv4_batch, heads: int, dtype: int, max_new: int, max_len: int) -> int:
+    return lib().moe_kv4_tree_attention_workspace_bytes(batch, heads, dtype, max_new, max_len)
 
 
 def moe_kv4_tree_attention(batch: moe_kv4_batch, q: int, q_stride: int, seen: int, words: int, o: int, o_stride: int,

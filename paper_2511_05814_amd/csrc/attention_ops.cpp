@@ -240,7 +240,8 @@ PyObject *kv4_attention(PyObject *, PyObject *const *a, Py_ssize_t got) {
       bytes = (size_t)workspace.numel();
       vector("workspace", workspace, at_.device, at::kByte, (int64_t)bytes);
     } else {
-      bytes = moe_kv4_attention_workspace_bytes(&b, small(heads), max_new, max_len);
+      bytes = given(a[10]) ? moe_kv4_tree_attention_workspace_bytes(&b, small(heads), at_.code, max_new, max_len)
+                           : moe_kv4_attention_workspace_bytes(&b, small(heads), max_new, max_len);
       if (bytes) workspace = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
     }
     void *const ws = bytes ? workspace.data_ptr() : nullptr, *const stream = stream_of(a[11]);

@@ -311,6 +311,7 @@ struct KvAttnArgs {
   int heads, splits, row_blocks, prompt;
   const uint32_t *seen;        // [tokens][words], which new tokens a token sees; NULL: those before it
   int words;
+  int32_t *plan;               // [seqs + 1], what the tree kernel's join needs to know
 };
 // Moves entries of new tokens to the places right behind the cached ones.
 constexpr int kKeepPools = 64;   // caches of a launch
@@ -327,9 +328,12 @@ hipError_t launch_kv4_keep(const KvKeepArgs &a, int pools, int head_dim, hipStre
 // rows, and whether rows go in the large blocks of the prompt kernel.
 struct KvAttnShape {
   int splits, row_blocks, prompt;
+  int tiles = 0;   // of 16 rows of a tree kernel, whose workgroups are `splits`; 0: the others
 };
 KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len);
 hipError_t launch_kv4_attention(const KvAttnArgs &a, int head_dim, bool f32, hipStream_t s);
+KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len, int64_t table_tokens, bool f32);
+hipError_t launch_kv4_tree(const KvAttnArgs &a, int tiles, int head_dim, bool f32, hipStream_t s);
 
 // Trees of drafted tokens.
 constexpr int kMaxTree = 1024;   // tokens of a sequence that can be in its tree

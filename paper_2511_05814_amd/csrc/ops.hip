@@ -100,6 +100,20 @@ int check_batch(const moe_kv4_batch *b) {
   return MOE_OK;
 }
 
+KvAttnShape tree_shape(const moe_kv4_batch *b, int heads, int dtype, int max_new, int max_len) {
+  return kv4_tree_shape(b->seqs, b->kv_heads, heads, b->tokens, max_new, max_len, (int64_t)b->table_cols * b->page_size, dtype == MOE_DTYPE_F32);
+}
+
+// Rows that a launch of attention leaves to be joined: of every split, or two
+// places of each of the tree kernel's workgroups.
+size_t parts_rows(const KvAttnShape &s, const moe_kv4_batch *b, int heads) {
+  return s.splits == 1 ? 0 : s.tiles ? (size_t)s.splits * 2 * 16 * s.tiles : (size_t)s.splits * b->tokens * heads;
+}
+size_t parts_bytes(const KvAttnShape &s, const moe_kv4_batch *b, int heads) {
+  const size_t rows = parts_rows(s, b, heads);
+  return rows * (b->head_dim + 2) * sizeof(float) + (s.tiles && rows ? ((size_t)b->seqs + 1) * sizeof(int32_t) : 0);
+}
+
 int check_heads(const moe_kv4_batch *b, int heads) {
   if (heads < 1 || heads > 4096 || heads % b->kv_heads)
     return fail(MOE_ERR_ARG, "heads (%d) must be a multiple of kv_heads (%d), at most 4096", heads, b->kv_heads);
@@ -263,8 +277,13 @@ int moe_kv4_read(const moe_kv4_batch *b, void *k, void *v, int dtype, void *stre
 size_t moe_kv4_attention_workspace_bytes(const moe_kv4_batch *b, int heads, int max_new, int max_len) {
   if (check_batch(b) != MOE_OK || check_heads(b, heads) != MOE_OK || max_new < 1 || max_len < 1) return 0;
   if (product(b->seqs, b->kv_heads) > kMaxGroups || product(b->tokens, heads) > (int64_t)1 << 30) return 0;
-  const int splits = kv4_attention_shape(b->seqs, b->kv_heads, heads, b->tokens, max_new, max_len).splits;
-  return splits == 1 ? 0 : (size_t)splits * b->tokens * heads * (b->head_dim + 2) * sizeof(float);
+  return parts_bytes(kv4_attention_shape(b->seqs, b->kv_heads, heads, b->tokens, max_new, max_len), b, heads);
+}
+
+size_t moe_kv4_tree_attention_workspace_bytes(const moe_kv4_batch *b, int heads, int dtype, int max_new, int max_len) {
+  if (check_dtype(dtype) != MOE_OK || check_batch(b) != MOE_OK || check_heads(b, heads) != MOE_OK || max_new < 1 || max_len < 1) return 0;
+  if (product(b->seqs, b->kv_heads) > kMaxGroups || product(b->tokens, heads) > (int64_t)1 << 30) return 0;
+  return parts_bytes(tree_shape(b, heads, dtype, max_new, max_len), b, heads);
 }
 
 }  // extern "C"
@@ -291,11 +310,12 @@ int attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, const uin
   a.o_stride = o_stride;
   a.scale = scale;
   a.heads = heads;
-  const KvAttnShape shape = kv4_attention_shape(b->seqs, b->kv_heads, heads, b->tokens, max_new, max_len);
+  const KvAttnShape shape = seen ? tree_shape(b, heads, dtype, max_new, max_len)
+                                 : kv4_attention_shape(b->seqs, b->kv_heads, heads, b->tokens, max_new, max_len);
   a.splits = shape.splits;
   a.row_blocks = shape.row_blocks;
   a.prompt = shape.prompt;
-  const size_t rows = (size_t)b->tokens * heads, need = a.splits == 1 ? 0 : (size_t)a.splits * rows * (d + 2) * sizeof(float);
+  const size_t rows = parts_rows(shape, b, heads), need = parts_bytes(shape, b, heads);
   if (workspace_bytes < need || (need && (!workspace || misaligned(workspace, 16))))
     return fail(MOE_ERR_ARG, "workspace must be 16-byte aligned and hold %zu bytes (got %zu)", need, workspace_bytes);
   if (b->tokens == 0) return MOE_OK;
@@ -311,10 +331,13 @@ int attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, const uin
     CHECK(check_apart("the workspace", block_of(workspace, (int64_t)need), "the cache", pool_of(b)));
   }
   a.part = static_cast<float *>(workspace);
-  a.ml = a.part ? a.part + (size_t)a.splits * rows * d : nullptr;
+  a.ml = a.part ? a.part + rows * d : nullptr;
+  a.plan = a.part ? reinterpret_cast<int32_t *>(a.ml + 2 * rows) : nullptr;
   a.seen = seen;
   a.words = words;
-  return launched(launch_kv4_attention(a, d, dtype == MOE_DTYPE_F32, static_cast<hipStream_t>(stream)), "cache attention");
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool f32 = dtype == MOE_DTYPE_F32;
+  return launched(shape.tiles ? launch_kv4_tree(a, shape.tiles, d, f32, s) : launch_kv4_attention(a, d, f32, s), "cache attention");
 }
 
 }  // namespace

@@ -59,7 +59,7 @@ def test_tree_attention_overlaps():
     far = batch(pool=P + (9 << 30), tokens=4)
     apart(b.moe_kv4_tree_attention, *tree_attend(far, seen=C, words=2, q=A, o=B))
     overlap(b.moe_kv4_tree_attention, *tree_attend(far, seen=B + 4 * 256 * 4 - 4, words=2, q=A, o=B))
-    need = b.moe_kv4_attention_workspace_bytes(far, 4, 1, 4096)
+    need = b.moe_kv4_tree_attention_workspace_bytes(far, 4, F32, 1, 4096)
     overlap(b.moe_kv4_tree_attention, *tree_attend(far, seen=D + need - 4, words=1, q=A, o=B, max_len=4096, ws=D, wsb=need))
     b.moe_kv4_tree_attention(*tree_attend(batch(tokens=0)))
 

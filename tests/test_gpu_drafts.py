@@ -144,27 +144,60 @@ SHAPES = [
     (128, 16, 16, 4, [70, 90], [64, 0])]
 
 
+# how long the caller says that sequences are: by it, and the rows, the kernels
+# differ (results are right whatever it is): without splits, or for lengths that
+# differ, of 16, 32 or (bf16, from 65 rows on) 128 rows
+HINTS = [None, 1000, 1 << 20]
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("kind", ["tree", "any", "none", "causal"])
+@pytest.mark.parametrize("hint", HINTS)
 @pytest.mark.parametrize("D,P,heads,kv,new,old", SHAPES)
-def test_tree_attention(D, P, heads, kv, new, old, kind, dtype):
+def test_tree_attention(D, P, heads, kv, new, old, hint, kind, dtype):
     bt = Batch(new, old, heads, kv, D, P, seed=D + P).fill(0.5)
     seen = masks(bt, np.random.default_rng(len(new)), kind)
-    o, _ = check_tree(bt, dtype, seen, bits=words(bt, seen, junk=True))
+    o, _ = check_tree(bt, dtype, seen, bits=words(bt, seen, junk=True), max_new=max(new), max_len=hint)
     for b, (n, m) in enumerate(zip(new, old)):
         if m == 0 and kind == "none":
             assert (o[bt.q_start[b]:bt.q_start[b] + n] == 0).all()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hint", HINTS)
+@pytest.mark.parametrize("D,P,heads,kv,new,old", [
+    (64, 16, 8, 2, [7, 3, 0, 12], [3000, 10, 700, 1900]), (128, 16, 4, 1, [9, 1, 20], [40, 2600, 5000]), (128, 32, 16, 2, [3] * 9, [i * 333 for i in range(9)]),
+    (64, 16, 4, 4, [40, 2], [1500, 3]), (128, 64, 8, 2, [30, 1, 50, 0, 5], [4000, 900, 64, 7, 0])])
+def test_tree_attention_of_unequal_lengths(D, P, heads, kv, new, old, hint, dtype):
+    """Sequences that share workgroups and sequences that lie in many."""
+    bt = Batch(new, old, heads, kv, D, P, seed=D + P).fill(0.4)
+    check_tree(bt, dtype, masks(bt, np.random.default_rng(5), "tree"), max_new=max(new), max_len=hint)
+
+
+@pytest.mark.parametrize("hint", HINTS)
+@pytest.mark.parametrize("new", [2, 13, 40])
+@pytest.mark.parametrize("down", [False, True])
+def test_scores_that_grow_along_the_cache(new, hint, down):
+    """Every reference is passed by far by a later token, or none is."""
+    bt = Batch([new, 1], [700, 90], 4, 2, 64, 16, seed=24).fill(0.3)
+    for i, pos in enumerate(range(3, 700, 37)):
+        change(bt, 0, 699 - pos if down else pos, 0, key_of(2.0 ** (i - 6)))
+    q = np.abs(np.random.default_rng(5).standard_normal((bt.tokens, 4, 64)))
+    for dtype in ("f32", "bf16"):
+        check_tree(bt, dtype, masks(bt, np.random.default_rng(6), "tree"), q=q, max_new=new, max_len=hint)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hint", HINTS)
 @pytest.mark.parametrize("D,P,heads,kv,new,old", SHAPES)
-def test_a_chain_is_attention(D, P, heads, kv, new, old, dtype):
+def test_a_chain_is_attention(D, P, heads, kv, new, old, hint, dtype):
     """With every token seeing those before it, what kv4_attention gives, within
     two roundings of the output and the tolerance between orders of sums."""
     bt = Batch(new, old, heads, kv, D, P, seed=9).fill(0.3)
     q = device(np.random.default_rng(1).standard_normal((bt.tokens, heads, D)), dtype)
     args, bits = bt.args(), words(bt, masks(bt, None, "causal"))
-    a, b = host(at().kv4_tree_attention(q, *args, bits, 0.1)), host(at().kv4_attention(q, *args, 0.1))
+    a = host(at().kv4_tree_attention(q, *args, bits, 0.1, max_new=max(new), max_len=hint))
+    b = host(at().kv4_attention(q, *args, 0.1))
     top = np.nanmax(np.abs(b), initial=1.0)
     tol = (2 * BF * np.abs(b) + top * 2.0 ** -9) if dtype == "bf16" else top * 2.0 ** -17
     assert (np.abs(a - b) <= tol).all()
@@ -189,25 +222,28 @@ def test_tree_attention_is_right_whatever_the_hints(max_new, max_len):
         check_tree(bt, dtype, seen, max_new=max_new, max_len=max_len)
 
 
+@pytest.mark.parametrize("hint", HINTS)
 @pytest.mark.parametrize("new", [[6, 1, 2], [30, 1, 9], [80, 1, 40]])
-def test_tokens_without_places_and_missing_pages(new):
+def test_tokens_without_places_and_missing_pages(new, hint):
     bt = Batch(new, [0, 0, 50], 4, 2, 64, 16, seed=7, short=1).fill(0.3)
     bt.table[2, 0] = -1
     bt.table[2, 2] = 999
     seen = masks(bt, np.random.default_rng(4), "causal")
-    o, _ = check_tree(bt, "f32", seen)
+    hints = dict(max_new=max(new), max_len=hint)
+    o, _ = check_tree(bt, "f32", seen, **hints)
     assert (o[0] == 0).all() and (o[new[0]] == 0).all() and (o[-1] != 0).any()
     bt.table[2, :] = -1
-    o, _ = check_tree(bt, "bf16", seen)
+    o, _ = check_tree(bt, "bf16", seen, **hints)
     assert (o[new[0] + 1:] == 0).all()
     bt.table[:, :] = 1 << 30
-    assert (check_tree(bt, "bf16", seen)[0] == 0).all()
+    assert (check_tree(bt, "bf16", seen, **hints)[0] == 0).all()
 
 
 @pytest.mark.parametrize("new", [3, 9, 25, 150])
 @pytest.mark.parametrize("part", [0, 2])
+@pytest.mark.parametrize("hint", HINTS)
 @pytest.mark.parametrize("D", [64, 128])
-def test_marked_entries_reach_only_rows_that_see_them_in_a_tree(new, part, D):
+def test_marked_entries_reach_only_rows_that_see_them_in_a_tree(new, hint, part, D):
     """A new token and a cached one marked as not stored, and all places behind
     the end."""
     for cached in (False, True):
@@ -224,14 +260,15 @@ def test_marked_entries_reach_only_rows_that_see_them_in_a_tree(new, part, D):
         seen = masks(bt, np.random.default_rng(new), "any")
         seen[0][0, j], seen[0][1, j] = True, False
         for dtype in ("f32", "bf16"):
-            o, _ = check_tree(bt, dtype, seen)
+            o, _ = check_tree(bt, dtype, seen, max_new=new, max_len=hint)
             hit = np.isnan(o[:new, :2]).any((1, 2))
             assert hit.all() if cached else np.array_equal(hit, seen[0][:, j])
             assert not np.isnan(o[:, 2:]).any() and not np.isnan(o[new:]).any()
 
 
+@pytest.mark.parametrize("hint", HINTS)
 @pytest.mark.parametrize("new", [2, 12, 70])
-def test_infinities_and_far_scores(new):
+def test_infinities_and_far_scores(new, hint):
     """A row of q with an infinity is NaN and alone; a key that takes all the
     weight is missed by rows that do not see it."""
     bt = Batch([new, 2], [40, 30], 4, 2, 64, 16, seed=24).fill(0.3)
@@ -240,27 +277,46 @@ def test_infinities_and_far_scores(new):
     seen[0][:, new - 1] = np.arange(new) % 2 == 0
     q = np.abs(np.random.default_rng(5).standard_normal((bt.tokens, 4, 64)))
     for dtype in ("f32", "bf16"):
-        check_tree(bt, dtype, seen, q=q)
-    q[0, 1, 9] = np.inf
-    o = host(at().kv4_tree_attention(device(q, "f32"), *bt.args(), words(bt, seen), 0.125))
-    assert np.isnan(o[0, 1]).all() and np.isnan(o).sum() == 64
+        check_tree(bt, dtype, seen, q=q, max_new=new, max_len=hint)
+    for value in (np.inf, -np.inf, np.nan):
+        q[0, 1, 9] = value
+        for dtype in ("f32", "bf16"):
+            o = host(at().kv4_tree_attention(device(q, dtype), *bt.args(), words(bt, seen), 0.125, max_new=new, max_len=hint))
+            assert np.isnan(o[0, 1]).all() and np.isnan(o).sum() == 64
     for scale in (np.nan, np.inf):
-        o = host(at().kv4_tree_attention(device(np.ones((bt.tokens, 4, 64)), "bf16"), *bt.args(), words(bt, seen), scale))
+        o = host(at().kv4_tree_attention(device(np.ones((bt.tokens, 4, 64)), "bf16"), *bt.args(), words(bt, seen), scale, max_new=new, max_len=hint))
         assert np.isnan(o).all()
+
+
+@pytest.mark.parametrize("hint", HINTS)
+@pytest.mark.parametrize("scale,size", [(1e-20, 1e20), (-1e-30, 1e30), (0.0, 1e25), (1e-36, 1e-10), (1e25, 1e-25)])
+def test_scales_and_queries_of_any_size_in_a_tree(scale, size, hint):
+    bt = Batch([20, 1, 33], [300, 20, 64], 4, 2, 64, 16, seed=23).fill(0.3)
+    q = np.random.default_rng(4).standard_normal((bt.tokens, 4, 64)) * size
+    for dtype in ("f32", "bf16"):
+        check_tree(bt, dtype, masks(bt, np.random.default_rng(6), "tree"), q=q, scale=scale, max_new=33, max_len=hint)
 
 
 def test_strided_queries_given_outputs_and_workspaces():
     bt = Batch([12, 5], [900, 40], 8, 2, 64, 32, seed=3).fill(0.3)
     seen = masks(bt, np.random.default_rng(7), "tree")
     bits, args = words(bt, seen), bt.args()
-    wide = torch.randn((17, 12, 64), device="cuda")
-    want = at().kv4_tree_attention(wide[:, 2:10].contiguous(), *args, bits, 0.125)
-    out = torch.full((17, 12, 64), 7.0, device="cuda")
-    ws = torch.full((1 << 22,), 255, dtype=torch.uint8, device="cuda")
-    got = at().kv4_tree_attention(wide[:, 2:10], *args, bits, 0.125, out=out[:, 1:9], workspace=ws)
-    assert torch.equal(got, want) and (out[:, :1] == 7).all() and (out[:, 9:] == 7).all()
-    at().kv4_tree_attention(wide[:, 2:10], *args, bits, 0.125, out=wide[:, 2:10])
-    assert torch.equal(wide[:, 2:10], want)
+    ws = torch.full((1 << 27,), 255, dtype=torch.uint8, device="cuda")   # NaN, were it read as it is
+    for hint in HINTS:
+        wide = torch.randn((17, 12, 64), device="cuda")
+        want = at().kv4_tree_attention(wide[:, 2:10].contiguous(), *args, bits, 0.125, max_len=hint)
+        out = torch.full((17, 12, 64), 7.0, device="cuda")
+        got = at().kv4_tree_attention(wide[:, 2:10], *args, bits, 0.125, out=out[:, 1:9], workspace=ws, max_len=hint)
+        assert torch.equal(got, want) and (out[:, :1] == 7).all() and (out[:, 9:] == 7).all()
+        at().kv4_tree_attention(wide[:, 2:10], *args, bits, 0.125, out=wide[:, 2:10], max_len=hint)
+        assert torch.equal(wide[:, 2:10], want)
+
+
+def test_more_sequences_than_a_plan_holds():
+    bt = Batch([2, 1] * 150, [5, 17] * 150, 2, 1, 64, 16, seed=3).fill(0.3)
+    check_tree(bt, "bf16", masks(bt, np.random.default_rng(7), "tree"), max_len=1 << 20)
+    bt = Batch([2, 0, 3, 1] * 64, [5, 17, 0, 200] * 64, 2, 1, 64, 16, seed=3).fill(0.3)
+    check_tree(bt, "bf16", masks(bt, np.random.default_rng(7), "tree"), max_len=1 << 20)
 
 
 # -- verification ----------------------------------------------------------------------
@@ -372,6 +428,20 @@ def test_verify_of_rows_that_are_no_distribution(drawn, dtype):
     p, q = (x if x is None or dtype == "f32" else bf16(x) for x in (p, q))
     _, _, after = check_verify(lists, p, q, ids, u, dtype)
     assert after[0] == -1
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("vocab", [66000, 140001])
+def test_verify_of_more_passes_than_are_shared(vocab, drawn):
+    """Workgroups that share a row tell each other the sums of sixteen passes;
+    every one works out the rest by itself."""
+    rng = np.random.default_rng(vocab)
+    lists, p, q, ids, u = case(rng, [25, 2], vocab, "f32", drawn, 1)
+    lists[0] = [-1] + [0] * 24
+    u[1:25] = 1
+    ids[1:25] = rng.choice(200, 24) if drawn else rng.integers(0, vocab, 24)
+    p[0, :200], q_ = p[0, :200] + np.float32(1e-3), q
+    check_verify(lists, p, q_, ids, u, "f32")
 
 
 @pytest.mark.parametrize("drawn", [True, False])
