@@ -21,28 +21,53 @@ __device__ __forceinline__ Tree tree_of(const int32_t *q_start, int seq, int tok
 // pos[t] = place of the sequence's first new token + depth(t); bit j of seen[t]:
 // new token j is t or one of its ancestors.  A parent that is not before its
 // token is none.
-constexpr int kPlanThreads = 256;
-__global__ __launch_bounds__(kPlanThreads) void draft_tree_kernel(DraftTreeArgs a) {
-  __shared__ int16_t s_parent[kMaxTree];
-  const int seq = blockIdx.x;
+//
+// Tokens lie in blocks of 32, a half wave each.  Within a block five rounds, in
+// which every token takes over what the ancestor that it has come to has, give its
+// ancestors there and the first one in front of the block; from there on a token goes
+// up a block at a time.  A walk up the parents one by one takes as long as the tree
+// is deep: 747 tokens, some 500 deep, 60 us so.  What is left is the launch and the
+// few loads that depend on each other; many long rows, their stores.
+__global__ __launch_bounds__(kMaxTree) void draft_tree_kernel(DraftTreeArgs a) {
+  __shared__ uint32_t s_mask[kMaxTree];
+  __shared__ int16_t s_exit[kMaxTree];
+  const int seq = blockIdx.x, lane = threadIdx.x % kWave, half = lane & 32;
   const Tree tree = tree_of(a.q_start, seq, a.tokens);
   const int n = min(tree.n, 32 * a.words), first = a.kv_len[seq] - tree.n;
-  for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-    const int p = a.parent[tree.start + i];
-    s_parent[i] = (int16_t)(p >= 0 && p < i ? p : -1);
+  for (int i0 = 0; i0 < n; i0 += blockDim.x) {
+    const int i = i0 + threadIdx.x, p = i < n ? a.parent[tree.start + i] : -1;
+    uint32_t mask = 1u << (i & 31);
+    int exit = p >= 0 && p < i ? p : -1, up = exit >= 0 && exit >> 5 == i >> 5 ? exit & 31 : -1;
+#pragma unroll
+    for (int round = 0; round < 5; ++round) {
+      const int from = half + max(up, 0);
+      const uint32_t theirs = __shfl(mask, from, kWave);
+      const int their_exit = __shfl(exit, from, kWave), their_up = __shfl(up, from, kWave);
+      if (up >= 0) mask |= theirs, exit = their_exit, up = their_up;
+    }
+    if (i < n) s_mask[i] = mask, s_exit[i] = (int16_t)exit;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < tree.n; i += kPlanThreads) {
+  for (int i = threadIdx.x; i < tree.n; i += blockDim.x) {
     uint32_t *row = a.seen + (int64_t)(tree.start + i) * a.words;
     int depth = -1, x = i < n ? i : -1;
-    for (int w = a.words - 1; w >= 0; --w) {
-      uint32_t bits = 0;
-      while (x >= 32 * w) {
-        bits |= 1u << (x & 31);
-        x = s_parent[x];
-        ++depth;
+    auto word = [&](int w) {
+      if (x < 32 * w) return 0u;
+      const uint32_t bits = s_mask[x];
+      x = s_exit[x];
+      depth += __builtin_popcount(bits);
+      return bits;
+    };
+    // lanes write to rows of their own: four words at a time where rows allow it (15
+    // chains of 1024: 20 us word by word)
+    if (a.words % 4 == 0 && reinterpret_cast<uintptr_t>(a.seen) % 16 == 0) {
+      for (int w = a.words - 4; w >= 0; w -= 4) {
+        uint4 four;
+        four.w = word(w + 3), four.z = word(w + 2), four.y = word(w + 1), four.x = word(w);
+        *reinterpret_cast<uint4 *>(row + w) = four;
       }
-      row[w] = bits;
+    } else {
+      for (int w = a.words - 1; w >= 0; --w) row[w] = word(w);
     }
     a.pos[tree.start + i] = i < n ? first + depth : -1;
   }
@@ -395,7 +420,8 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_drafts_kernel(VerifyArg
 }  // namespace
 
 hipError_t launch_draft_tree(const DraftTreeArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL(draft_tree_kernel, dim3((unsigned)a.seqs), dim3(kPlanThreads), 0, s, a);
+  const int threads = a.words <= 2 ? 64 : 32 * a.words;   // a token each, in whole blocks
+  hipLaunchKernelGGL(draft_tree_kernel, dim3((unsigned)a.seqs), dim3((unsigned)threads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -182,51 +182,59 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(KvReadArgs a) {
 }
 
 // Entry base + path[k] of a sequence to base + k, k below count, base its first
-// new place; one workgroup a cache and sequence, D / 8 lanes an entry.  A path
-// that does not go back (path[k] >= k; others are left alone) lets groups of
-// entries go in order, each read whole before it is written: what a group reads
-// lies at or past its own first place, and earlier groups wrote below that.
+// new place; one workgroup a cache and sequence, D / 8 lanes an entry, and as many
+// heads at once as the kept entries leave lanes.  Every group of entries is read
+// whole before it is written.  Paths that do not go back (path[k] > k; other entries
+// stay) let groups go in order: what a group reads lies past its own first
+// place, and earlier groups wrote in front of that.  The loads bound it, three that each need the
+// one before: path, page, entry.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv4_keep_kernel(KvKeepArgs a) {
-  constexpr int kLanes = D / 8, kItems = kThreads / kLanes;
+  constexpr int kLanes = D / 8, kItems = kThreads / kLanes, kAhead = 4;
   const int seq = blockIdx.x, o = threadIdx.x % kLanes, item = threadIdx.x / kLanes;
   Kv4 kv = a.kv;
   kv.pool = a.pools[blockIdx.y];
   const int start = min(max(kv.q_start[seq], 0), kv.tokens), end = min(max(kv.q_start[seq + 1], start), kv.tokens);
-  const int n = end - start, kept = min(a.count[seq], n), base = kv.kv_len[seq] - n;
-  for (int head = 0; head < kv.kv_heads; ++head) {
-    for (int k0 = 0; k0 < kept; k0 += kItems) {
-      const int k = k0 + item;
-      uint8_t *from = nullptr, *to = nullptr;
-      uint32_t codes[2];
-      uint16_t metas[2];
-      int in_to = 0;
-      if (k < kept) {
-        const int source = a.path[start + k];
-        if (source > k && source < n) {
-          from = record_of<D>(kv, seq, base + source, head);
-          to = record_of<D>(kv, seq, base + k, head);
-          const int mask = (1 << kv.page_log2) - 1, in = (base + source) & mask;
-          in_to = (base + k) & mask;
-          if (from && to) {
+  const int n = end - start, kept = min(a.count[seq], n), base = kv.kv_len[seq] - n, mask = (1 << kv.page_log2) - 1;
+  if (kept <= 1) return;   // the first stays in any case
+  // entries of a group, a power of two; heads of a step, kAhead steps at a time
+  const int group = kept >= kItems ? kItems : 1 << (32 - __builtin_clz(kept - 1)), heads = kItems / group;
+  for (int k0 = 0; k0 < kept; k0 += group) {
+    const int k = k0 + item % group, source = k < kept ? a.path[start + k] : 0;
+    const bool moves = k < kept && source > k && source < n;
+    const int in = (base + source) & mask, in_to = (base + k) & mask;
+    for (int h0 = item / group; h0 - item / group < kv.kv_heads; h0 += heads * kAhead) {
+      uint8_t *to[kAhead];
+      uint32_t codes[kAhead][2];
+      uint16_t metas[kAhead][2];
 #pragma unroll
-            for (int v = 0; v < 2; ++v) {
-              codes[v] = *reinterpret_cast<const uint32_t *>(from + code_at<D>(kv, v, in, o));
-              metas[v] = *reinterpret_cast<const uint16_t *>(from + meta_at<D>(kv, v, in, o / 4));
-            }
-          }
+      for (int x = 0; x < kAhead; ++x) {
+        const int head = h0 + x * heads;
+        uint8_t *from = nullptr;
+        to[x] = nullptr;
+        if (moves && head < kv.kv_heads) {
+          from = record_of<D>(kv, seq, base + source, head);
+          to[x] = from ? record_of<D>(kv, seq, base + k, head) : nullptr;
         }
-      }
-      __syncthreads();
-      if (from && to) {
+        if (!to[x]) continue;
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
-          *reinterpret_cast<uint32_t *>(to + code_at<D>(kv, v, in_to, o)) = codes[v];
-          if (o % 4 == 0) *reinterpret_cast<uint16_t *>(to + meta_at<D>(kv, v, in_to, o / 4)) = metas[v];
+          codes[x][v] = *reinterpret_cast<const uint32_t *>(from + code_at<D>(kv, v, in, o));
+          metas[x][v] = *reinterpret_cast<const uint16_t *>(from + meta_at<D>(kv, v, in, o / 4));
         }
       }
       __syncthreads();
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x) {
+        if (!to[x]) continue;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          *reinterpret_cast<uint32_t *>(to[x] + code_at<D>(kv, v, in_to, o)) = codes[x][v];
+          if (o % 4 == 0) *reinterpret_cast<uint16_t *>(to[x] + meta_at<D>(kv, v, in_to, o / 4)) = metas[x][v];
+        }
+      }
     }
+    __syncthreads();   // written before the next group reads
   }
 }
 

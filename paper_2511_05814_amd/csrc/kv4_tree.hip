@@ -853,8 +853,9 @@ void launch(const KvAttnArgs &a, int tiles, hipStream_t s) {
 //   64 of 8 over 700 / over 4095              25 / 105  31 / 85   30 / 66    44 / 106
 //   fp32: 16 of 12 over 8191 / 4 of 48 over 16000  69 / 179  63 / 135  72 / 123  116 / 138
 //   fp32, 16 heads: 32 of 32 over 2047 / 6000  56 / 132  62 / 121  68 / 126  142 / 306
+//   1 of 1 over 600                                8       11        12         12
 // The plan and the join cost more than they save where a unit has few steps and there
-// are enough units without it, and where 512 tokens at most need no split at all.
+// are enough units without it, and where there is little to share out.
 KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len, int64_t table_tokens, bool f32) {
   KvAttnShape s = kv4_attention_shape(seqs, kv_heads, heads, tokens, max_new, max_len);
   const int64_t full = (int64_t)tokens * (heads / kv_heads);   // rows, were they all of one sequence
@@ -862,6 +863,7 @@ KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int ma
   const int64_t pairs = (int64_t)seqs * kv_heads, units = pairs * ((rows + 15) / 16), steps = ((int64_t)max_len + kStepTokens - 1) / kStepTokens;
   if (seqs > kMaxSeqs || max_len <= 512 || (units >= 512 && steps <= 20)) return s;
   const int64_t work = units * steps;
+  if (work < 512) return s;
   int tiles = rows > 16 && work >= 12288 ? 2 : 1;
   if (f32 && rows < 64) tiles = 1;
   if (!f32 && rows > 64 && work >= 24576) tiles = 8;
