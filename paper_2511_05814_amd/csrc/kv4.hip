@@ -78,7 +78,8 @@ __device__ __forceinline__ size_t meta_at(const Kv4 &kv, bool value, int t, int 
 // that codes do not depend on how an expression was compiled.  A token's bytes
 // pass once, so HBM bounds it: 4098 tokens of 16 heads of 128 in fp32 take 31
 // us, and reading them back in fp32 18.  A few tokens take the launch.
-template <int D, typename T>
+// AT: rotated for positions of the caller's.
+template <int D, typename T, bool AT>
 __global__ __launch_bounds__(kThreads) void kv4_append_kernel(KvAppendArgs a) {
 #pragma clang fp contract(off)
   constexpr int kLanes = D / 8;
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(KvAppendArgs a) {
   src += head * D;
   float x[8];
   load8(src + 8 * o, x);
-  const int turn = a.pos ? a.pos[t] : pos;   // the position that it is rotated for
+  const int turn = AT ? a.pos[t] : pos;   // the position that it is rotated for
   const bool placed = pos >= 0 && turn >= 0 && turn < a.max_pos;
   if (!value && 8 * o < a.rot && placed) {
     const int half = a.rot / 2, i = 8 * o < half ? 8 * o : 8 * o - half;
@@ -243,16 +244,22 @@ unsigned blocks(int64_t items) {
   return (unsigned)((items * (D / 8) + kThreads - 1) / kThreads);
 }
 
+template <int D, typename T>
+void append(const KvAppendArgs &a, hipStream_t s) {
+  const dim3 grid(blocks<D>((int64_t)a.kv.tokens * (a.heads + 2 * a.kv.kv_heads)));
+  if (a.pos) hipLaunchKernelGGL((kv4_append_kernel<D, T, true>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((kv4_append_kernel<D, T, false>), grid, dim3(kThreads), 0, s, a);
+}
+
 }  // namespace
 
 hipError_t launch_kv4_append(const KvAppendArgs &a, int head_dim, bool f32, hipStream_t s) {
-  const int64_t items = (int64_t)a.kv.tokens * (a.heads + 2 * a.kv.kv_heads);
   if (head_dim == 64) {
-    if (f32) hipLaunchKernelGGL((kv4_append_kernel<64, float>), dim3(blocks<64>(items)), dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((kv4_append_kernel<64, uint16_t>), dim3(blocks<64>(items)), dim3(kThreads), 0, s, a);
+    if (f32) append<64, float>(a, s);
+    else append<64, uint16_t>(a, s);
   } else {
-    if (f32) hipLaunchKernelGGL((kv4_append_kernel<128, float>), dim3(blocks<128>(items)), dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((kv4_append_kernel<128, uint16_t>), dim3(blocks<128>(items)), dim3(kThreads), 0, s, a);
+    if (f32) append<128, float>(a, s);
+    else append<128, uint16_t>(a, s);
   }
   return hipGetLastError();
 }

@@ -499,8 +499,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
           page_of(t0 + 16 * x, held);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int in = 8 * (i / 4) + i % 4, at = t0 + 16 * x + 4 * hi + in;
-            if ((TREE ? at >= end || !(bits[x / 2] >> (16 * (x % 2) + in) & 1) : at > last) || !held) s[x / 2][8 * (x % 2) + i] = -__builtin_inff();
+            const int at = t0 + 16 * x + 8 * (i / 4) + 4 * hi + i % 4;
+            if ((TREE ? at >= end || !(bits[x / 2] >> (16 * (x % 2) + 8 * (i / 4) + i % 4) & 1) : at > last) || !held)
+              s[x / 2][8 * (x % 2) + i] = -__builtin_inff();
           }
         }
       }
@@ -549,9 +550,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 1 : 2) void kv4_prompt_k
           half8 mark, seen;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const int in = 8 * (e / 4) + e % 4, at = 16 * x + 4 * hi + in;
+            const int at = 16 * x + 8 * (e / 4) + 4 * hi + e % 4;
             mark[e] = (_Float16)(any4[x / 2 + 2 * (x % 2)] & 1 ? (float)marks[at] : 0.0f);
-            seen[e] = (_Float16)((TREE ? bits[x / 2] >> (16 * (x % 2) + in) & 1 : t0 + at <= last) ? 1.0f : 0.0f);
+            seen[e] = (_Float16)((TREE ? bits[x / 2] >> (16 * (x % 2) + 8 * (e / 4) + e % 4) & 1 : t0 + at <= last) ? 1.0f : 0.0f);
           }
           count = __builtin_amdgcn_mfma_f32_32x32x16_f16(mark, seen, count, 0, 0, 0);
         }
