@@ -332,7 +332,8 @@ struct KvAttnShape {
 };
 KvAttnShape kv4_attention_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len);
 hipError_t launch_kv4_attention(const KvAttnArgs &a, int head_dim, bool f32, hipStream_t s);
-KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len, int64_t table_tokens, bool f32);
+KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len, int64_t table_tokens, int head_dim,
+                           bool f32);
 hipError_t launch_kv4_tree(const KvAttnArgs &a, int tiles, int head_dim, bool f32, hipStream_t s);
 
 // Trees of drafted tokens.

@@ -24,18 +24,31 @@ __device__ __forceinline__ float weight(float above, float down) {
 }
 constexpr float kRange = 32768.0f;   // 2^(shift + slack): weights below it fit fp16
 
+// Sums over a wave's lanes up to each.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_plus(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int wave_scan(int v) {
+  v = dpp_plus<0x111, 0xF>(v);  // row_shr:1
+  v = dpp_plus<0x112, 0xF>(v);  // row_shr:2
+  v = dpp_plus<0x114, 0xF>(v);  // row_shr:4
+  v = dpp_plus<0x118, 0xF>(v);  // row_shr:8
+  v = dpp_plus<0x142, 0xA>(v);  // row_bcast:15
+  v = dpp_plus<0x143, 0xC>(v);  // row_bcast:31
+  return v;
+}
+
 // A launch's work: units, each ROWS rows of a sequence and kv head, of as many
 // steps as the sequence has STEP tokens, and AHEAD more for what it takes to begin
 // and end one, all one behind the other.  Each of W workgroups takes as much of all
 // T as the others (W is at most T), whatever the lengths are.  A unit that lies in several workgroups is joined afterwards: a workgroup
 // has at most one whose first steps others have and one whose last ones others
 // have, and a place for the rows of each.
-constexpr int kMaxSeqs = kThreads;   // of a call
+constexpr int kMaxSeqs = 256;   // of a call; workgroups have no fewer threads
 template <int ROWS, int STEP, int AHEAD>
 struct Plan {
   int before[kMaxSeqs + 1];   // T of the sequences before each
   int start[kMaxSeqs], rows[kMaxSeqs], first[kMaxSeqs], held[kMaxSeqs];
-  int sums[kWaves];
+  int sums[kMaxSeqs / kWave];
 
   static __device__ __forceinline__ int blocks_of(int rows) { return (rows + ROWS - 1) / ROWS; }
   // rows that see nothing have a step as well: it writes their zeros
@@ -51,17 +64,15 @@ struct Plan {
       start[b] = s.start, rows[b] = s.rows, first[b] = s.first, held[b] = s.held;
       mine = blocks_of(s.rows) * a.kv.kv_heads * (steps_of(s.rows, s.first, s.held, group) + AHEAD);
     }
-    int upto = mine;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const int other = __shfl_up(upto, d, kWave);
-      if (lane >= d) upto += other;
-    }
-    if (lane == kWave - 1) sums[wave] = upto;
+    int upto = wave_scan(mine);
+    constexpr int kScan = kMaxSeqs / kWave;   // waves that have sequences
+    if (lane == kWave - 1 && wave < kScan) sums[wave] = upto;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) upto += sums[w];
-    before[b + 1] = upto;
-    if (b == 0) before[0] = 0;
+    if (wave < kScan) {
+      for (int w = 0; w < wave; ++w) upto += sums[w];
+      before[b + 1] = upto;
+      if (b == 0) before[0] = 0;
+    }
     __syncthreads();
   }
 };
@@ -124,7 +135,7 @@ __device__ __forceinline__ Range range_of(const KvAttnArgs &a, const Plan<ROWS, 
   Range r;
   r.me = blockIdx.x;
   if (r.me == 0)
-    for (int b = threadIdx.x; b <= a.kv.seqs; b += kThreads) a.plan[b] = p.before[b];
+    for (int b = threadIdx.x; b <= a.kv.seqs; b += blockDim.x) a.plan[b] = p.before[b];
   r.at = r.stop = 0;
   if (r.me < groups) {
     const Shares s = shares(all, groups);
@@ -146,13 +157,13 @@ __global__ __launch_bounds__(kThreads, R == 1 && sizeof(T) == 2 ? 3 : 2) void kv
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
   constexpr int KW = D / 32;   // words of codes of a lane's part of a key, steps of the dot product
   constexpr int NU = D / 16;   // output blocks of 16 dimensions
-  constexpr int kQueries = R * PARTS * KW * kWave * 16, kJoin = kWaves * 16 * (D + 4) * 4;
+  constexpr int kQueries = R * PARTS * KW * kWave * 16, kJoin = R * kWaves * 16 * (D + 4) * 4;
   __shared__ __align__(16) uint8_t s_mem[kQueries > kJoin ? kQueries : kJoin];
   __shared__ float s_down[R * 16];
-  __shared__ float s_ml[kWaves][16][2];
+  __shared__ float s_ml[R][kWaves][16][2];
   __shared__ TilePlan<R> s_plan;
   half8 *const s_q = reinterpret_cast<half8 *>(s_mem);                               // [tile][part][step][lane]
-  float (*const s_o)[16][D + 4] = reinterpret_cast<float (*)[16][D + 4]>(s_mem);   // [wave], after the loop
+  float (*const s_o)[kWaves][16][D + 4] = reinterpret_cast<float (*)[kWaves][16][D + 4]>(s_mem);   // [tile][wave], after the loop
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane & 15, j = lane >> 4;
@@ -393,36 +404,39 @@ __global__ __launch_bounds__(kThreads, R == 1 && sizeof(T) == 2 ? 3 : 2) void kv
       }
     }
 
-    // join the four waves, tile by tile: lane (r, j) has dimensions dim(i, u) of row r
+    // join the four waves: lane (r, j) has dimensions dim(i, u) of row r of each tile
     constexpr int kPer = 16 * D / kThreads;   // 8 or 4 dimensions a thread
     const int orow = threadIdx.x / (D / kPer), dim = threadIdx.x % (D / kPer) * kPer;
+    __syncthreads();   // the queries are done with
 #pragma unroll
     for (int x = 0; x < R; ++x) {
-      if (x >= tiles) break;
-      __syncthreads();   // the queries, or the tile before, are done with
       float sum = sum_over_j(l[x]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int cc = 4 * j + i, at = D == 128 ? 8 * cc : 8 * (cc & 7) + 4 * (cc >> 3);
 #pragma unroll
         for (int u = 0; u < NU; u += 4)
-          *reinterpret_cast<float4 *>(&s_o[wave][r][at + u]) = make_float4(o[x][u][i], o[x][u + 1][i], o[x][u + 2][i], o[x][u + 3][i]);
+          *reinterpret_cast<float4 *>(&s_o[x][wave][r][at + u]) = make_float4(o[x][u][i], o[x][u + 1][i], o[x][u + 2][i], o[x][u + 3][i]);
       }
       if (j == 0) {
-        s_ml[wave][r][0] = joined_max(-under[x][0], unit(down[x], factor), sum);
-        s_ml[wave][r][1] = sum;
+        s_ml[x][wave][r][0] = joined_max(-under[x][0], unit(down[x], factor), sum);
+        s_ml[x][wave][r][1] = sum;
       }
-      __syncthreads();
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < R; ++x) {
+      if (x >= tiles) break;
       float top = -__builtin_inff(), total = 0.0f, acc[kPer] = {};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_ml[w][orow][0]);
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_ml[x][w][orow][0]);
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        if (s_ml[w][orow][1] == 0.0f) continue;
-        const float f = s_ml[w][orow][0] == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((s_ml[w][orow][0] - top) * factor);
-        total += s_ml[w][orow][1] * f;
+        if (s_ml[x][w][orow][1] == 0.0f) continue;
+        const float f = s_ml[x][w][orow][0] == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((s_ml[x][w][orow][0] - top) * factor);
+        total += s_ml[x][w][orow][1] * f;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] += s_o[w][orow][dim + e] * f;
+        for (int e = 0; e < kPer; ++e) acc[e] += s_o[x][w][orow][dim + e] * f;
       }
       const int row = row0 + 16 * x + orow;
       if (row < seq.rows) {
@@ -450,10 +464,9 @@ __global__ __launch_bounds__(kThreads, R == 1 && sizeof(T) == 2 ? 3 : 2) void kv
 }
 
 // Rows in blocks of 128, 32 a wave: the layout of kv4_prompt_kernel.
-constexpr int kWideTile = 64, kWideRows = 128;
-typedef Plan<kWideRows, kWideTile, kAhead> WidePlan;
-template <int D>
-__global__ __launch_bounds__(kThreads, 2) void kv4_tree_wide_kernel(KvAttnArgs a) {
+constexpr int kWideTile = 64;
+template <int D, int WAVES>
+__global__ __launch_bounds__(kWave * WAVES, 2) void kv4_tree_wide_kernel(KvAttnArgs a) {
   typedef uint16_t T;
   constexpr int KS = D / 16;           // steps of a score's dot product
   constexpr int NB = D / 32;           // output blocks of 32 dimensions
@@ -461,12 +474,12 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_tree_wide_kernel(KvAttnArgs a
   constexpr int KB = 32 * D * 2;       // LDS bytes of 32 keys, or of 32 values
   __shared__ __align__(16) uint8_t s_kv[2][4 * KB];          // keys of both blocks, values of both
   __shared__ __align__(16) uint8_t s_mark[2][D / 32][kWideTile];  // marks of value groups, where s_any says there are
-  __shared__ __align__(16) uint32_t s_any[2][kWaves];        // bit 0: marks in the wave's share, bit 1: a page is missing
+  __shared__ __align__(16) uint32_t s_any[2][4];        // bit 0: marks in the wave's share, bit 1: a page is missing
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane & 31, hi = lane >> 5;
   const Masks masks_ = masks();
-  __shared__ WidePlan s_plan;
+  __shared__ Plan<32 * WAVES, kWideTile, kAhead> s_plan;
   const int group = a.heads / a.kv.kv_heads;
   s_plan.make(a, group);
   const Range range = range_of(a, s_plan);
@@ -526,46 +539,45 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_tree_wide_kernel(KvAttnArgs a
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[u][i] = 0.0f;
 
-    // A thread's share of a tile: words KW * (2 (wave / 2) + hi) .. of key
-    // 32 (wave % 2) + r, and, of the 8 dimensions of octet r / (8 / NB), NB of
-    // values 32 (wave % 2) + 16 (wave / 2) + 4 hi + 0 .. 3 and + 8.
-    uint32_t kw[KW], km;
+    // A wave's share of a tile are 16 tokens, `mine16` of them first, with eight
+    // waves half of their dimensions; a thread's: KL words of key lane % 16 from
+    // word w0 on, and, of the 8 dimensions of octet r / (8 / NB), NB (half of them) of values 4
+    // hi + 0 .. 3 and + 8.
+    constexpr int SHARE = WAVES / 4, KL = KW / SHARE;
+    const int block = wave & 1, half16 = wave >> 1 & 1, other = wave >> 2;
+    const int w0 = KW * (lane >> 4) + KL * other;
+    const uint32_t k_lane = (lane & 15) * (D / 2) + w0 * 4, km_lane = kmetas + (lane & 15) * (D / 16) + w0 / 4 * 2;
+    const uint32_t oct = (uint32_t)r / (8 / NB), v_lane = values + hi * (2 * D) + oct * 16, vm_lane = vmetas + hi * (D / 4) + oct / 4 * 8;
+    uint32_t kw[KL], km;
     u32x4 vw[2];
     u32x2 vm[2];
-    bool v_held, both_held;
+    bool v_held;
     auto fetch = [&](int t0) {
-      const int sub = t0 + 32 * (wave & 1);
-      bool h0, h1;
-      const uint8_t *p0 = page_of(sub, h0), *p1 = page_of(sub + 16, h1);
-      const uint8_t *rec = r < 16 ? p0 : p1;
-      const uint32_t in = (sub + r) & page_mask, part = 2 * (wave >> 1) + hi;
-      const uint8_t *kp = rec + in * (D / 2) + KW * 4 * part;
-      if constexpr (KW == 4) *reinterpret_cast<u32x4 *>(kw) = *reinterpret_cast<const u32x4 *>(kp);
+      const int mine16 = t0 + 32 * block + 16 * half16;
+      const uint8_t *rec = page_of(mine16, v_held);
+      const uint32_t in = mine16 & page_mask;
+      const uint8_t *kp = rec + in * (D / 2) + k_lane;
+      if constexpr (KL == 4) *reinterpret_cast<u32x4 *>(kw) = *reinterpret_cast<const u32x4 *>(kp);
       else *reinterpret_cast<u32x2 *>(kw) = *reinterpret_cast<const u32x2 *>(kp);
-      km = *reinterpret_cast<const uint16_t *>(rec + kmetas + in * (D / 16) + (D == 128 ? part : part / 2) * 2);
-      const uint8_t *vrec = wave >> 1 ? p1 : p0;
-      v_held = wave >> 1 ? h1 : h0;
-      both_held = h0 && h1;
-      const uint32_t quad = (((sub + 16 * (wave >> 1)) & page_mask) >> 2) + hi, oct = (uint32_t)r / (8 / NB);
+      km = *reinterpret_cast<const uint16_t *>(rec + in * (D / 16) + km_lane);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        vw[x] = *reinterpret_cast<const u32x4 *>(vrec + values + (quad + 2 * x) * (2 * D) + oct * 16);
-        vm[x] = *reinterpret_cast<const u32x2 *>(vrec + vmetas + (quad + 2 * x) * (D / 4) + oct / 4 * 8);
+        vw[x] = *reinterpret_cast<const u32x4 *>(rec + in * (D / 2) + 2 * x * (2 * D) + v_lane);
+        vm[x] = *reinterpret_cast<const u32x2 *>(rec + in * (D / 16) + 2 * x * (D / 4) + vm_lane);
       }
     };
     auto stage = [&](int t0, int buf) {
       uint8_t *to = s_kv[buf];
       {
         const Pair pair = key_pair(km);
-        const int w0 = KW * (2 * (wave >> 1) + hi);
 #pragma unroll
-        for (int x = 0; x < KW; ++x)
-          *reinterpret_cast<half8 *>(to + (wave & 1) * KB + (w0 + x) * 512 + r * 16) = key_values(kw[x], pair, masks_);
+        for (int x = 0; x < KL; ++x)
+          *reinterpret_cast<half8 *>(to + block * KB + (w0 + x) * 512 + (16 * half16 + (lane & 15)) * 16) = key_values(kw[x], pair, masks_);
       }
       // tokens that no row sees must not reach the products, whatever their bytes are
       uint32_t metas[4] = {vm[0][0], vm[0][1], vm[1][0], vm[1][1]};
       if (!v_held || t0 + kWideTile > end) {
-        const int tok = t0 + 32 * (wave & 1) + 16 * (wave >> 1) + 4 * hi;
+        const int tok = t0 + 32 * block + 16 * half16 + 4 * hi;
 #pragma unroll
         for (int e = 0; e < 4; ++e) metas[e] = inside(metas[e], tok + 8 * (e / 2) + 2 * (e % 2), v_held ? end : 0);
       }
@@ -573,17 +585,18 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_tree_wide_kernel(KvAttnArgs a
       const bool marked = value_pairs(metas, pairs);
       const uint32_t first_byte = pick_byte(r % (8 / NB) * (NB / 2));
 #pragma unroll
-      for (int bt = 0; bt < NB / 2; ++bt) {
+      for (int i = 0; i < NB / 2 / SHARE; ++i) {
+        const int bt = SHARE == 1 ? i : other;
         half8 v0, v1;
         value_byte(vw, first_byte + bt * 0x00010001u, pairs, masks_, v0, v1);
-        uint8_t *at = to + 2 * KB + (wave & 1) * KB + (wave >> 1) * 1024 + lane * 16;
+        uint8_t *at = to + 2 * KB + block * KB + half16 * 1024 + lane * 16;
         *reinterpret_cast<half8 *>(at + (2 * bt) * 2048) = v0;
         *reinterpret_cast<half8 *>(at + (2 * bt + 1) * 2048) = v1;
       }
       const bool any = __builtin_amdgcn_ballot_w64(marked) != 0;
-      if (lane == 0) s_any[buf][wave] = (any ? 1u : 0u) | (both_held ? 0u : 2u);
-      if (any && r % 8 == 0) {   // a lane of each group of 32 dimensions (D 64: of each half)
-        uint8_t *mp = &s_mark[buf][r / (8 / NB) / 4][32 * (wave & 1) + 16 * (wave >> 1) + 4 * hi];
+      if (lane == 0 && other == 0) s_any[buf][wave] = (any ? 1u : 0u) | (v_held ? 0u : 2u);
+      if (any && r % 8 == 0 && other == 0) {   // a lane of each group of 32 dimensions (D 64: of each half)
+        uint8_t *mp = &s_mark[buf][r / (8 / NB) / 4][32 * block + 16 * half16 + 4 * hi];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t two = metas[e];
@@ -699,7 +712,7 @@ __global__ __launch_bounds__(kThreads, 2) void kv4_tree_wide_kernel(KvAttnArgs a
     }
     l = sum_of_halves(l);
     if (wrow + r >= seq.rows) continue;
-    const int64_t to = ((int64_t)range.me * 2 + (work.first ? 0 : 1)) * kWideRows + wave * 32 + r;
+    const int64_t to = ((int64_t)range.me * 2 + (work.first ? 0 : 1)) * (32 * WAVES) + wave * 32 + r;
     const float inv = divided ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -822,18 +835,20 @@ void launch_tiles(const KvAttnArgs &a, hipStream_t s) {
   launch_join<D, T, 16 * R, kStepTokens, kAhead>(a, units, s);
 }
 
-template <int D>
+template <int D, int WAVES>
 void launch_wide(const KvAttnArgs &a, hipStream_t s) {
   const unsigned units = (unsigned)a.kv.seqs * a.kv.kv_heads * a.row_blocks;
-  hipLaunchKernelGGL((kv4_tree_wide_kernel<D>), dim3((unsigned)a.splits), dim3(kThreads), 0, s, a);
-  launch_join<D, uint16_t, kWideRows, kWideTile, kAhead>(a, units, s);
+  hipLaunchKernelGGL((kv4_tree_wide_kernel<D, WAVES>), dim3((unsigned)a.splits), dim3(kWave * WAVES), 0, s, a);
+  launch_join<D, uint16_t, 32 * WAVES, kWideTile, kAhead>(a, units, s);
 }
 
 template <int D, typename T>
 void launch(const KvAttnArgs &a, int tiles, hipStream_t s) {
   if (tiles == 1) return launch_tiles<D, T, 1>(a, s);
   if constexpr (sizeof(T) == 2)
-    if (tiles == 8) return launch_wide<D>(a, s);
+    if (tiles == 8) return launch_wide<D, 4>(a, s);
+  if constexpr (sizeof(T) == 2 && D == 128)
+    if (tiles == 16) return launch_wide<D, 8>(a, s);
   launch_tiles<D, T, 2>(a, s);
 }
 
@@ -856,7 +871,7 @@ void launch(const KvAttnArgs &a, int tiles, hipStream_t s) {
 //   1 of 1 over 600                                8       11        12         12
 // The plan and the join cost more than they save where a unit has few steps and there
 // are enough units without it, and where there is little to share out.
-KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len, int64_t table_tokens, bool f32) {
+KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len, int64_t table_tokens, int head_dim, bool f32) {
   KvAttnShape s = kv4_attention_shape(seqs, kv_heads, heads, tokens, max_new, max_len);
   const int64_t full = (int64_t)tokens * (heads / kv_heads);   // rows, were they all of one sequence
   const int64_t hinted = (int64_t)max_new * (heads / kv_heads), rows = hinted < full ? hinted : full;
@@ -866,14 +881,14 @@ KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int ma
   if (work < 512) return s;
   int tiles = rows > 16 && work >= 12288 ? 2 : 1;
   if (f32 && rows < 64) tiles = 1;
-  if (!f32 && rows > 64 && work >= 24576) tiles = 8;
+  if (!f32 && rows > 64 && work >= 24576) tiles = head_dim == 128 && rows > 192 ? 16 : 8;
   const int per = 16 * tiles;
   // T has to fit an int, for the longest sequences that the table has room for
   if ((full / per + seqs) * kv_heads >= ((int64_t)1 << 31) / (table_tokens / kWideTile + kAhead + 2)) return s;
   s.tiles = tiles;
   const int64_t blocks = (rows + per - 1) / per, room = kMaxGroups / (pairs * per);
   s.row_blocks = (int)(blocks < 1 || room < 1 ? 1 : blocks > room ? room : blocks);
-  s.splits = 512;   // workgroups, two a compute unit
+  s.splits = tiles == 16 ? 256 : 512;   // workgroups, of 512 threads one a compute unit, others two
   return s;
 }
 

@@ -101,7 +101,8 @@ int check_batch(const moe_kv4_batch *b) {
 }
 
 KvAttnShape tree_shape(const moe_kv4_batch *b, int heads, int dtype, int max_new, int max_len) {
-  return kv4_tree_shape(b->seqs, b->kv_heads, heads, b->tokens, max_new, max_len, (int64_t)b->table_cols * b->page_size, dtype == MOE_DTYPE_F32);
+  return kv4_tree_shape(b->seqs, b->kv_heads, heads, b->tokens, max_new, max_len, (int64_t)b->table_cols * b->page_size, b->head_dim,
+                        dtype == MOE_DTYPE_F32);
 }
 
 // Rows that a launch of attention leaves to be joined: of every split, or two
