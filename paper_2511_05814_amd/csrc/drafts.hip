@@ -186,7 +186,8 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_drafts_kernel(VerifyArg
   // the end cuts the last ones are read, those that are not the lane's left out.
   auto steps_of = [&](auto ahead, int t, int upto, auto f) {
     constexpr int AHEAD = decltype(ahead)::value;
-    const T *const p = p0 + cur * a.p_stride, *const q = DRAWN ? q0 + cur * a.q_stride : p;
+    // p itself is p less 0 times p: no choice to make for every entry
+    const T *const p = p0 + cur * a.p_stride, *const q = DRAWN && !bare ? q0 + cur * a.q_stride : p;
     Entries<T> fs[AHEAD], gs[AHEAD];
 #pragma unroll
     for (int x = 0; x < AHEAD; ++x) {
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_drafts_kernel(VerifyArg
 #pragma unroll
       for (int k = 0; k < kRow; ++k) {
         const float e = fs[x].at(k);
-        w[k] = positive(DRAWN && !bare ? fma(-share, (double)gs[x].at(k), (double)e) : (double)e);
+        w[k] = positive(DRAWN ? fma(-share, (double)gs[x].at(k), (double)e) : (double)e);
       }
       const int first = i - skip;
       if (!DRAWN && masked) {
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_drafts_kernel(VerifyArg
     int first, steps;
     part_of(c, wave, first, steps);
     double sum = 0.0;
-    for (int t = 0; t < steps; t += kAhead) 
+    for (int t = 0; t < steps; t += kAhead)
       steps_of(std::integral_constant<int, kAhead>(), first + t, first + steps, [&](int, const double (&w)[kRow]) { sum += sum_of(w); });
     sum = wave_scan_d(sum);
     __syncthreads();   // s_wave is free
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_drafts_kernel(VerifyArg
     }
     total = whole_row();
     if (!ended) left = total, stale = false;
-    else if (total == 0.0 && !bare) bare = true, masked = false;   // nothing is left: p itself
+    else if (total == 0.0 && !bare) bare = true, masked = false, share = 0.0;   // nothing is left: p itself
     else break;
   }
   if (chunk == 0) {
