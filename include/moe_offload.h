@@ -545,7 +545,8 @@ int moe_kv4_tree_attention(const moe_kv4_batch *b, const void *q, int64_t q_stri
  * distribution of the token behind t, taken as it is (entries >= 0 that sum to
  * 1; a negative one counts as 0), row t of q that which t's children were drawn
  * from, independently and in their order; without q (NULL) they were chosen
- * otherwise, as the draft's likeliest for one.  Rows of p and q need only be
+ * otherwise, as the draft's likeliest for one.  Rows of q of tokens without children
+ * are not looked at.  Rows of p and q need only be
  * aligned to their type.  ids [tokens] are the tokens, u [tokens] random numbers
  * in [0, 1) (less counts as 0).  From a sequence's first token, which
  * is certain, the walk tries the children c of where it stands, in their order:

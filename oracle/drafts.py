@@ -73,7 +73,7 @@ def verify(p, ids, parents, u, q=None):
             break
         path.append(accepted)
     if q is not None:
-        rest = positive(row - share * q[at])
+        rest = positive(row - share * q[at]) if gone else positive(row)   # a row of q that drew nothing may hold anything
     else:
         rest = positive(row).copy()
         rest[[x for x in gone if 0 <= x < vocab]] = 0.0

@@ -186,8 +186,9 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_drafts_kernel(VerifyArg
   // the end cuts the last ones are read, those that are not the lane's left out.
   auto steps_of = [&](auto ahead, int t, int upto, auto f) {
     constexpr int AHEAD = decltype(ahead)::value;
-    // p itself is p less 0 times p: no choice to make for every entry
-    const T *const p = p0 + cur * a.p_stride, *const q = DRAWN && !bare ? q0 + cur * a.q_stride : p;
+    // p itself, where no child was refused or nothing is left, is p less 0 times p: no
+    // choice to make for every entry, and a row of q that drew nothing may hold anything
+    const T *const p = p0 + cur * a.p_stride, *const q = DRAWN && share != 0.0 ? q0 + cur * a.q_stride : p;
     Entries<T> fs[AHEAD], gs[AHEAD];
 #pragma unroll
     for (int x = 0; x < AHEAD; ++x) {

@@ -444,6 +444,25 @@ def test_verify_of_more_passes_than_are_shared(vocab, drawn):
     check_verify(lists, p, q_, ids, u, "f32")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [60, 5000, 70001])
+def test_verify_reads_no_q_of_tokens_without_children(vocab, dtype):
+    """A draft has no distribution behind its last tokens: NaN there changes
+    nothing, also where all is accepted up to them."""
+    rng = np.random.default_rng(vocab)
+    for value in (None, 0.0):
+        lists, p, q, ids, u = case(rng, [5, 1, 9], vocab, dtype, True)
+        if value is not None:
+            u[:] = value
+        want = check_verify(lists, p, q, ids, u, dtype)
+        at_ = 0
+        for l in lists:
+            q[[at_ + i for i in range(len(l)) if i not in l]] = np.nan
+            at_ += len(l)
+        got = check_verify(lists, p, q, ids, u, dtype)
+        assert all(np.array_equal(a, b) for a, b in zip(want, got)) and min(got[2]) >= 0
+
+
 @pytest.mark.parametrize("drawn", [True, False])
 def test_verify_without_tokens(drawn):
     p = torch.zeros((0, 50), device="cuda")

@@ -54,6 +54,8 @@ def test_verification_by_hand():
     # refused, then again: nothing is left of token 2; of [0.5, 0.25] the draw takes 0 up to two thirds
     assert od.verify(p, ids, parents, [0.6, 0.25, 0.0], q) == ([0], 0)
     assert od.verify(p, ids, parents, [0.7, 0.25, 0.0], q) == ([0], 1)
+    # a row of q that drew nothing may hold anything
+    assert od.verify(p, ids, parents, [0.9, 0.2, 0.0], np.array([q[0], q[0] * np.nan, q[0] * np.nan])) == ([0, 1], 3)
     # without q: 0.3 >= 0.25 refused, the same id again has no weight
     assert od.verify(p, ids, parents, [0.0, 0.3, 0.0]) == ([0], 0)
     # nothing left at all: the draw is from p itself
