@@ -207,6 +207,8 @@ class Speculation:
     the embedding alone, without any layer."""
 
     def __init__(self, stack: DecoderStack, vocab: int, nodes: int, width: int = 2, seed: int = 0):
+        if vocab < 1 or not 1 <= nodes <= 1024 or width < 1:
+            raise ValueError(f"trees of {nodes} tokens (1 .. 1024), {width} behind each, of {vocab} ids cannot be drafted")
         self.stack, self.vocab, self.nodes, self.width = stack, vocab, nodes, width
         d, rng = stack.moe.cfg.d_model, np.random.default_rng(seed)
         self.embedding = torch.from_numpy(rng.standard_normal((vocab, d), dtype=np.float32)).to("cuda")
@@ -250,8 +252,10 @@ class Speculation:
         path, kept, after = drafts.verify_drafts(self.probabilities(H), tokens.flatten().int(), batch["parent"], u, batch["q_start"],
                                                  q.flatten(0, 1))
         stack.keep(batch, path, kept)
-        taken = kept.tolist()
+        taken, ids = torch.stack([kept, after]).tolist()
         seqs.keep(taken)
+        if any(n and i < 0 for n, i in zip(taken, ids)):
+            raise RuntimeError("probabilities of a next token that are not finite")
         return torch.where(kept > 0, after.long(), pending), taken
 
 

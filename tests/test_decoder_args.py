@@ -120,3 +120,9 @@ def test_more_kept_than_there_was(count, monkeypatch):
     with pytest.raises(ValueError, match="cannot be kept"):
         s.keep(count)
     assert s.length == [2, 0]
+
+
+@pytest.mark.parametrize("vocab,nodes,width", [(0, 4, 2), (9, 0, 2), (9, -1, 2), (9, 1025, 2), (9, 4, 0)])
+def test_trees_that_cannot_be_drafted(vocab, nodes, width):
+    with pytest.raises(ValueError, match="cannot be drafted"):
+        decoder.Speculation(None, vocab, nodes, width)
