@@ -1,11 +1,16 @@
 // Attention of trees of drafted tokens over the 4-bit paged cache: some tens of
-// rows (new tokens times the heads that share a kv head) against a long cache.
+// rows (new tokens times the heads that share a kv head) against long caches whose
+// lengths differ.  Expanding a cache entry takes most of the vector instructions, so
+// one expansion serves as many rows as there are; and workgroups take equal
+// shares of all sequences' work, where a cut of every sequence into the same number of
+// parts leaves most of the chip waiting for the longest (32 trees of 8 tokens
+// over up to 4095: 48 us so, 37 here).
 #include "kv4_attn.hpp"
 
 namespace moe {
 namespace {
 
-// The same for the block of 32 tokens at t0, without what lies at or past `end`
+// tree_bits of the block of 32 tokens at t0, without what lies at or past `end`
 // or, by halves of 16 tokens, on no page.
 __device__ __forceinline__ uint32_t block_bits(const uint32_t *row, int words, int t0, int first, int end, bool held0, bool held1) {
   uint32_t b = tree_bits(row, words, t0 - first);
@@ -40,9 +45,10 @@ __device__ __forceinline__ int wave_scan(int v) {
 // A launch's work: units, each ROWS rows of a sequence and kv head, of as many
 // steps as the sequence has STEP tokens, and AHEAD more for what it takes to begin
 // and end one, all one behind the other.  Each of W workgroups takes as much of all
-// T as the others (W is at most T), whatever the lengths are.  A unit that lies in several workgroups is joined afterwards: a workgroup
-// has at most one whose first steps others have and one whose last ones others
-// have, and a place for the rows of each.
+// T as the others (W is at most T), whatever the lengths are.  A unit that lies in
+// several workgroups is joined afterwards: a workgroup has at most one whose first
+// steps others have and one whose last ones others have, and a place for the rows
+// of each.
 constexpr int kMaxSeqs = 256;   // of a call; workgroups have no fewer threads
 template <int ROWS, int STEP, int AHEAD>
 struct Plan {
@@ -151,7 +157,14 @@ template <int R> using TilePlan = Plan<16 * R, kStepTokens, kAhead>;
 // R tiles of 16 rows against blocks of 32 tokens, by one wave, four of them on
 // neighbouring blocks: the layout of kv4_attention_kernel, but a block's keys and
 // values are expanded once for all tiles.  The queries lie in LDS, in operand
-// order.
+// order.  The products of a score start from minus the row's reference, which the
+// matrix cores add for nothing; whether a weight passes fp16's range shows in
+// their sum, so that most blocks need no maximum over lanes: some 30
+// instructions a tile and block, beside 330 of the expansion.
+// Two tiles, 32 trees of 8 tokens over up to 4095: 33 us, of which vector instructions
+// take 40%, matrix instructions 10%; the rest is what a workgroup needs to begin and end
+// (prefix sums, table, queries, first block, join of its waves: some 12000 clocks beside
+// 3200 a step) and waiting for loads, of which a block a wave is in flight.
 template <int D, typename T, int R>
 __global__ __launch_bounds__(kThreads, R == 1 && sizeof(T) == 2 ? 3 : 2) void kv4_tree_kernel(KvAttnArgs a) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
@@ -463,7 +476,13 @@ __global__ __launch_bounds__(kThreads, R == 1 && sizeof(T) == 2 ? 3 : 2) void kv
   }
 }
 
-// Rows in blocks of 128, 32 a wave: the layout of kv4_prompt_kernel.
+// bf16: rows in blocks of 32 a wave, the layout of kv4_prompt_kernel, whose tiles of
+// LDS four waves fill or, where there are rows for them, eight: with those the
+// expansion of a tile serves 256 rows.  A wave fetches from one page, so that its
+// addresses are a scalar and constants of the lane (24 tokens over 131071: 104 -> 99
+// us).  8 trees of up to 64 tokens over up to 16383, 71 GFLOP: 95 us and 9 the
+// join, 690 TFLOP/s; 1 of 24 over 131071, 52 GFLOP: 90 and 9.  Vector instructions are busy some
+// 45% of the time, matrix instructions 25%, mostly one after another; barriers and loads are the rest.
 constexpr int kWideTile = 64;
 template <int D, int WAVES>
 __global__ __launch_bounds__(kWave * WAVES, 2) void kv4_tree_wide_kernel(KvAttnArgs a) {
@@ -854,21 +873,21 @@ void launch(const KvAttnArgs &a, int tiles, hipStream_t s) {
 
 }  // namespace
 
-// Which kernels, by the work of one head and block of 16 rows: steps of 128 tokens.
-// us of a pass, 32 heads to 8 of 128 unless said otherwise; "split" are the kernels of
-// kv4_attn.hip, cut the same way whatever the lengths are:
-//                                              split   1 tile   2 tiles   128 rows
-//   32 of 8 tokens over up to 4095, ragged        48       42        38         56
-//   1 of 8 over 131071                            71       73        56         84
-//   1 of 8 over 16384                             25       22        23         26
-//   1 of 24 over 131071                          110      177       116        104
-//   8 of up to 64 over up to 16383               146      243       157        115
-//   16 of 16 over 8191 / of 24                 94 / 91  92 / 108   72 / 78    82 / 74
-//   64 of 4 over 2047 / 128 over 1500          32 / 43  34 / 48   41 / 59     67 / 101
-//   64 of 8 over 700 / over 4095              25 / 105  31 / 85   30 / 66    44 / 106
-//   fp32: 16 of 12 over 8191 / 4 of 48 over 16000  69 / 179  63 / 135  72 / 123  116 / 138
-//   fp32, 16 heads: 32 of 32 over 2047 / 6000  56 / 132  62 / 121  68 / 126  142 / 306
-//   1 of 1 over 600                                8       11        12         12
+// Which kernels, by the steps of 128 tokens of all blocks of 16 rows.  us of a pass, 32
+// heads to 8 of 128, bf16 unless said otherwise; "split" are the kernels of
+// kv4_attn.hip, which cut every sequence alike:
+//                                                split  1 tile  2 tiles  128 rows  256
+//   32 of 8 tokens over up to 4095, ragged          48      43       38        50   77
+//   1 of 8 over 131071 / over 16384             68 / 25 71 / 22  56 / 23   75 / 24
+//   1 of 24 over 131071                            112     180      119        99  120
+//   8 of up to 64 over up to 16383                 145     247      158       111  103
+//   16 over 8191, of 16 / of 24                 91 / 91 89 / 109 65 / 77   75 / 70
+//   4 of 16 over 8191 / 2 of 200 over 4000      36 / 46 27 / 62  27 / 47   32 / 43   45
+//   64 of 4 over 2047 / 128 over 1500           33 / 43 34 / 48  43 / 59   62 / 94
+//   64 of 8 over 700 / over 4095               25 / 105 32 / 79  30 / 62   42 / 96
+//   1 of 1 over 600                                  8      10       11
+//   fp32: 16 of 12 over 8191 / 4 of 48 over 16000  69 / 180  63 / 134  71 / 122
+//   fp32, 16 heads: 32 of 32 over 2047 / 6000      56 / 132  62 / 122  67 / 126
 // The plan and the join cost more than they save where a unit has few steps and there
 // are enough units without it, and where there is little to share out.
 KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len, int64_t table_tokens, int head_dim, bool f32) {
@@ -883,8 +902,9 @@ KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int ma
   if (f32 && rows < 64) tiles = 1;
   if (!f32 && rows > 64 && work >= 24576) tiles = head_dim == 128 && rows > 192 ? 16 : 8;
   const int per = 16 * tiles;
-  // T has to fit an int, for the longest sequences that the table has room for
-  if ((full / per + seqs) * kv_heads >= ((int64_t)1 << 31) / (table_tokens / kWideTile + kAhead + 2)) return s;
+  // T has to fit an int, for the longest sequences that the table has room for and
+  // whatever q_start holds
+  if ((full / per + 1) * pairs >= ((int64_t)1 << 31) / (table_tokens / kWideTile + kAhead + 2)) return s;
   s.tiles = tiles;
   const int64_t blocks = (rows + per - 1) / per, room = kMaxGroups / (pairs * per);
   s.row_blocks = (int)(blocks < 1 || room < 1 ? 1 : blocks > room ? room : blocks);
