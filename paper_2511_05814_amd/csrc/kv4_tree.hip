@@ -480,9 +480,13 @@ __global__ __launch_bounds__(kThreads, R == 1 && sizeof(T) == 2 ? 3 : 2) void kv
 // LDS four waves fill or, where there are rows for them, eight: with those the
 // expansion of a tile serves 256 rows.  A wave fetches from one page, so that its
 // addresses are a scalar and constants of the lane (24 tokens over 131071: 104 -> 99
-// us).  8 trees of up to 64 tokens over up to 16383, 71 GFLOP: 95 us and 9 the
-// join, 690 TFLOP/s; 1 of 24 over 131071, 52 GFLOP: 90 and 9.  Vector instructions are busy some
-// 45% of the time, matrix instructions 25%, mostly one after another; barriers and loads are the rest.
+// us), and scores start from minus the row's reference, as above (97 -> 95).
+// 8 trees of up to 64 tokens over up to 16383, 71 GFLOP: 98 us with 9 for the join, 720
+// TFLOP/s; 1 of 24 over 131071, 52 GFLOP: 96 and 9.  A tile takes some 5000 clocks, of
+// which the matrix cores work 2000; what a workgroup needs to begin and to write its parts
+// is 11 us.  Waves in two groups half a tile apart, products of one beside weights of
+// the other, come to the same: vector instructions of one wave alone take 5 to 6
+// clocks each, and both groups' follow each other.
 constexpr int kWideTile = 64;
 template <int D, int WAVES>
 __global__ __launch_bounds__(kWave * WAVES, 2) void kv4_tree_wide_kernel(KvAttnArgs a) {
@@ -552,47 +556,66 @@ __global__ __launch_bounds__(kWave * WAVES, 2) void kv4_tree_wide_kernel(KvAttnA
     }
 
     float m = -__builtin_inff(), l = 0.0f;
-    floatx16 o[NB];
+    floatx16 o[NB], under;   // under: minus the row's reference score, or 0
+#pragma unroll
+    for (int i = 0; i < 16; ++i) under[i] = 0.0f;
 #pragma unroll
     for (int u = 0; u < NB; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[u][i] = 0.0f;
 
-    // A wave's share of a tile are 16 tokens, `mine16` of them first, with eight
-    // waves half of their dimensions; a thread's: KL words of key lane % 16 from
-    // word w0 on, and, of the 8 dimensions of octet r / (8 / NB), NB (half of them) of values 4
-    // hi + 0 .. 3 and + 8.
-    constexpr int SHARE = WAVES / 4, KL = KW / SHARE;
-    const int block = wave & 1, half16 = wave >> 1 & 1, other = wave >> 2;
-    const int w0 = KW * (lane >> 4) + KL * other;
+    // A wave expands 16 tokens of a tile; with eight waves four their keys and four
+    // their values, so that none expands both metas for half of the codes.  A
+    // thread's are the KW words of key lane % 16 from word w0 on, and, of the 8 dimensions
+    // of octet r / (8 / NB), NB of values 4 hi + 0 .. 3 and + 8.
+    const bool does_keys = wave < 4, does_values = WAVES == 4 || wave >= 4;
+    const int block = wave & 1, half16 = wave >> 1 & 1;
+    const int w0 = KW * (lane >> 4);
     const uint32_t k_lane = (lane & 15) * (D / 2) + w0 * 4, km_lane = kmetas + (lane & 15) * (D / 16) + w0 / 4 * 2;
     const uint32_t oct = (uint32_t)r / (8 / NB), v_lane = values + hi * (2 * D) + oct * 16, vm_lane = vmetas + hi * (D / 4) + oct / 4 * 8;
-    uint32_t kw[KL], km;
-    u32x4 vw[2];
+    u32x4 kw, vw[2];
+    uint32_t km;
     u32x2 vm[2];
     bool v_held;
-    auto fetch = [&](int t0) {
-      const int mine16 = t0 + 32 * block + 16 * half16;
-      const uint8_t *rec = page_of(mine16, v_held);
-      const uint32_t in = mine16 & page_mask;
-      const uint8_t *kp = rec + in * (D / 2) + k_lane;
-      if constexpr (KL == 4) *reinterpret_cast<u32x4 *>(kw) = *reinterpret_cast<const u32x4 *>(kp);
-      else *reinterpret_cast<u32x2 *>(kw) = *reinterpret_cast<const u32x2 *>(kp);
-      km = *reinterpret_cast<const uint16_t *>(rec + in * (D / 16) + km_lane);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        vw[x] = *reinterpret_cast<const u32x4 *>(rec + in * (D / 2) + 2 * x * (2 * D) + v_lane);
-        vm[x] = *reinterpret_cast<const u32x2 *>(rec + in * (D / 16) + 2 * x * (D / 4) + vm_lane);
-      }
+    const int base = work.first * kWideTile, count = max(0, (end - base + kWideTile - 1) / kWideTile);
+    int page;   // of the tile that is fetched next
+    auto find = [&](int n) {
+      const int col = (base + n * kWideTile + 32 * block + 16 * half16) >> a.kv.page_log2;
+      page = col < a.kv.table_cols ? table[col] : -1;
     };
-    auto stage = [&](int t0, int buf) {
-      uint8_t *to = s_kv[buf];
-      {
+    auto fetch = [&](int n) {
+      if (n >= count) return;
+      v_held = page >= 0 && page < a.kv.pages;
+      const uint8_t *rec = a.kv.pool + ((size_t)(v_held ? page : 0) * a.kv.kv_heads + g) * page_bytes;
+      const uint32_t in = (base + n * kWideTile + 32 * block + 16 * half16) & page_mask;
+      if (does_keys) {
+        const uint8_t *kp = rec + in * (D / 2) + k_lane;
+        if constexpr (KW == 4) {
+          kw = *reinterpret_cast<const u32x4 *>(kp);
+        } else {
+          const u32x2 two = *reinterpret_cast<const u32x2 *>(kp);
+          kw[0] = two[0], kw[1] = two[1];
+        }
+        km = *reinterpret_cast<const uint16_t *>(rec + in * (D / 16) + km_lane);
+      }
+      if (does_values) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          vw[x] = *reinterpret_cast<const u32x4 *>(rec + in * (D / 2) + 2 * x * (2 * D) + v_lane);
+          vm[x] = *reinterpret_cast<const u32x2 *>(rec + in * (D / 16) + 2 * x * (D / 4) + vm_lane);
+        }
+      }
+      find(n + 1);
+    };
+    auto stage = [&](int n) {
+      const int t0 = base + n * kWideTile, buf = n & 1;
+      if (does_keys) {
         const Pair pair = key_pair(km);
 #pragma unroll
-        for (int x = 0; x < KL; ++x)
-          *reinterpret_cast<half8 *>(to + block * KB + (w0 + x) * 512 + (16 * half16 + (lane & 15)) * 16) = key_values(kw[x], pair, masks_);
+        for (int x = 0; x < KW; ++x)
+          *reinterpret_cast<half8 *>(s_kv[buf] + block * KB + (w0 + x) * 512 + (16 * half16 + (lane & 15)) * 16) = key_values(kw[x], pair, masks_);
       }
+      if (!does_values) return;
       // tokens that no row sees must not reach the products, whatever their bytes are
       uint32_t metas[4] = {vm[0][0], vm[0][1], vm[1][0], vm[1][1]};
       if (!v_held || t0 + kWideTile > end) {
@@ -604,17 +627,16 @@ __global__ __launch_bounds__(kWave * WAVES, 2) void kv4_tree_wide_kernel(KvAttnA
       const bool marked = value_pairs(metas, pairs);
       const uint32_t first_byte = pick_byte(r % (8 / NB) * (NB / 2));
 #pragma unroll
-      for (int i = 0; i < NB / 2 / SHARE; ++i) {
-        const int bt = SHARE == 1 ? i : other;
+      for (int bt = 0; bt < NB / 2; ++bt) {
         half8 v0, v1;
         value_byte(vw, first_byte + bt * 0x00010001u, pairs, masks_, v0, v1);
-        uint8_t *at = to + 2 * KB + block * KB + half16 * 1024 + lane * 16;
+        uint8_t *at = s_kv[buf] + 2 * KB + block * KB + half16 * 1024 + lane * 16;
         *reinterpret_cast<half8 *>(at + (2 * bt) * 2048) = v0;
         *reinterpret_cast<half8 *>(at + (2 * bt + 1) * 2048) = v1;
       }
       const bool any = __builtin_amdgcn_ballot_w64(marked) != 0;
-      if (lane == 0 && other == 0) s_any[buf][wave] = (any ? 1u : 0u) | (v_held ? 0u : 2u);
-      if (any && r % 8 == 0 && other == 0) {   // a lane of each group of 32 dimensions (D 64: of each half)
+      if (lane == 0) s_any[buf][wave & 3] = (any ? 1u : 0u) | (v_held ? 0u : 2u);
+      if (any && r % 8 == 0) {   // a lane of each group of 32 dimensions (D 64: of each half)
         uint8_t *mp = &s_mark[buf][r / (8 / NB) / 4][32 * block + 16 * half16 + 4 * hi];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -623,26 +645,25 @@ __global__ __launch_bounds__(kWave * WAVES, 2) void kv4_tree_wide_kernel(KvAttnA
         }
       }
     };
-
-    // the first pass only stages
-    int t0 = (work.first - 1) * kWideTile, buf = 1;
-    if (t0 + kWideTile < end) fetch(t0 + kWideTile);
-    for (bool staged = false; t0 < end; t0 += kWideTile, buf ^= 1, staged = true, __syncthreads()) {
+    __syncthreads();   // the unit before is done with
+    if (count) {
+      find(0);
+      fetch(0);
+      stage(0);
+      fetch(1);
+      __syncthreads();
+    }
+    for (int n = 0; n < count; ++n, __syncthreads()) {
+      const int t0 = base + n * kWideTile, buf = n & 1;
       const uint8_t *from = s_kv[buf];
-      if (t0 + kWideTile < end) {
-        stage(t0 + kWideTile, buf ^ 1);
-        if (t0 + 2 * kWideTile < end) fetch(t0 + 2 * kWideTile);
-      }
-      if (!staged || wrow >= seq.rows) continue;
+      if (n + 1 < count) stage(n + 1);
+      fetch(n + 2);
+      if (wrow >= seq.rows) continue;
       __builtin_amdgcn_sched_barrier(0);   // staging's registers are free again before the scores take theirs
       const u32x4 any4 = *reinterpret_cast<const u32x4 *>(s_any[buf]);
       const uint32_t any = __builtin_amdgcn_readfirstlane(any4[0] | any4[1] | any4[2] | any4[3]);
       // two chains of products, the operands of the next two steps on their way
-      floatx16 s[2];
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[x][i] = 0.0f;
+      floatx16 s[2] = {under, under};
       half8 k[3][2];
       auto keys = [&](int x, int t) { return *reinterpret_cast<const half8 *>(from + x * KB + t * 1024 + lane * 16); };
 #pragma unroll
@@ -678,22 +699,23 @@ __global__ __launch_bounds__(kWave * WAVES, 2) void kv4_tree_wide_kernel(KvAttnA
 #pragma unroll
       for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
       top = max_of_halves(top);
-      if (__builtin_amdgcn_ballot_w64((top - m) * rs.down > Hold<1>::slack)) {
-        top = fmaxf(m, top);
-        const float keep = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - top) * rs.down);
-        m = top;
+      if (__builtin_amdgcn_ballot_w64(m == -__builtin_inff() || top * rs.down > Hold<1>::slack)) {
+        // without a reference, what is largest up to now, else no less than that
+        const float by = m == -__builtin_inff() ? (top == -__builtin_inff() ? 0.0f : top) : fmaxf(top, 0.0f);
+        const float high = m == -__builtin_inff() ? top : m + by, keep = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(-by * rs.down);
+        m = high;
         l *= keep;
 #pragma unroll
         for (int u = 0; u < NB; ++u) o[u] *= keep;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) under[i] -= by, s[0][i] -= by, s[1][i] -= by;
       }
-      const float ref = m == -__builtin_inff() ? 0.0f : m;
       // probabilities of the next 16 tokens ahead of the products of these
       half8 p[4][1];
       auto weigh = [&](int part) {
 #pragma unroll
         for (int e = 0; e < 8; e += 2)
-          add_pair<1>(power<1>(s[part / 2][8 * (part % 2) + e], ref, rs.down), power<1>(s[part / 2][8 * (part % 2) + e + 1], ref, rs.down), e,
-                          p[part], l);
+          add_pair<1>(weight<1>(s[part / 2][8 * (part % 2) + e], rs.down), weight<1>(s[part / 2][8 * (part % 2) + e + 1], rs.down), e, p[part], l);
       };
       weigh(0);
 #pragma unroll
@@ -877,12 +899,12 @@ void launch(const KvAttnArgs &a, int tiles, hipStream_t s) {
 // heads to 8 of 128, bf16 unless said otherwise; "split" are the kernels of
 // kv4_attn.hip, which cut every sequence alike:
 //                                                split  1 tile  2 tiles  128 rows  256
-//   32 of 8 tokens over up to 4095, ragged          48      43       38        50   77
+//   32 of 8 tokens over up to 4095, ragged          48      43       37        50   67
 //   1 of 8 over 131071 / over 16384             68 / 25 71 / 22  56 / 23   75 / 24
-//   1 of 24 over 131071                            112     180      119        99  120
-//   8 of up to 64 over up to 16383                 145     247      158       111  103
-//   16 over 8191, of 16 / of 24                 91 / 91 89 / 109 65 / 77   75 / 70
-//   4 of 16 over 8191 / 2 of 200 over 4000      36 / 46 27 / 62  27 / 47   32 / 43   45
+//   1 of 24 over 131071                            112     180      118        97  103
+//   8 of up to 64 over up to 16383                 145     247      157       111   99
+//   16 over 8191, of 16 / of 24                 91 / 91 89 / 109 65 / 77   74 / 71 85 / 77
+//   4 of 16 over 8191 / 2 of 200 over 4000      36 / 46 27 / 62  27 / 47   32 / 43 31 / 44
 //   64 of 4 over 2047 / 128 over 1500           33 / 43 34 / 48  43 / 59   62 / 94
 //   64 of 8 over 700 / over 4095               25 / 105 32 / 79  30 / 62   42 / 96
 //   1 of 1 over 600                                  8      10       11
