@@ -895,34 +895,51 @@ void launch(const KvAttnArgs &a, int tiles, hipStream_t s) {
 
 }  // namespace
 
-// Which kernels, by the steps of 128 tokens of all blocks of 16 rows.  us of a pass, 32
+// Which kernels: by `units`, blocks of 16 rows of all sequences and kv heads, `steps`
+// of 128 tokens of the longest sequence, and their product `work`.  us of a pass, 32
 // heads to 8 of 128, bf16 unless said otherwise; "split" are the kernels of
-// kv4_attn.hip, which cut every sequence alike:
-//                                                split  1 tile  2 tiles  128 rows  256
-//   32 of 8 tokens over up to 4095, ragged          48      43       37        50   67
-//   1 of 8 over 131071 / over 16384             68 / 25 71 / 22  56 / 23   75 / 24
-//   1 of 24 over 131071                            112     180      118        97  103
-//   8 of up to 64 over up to 16383                 145     247      157       111   99
-//   16 over 8191, of 16 / of 24                 91 / 91 89 / 109 65 / 77   74 / 71 85 / 77
-//   4 of 16 over 8191 / 2 of 200 over 4000      36 / 46 27 / 62  27 / 47   32 / 43 31 / 44
-//   64 of 4 over 2047 / 128 over 1500           33 / 43 34 / 48  43 / 59   62 / 94
-//   64 of 8 over 700 / over 4095               25 / 105 32 / 79  30 / 62   42 / 96
-//   1 of 1 over 600                                  8      10       11
-//   fp32: 16 of 12 over 8191 / 4 of 48 over 16000  69 / 180  63 / 134  71 / 122
-//   fp32, 16 heads: 32 of 32 over 2047 / 6000      56 / 132  62 / 122  67 / 126
-// The plan and the join cost more than they save where a unit has few steps and there
-// are enough units without it, and where there is little to share out.
+// kv4_attn.hip, which cut every sequence alike (from 64 rows on, those of prompts):
+//                                             units steps  split 1 tile 2 tiles 128 rows  256
+//   up to 16 rows: 64 of 4 tokens over 2047     512    17     33     34      43       62   96
+//     1 of 4 over 8000                            8    63     16     17      18       18
+//   up to 63: 64 of 8 over 700                 1024     6     25     32      30       42   61
+//     64 of 8 over 1200                        1024    10     35     36      34       48
+//     64 of 8 over 1800                        1024    15     50     50      44       63
+//     16 of 8 over 1200                         256    10     18     20      20       22
+//     1 of 8 over 2000                           16    17     13     13      13       15
+//     1 of 8 over 4096                           16    33     19     17      17       19   18
+//     32 of 8 over up to 4095, ragged           512    33     48     43      37       50   67
+//     1 of 8 over 131071                         16  1025     68     71      56       75
+//   from 64: 1 of 16 over 1500                   32    12     18     14      14       16   18
+//     4 of 16 over 8191                         128    65     36     27      27       32   31
+//     100 of 16 over 1024                      3200     9     74     85      67       75   98
+//     64 of 32 over 100                        4096     2     20     52      46       35   47
+//     16 of 24 over 8191                        768    65     91    109      77       71   77
+//     32 of 32 over 1000                       2048     9     44     56      45       37   43
+//     4 of 64 over 1500                         512    13     31     27      26       30   32
+//     2 of 1000 over 1000                      4000    16    121    159     112       79   74
+//     1 of 24 over 131071                        48  1025    112    180     118       97  103
+//     8 of up to 64 over up to 16383           1024   129    145    247     157      111   99
+//   fp32: 16 of 12 over 8191                    384    65     69     63      71
+//     10 of 49 over 1393                       1040    12     50     46      50
+//     4 of 48 over 16000                        384   126    180    134     122
+//     16 heads to 16, 32 of 32 over 2047       1024    17     56     62      67
+//     the same over 6000                       1024    48    132    122     126
+// The plan and the join cost more than they save where units have few steps, and where there
+// is little to share out.
 KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len, int64_t table_tokens, int head_dim, bool f32) {
   KvAttnShape s = kv4_attention_shape(seqs, kv_heads, heads, tokens, max_new, max_len);
   const int64_t full = (int64_t)tokens * (heads / kv_heads);   // rows, were they all of one sequence
   const int64_t hinted = (int64_t)max_new * (heads / kv_heads), rows = hinted < full ? hinted : full;
   const int64_t pairs = (int64_t)seqs * kv_heads, units = pairs * ((rows + 15) / 16), steps = ((int64_t)max_len + kStepTokens - 1) / kStepTokens;
-  if (seqs > kMaxSeqs || max_len <= 512 || (units >= 512 && steps <= 20)) return s;
   const int64_t work = units * steps;
-  if (work < 512) return s;
-  int tiles = rows > 16 && work >= 12288 ? 2 : 1;
-  if (f32 && rows < 64) tiles = 1;
-  if (!f32 && rows > 64 && work >= 24576) tiles = head_dim == 128 && rows > 192 ? 16 : 8;
+  if (seqs > kMaxSeqs) return s;
+  if (rows < 64 && (steps <= 12 || work < 512 || (units >= 512 && steps <= 20 && (f32 || rows <= 16)))) return s;
+  if (work < 64 || (units >= 512 && steps <= 2)) return s;
+  int tiles;
+  if (f32) tiles = rows >= 64 && work >= 24576 ? 2 : 1;
+  else if (rows > 64 && work >= 8192) tiles = head_dim == 128 && rows > 224 ? 16 : 8;
+  else tiles = rows > 16 && work >= (rows < 64 ? 12288 : 4096) ? 2 : 1;
   const int per = 16 * tiles;
   // T has to fit an int, for the longest sequences that the table has room for and
   // whatever q_start holds

@@ -145,8 +145,8 @@ SHAPES = [
 
 
 # how long the caller says that sequences are: by it, and the rows, the kernels
-# differ (results are right whatever it is): without splits, or for lengths that
-# differ, of 16, 32 or (bf16, from 65 rows on) 128 rows
+# differ (results are right whatever it is): those of kv4_attention, or for lengths that
+# differ, of 16, 32 or (bf16, from 65 rows on) 128 or 256 rows
 HINTS = [None, 1000, 1 << 20]
 
 
@@ -237,6 +237,23 @@ def test_tokens_without_places_and_missing_pages(new, hint):
     assert (o[new[0] + 1:] == 0).all()
     bt.table[:, :] = 1 << 30
     assert (check_tree(bt, "bf16", seen, **hints)[0] == 0).all()
+
+
+@pytest.mark.parametrize("hint", HINTS)
+@pytest.mark.parametrize("kind", ["tree", "any", "none"])
+@pytest.mark.parametrize("heads", [4, 6, 8])
+def test_large_blocks_with_holes_and_growing_scores(heads, kind, hint):
+    """More rows of a sequence than a block has, pages that are missing in the middle
+    of a tile or take all of it, references that many tokens pass."""
+    bt = Batch([120, 3, 60], [1500, 0, 90], heads, 2, 128, 16, seed=heads).fill(0.3)
+    for i, pos in enumerate(range(7, 1500, 61)):
+        change(bt, 0, pos, i % 2, key_of(2.0 ** (i / 3 - 4)))
+    for col in (2, 16, 17, 18, 19, 95):
+        bt.table[0, col] = -1
+    bt.table[2, 1] = 1 << 30
+    q = np.abs(np.random.default_rng(5).standard_normal((bt.tokens, heads, 128)))
+    for dtype in ("f32", "bf16"):
+        check_tree(bt, dtype, masks(bt, np.random.default_rng(heads), kind), q=q, max_new=120, max_len=hint)
 
 
 @pytest.mark.parametrize("new", [3, 9, 25, 150])
