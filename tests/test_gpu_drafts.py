@@ -605,6 +605,41 @@ def test_a_step_in_a_graph_and_on_another_stream(most):
             assert all(torch.equal(a, b) for a, b in zip(out + pools, eager))
 
 
+def test_calls_on_two_streams_and_in_a_graph_at_once():
+    """Rows that workgroups share and sequences that lie in many: calls that run
+    beside each other, on other streams and as replays, give what they give alone."""
+    calls = []
+    for seed, dtype in ((1, "bf16"), (2, "f32")):
+        rng = np.random.default_rng(seed)
+        bt = Batch([30, 1, 50], [3000, 40, 900], 8, 2, 128, 16, seed=seed).fill(0.3)
+        args, seen = bt.args(), words(bt, masks(bt, rng, "tree"))
+        q = device(rng.standard_normal((bt.tokens, 8, 128)), dtype)
+        lists, p, d, ids, u = case(rng, [12, 1, 16, 7], 140001, dtype, True)
+        rest = ints(ids), ints([x for l in lists for x in l]), torch.from_numpy(u).cuda(), ints(starts([len(l) for l in lists])), device(d, dtype)
+        P = device(p, dtype)
+        calls.append(lambda args=args, seen=seen, q=q, rest=rest, P=P: [
+            at().kv4_tree_attention(q, *args, seen, 0.1, max_new=50, max_len=3050), *dr().verify_drafts(P, *rest)])
+    want = [call() for call in calls]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        replayed = calls[0]()
+    sides = [torch.cuda.Stream() for _ in calls]
+    for _ in range(8):
+        got = []
+        for t in replayed:
+            t.zero_()
+        for side in sides:
+            side.wait_stream(torch.cuda.current_stream())
+        graph.replay()
+        for side, call in zip(sides, calls):
+            with torch.cuda.stream(side):
+                got.append(call())
+        torch.cuda.synchronize()
+        for a, b in zip(got + [replayed], want + [want[0]]):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
 def test_what_is_kept_is_what_a_chain_would_have_stored():
     """Accepted tokens' entries and outputs are those that the same tokens,
     taken one after another without drafts, have: the keys' bits to the last one."""
