@@ -256,6 +256,26 @@ def test_large_blocks_with_holes_and_growing_scores(heads, kind, hint):
         check_tree(bt, dtype, masks(bt, np.random.default_rng(heads), kind), q=q, max_new=120, max_len=hint)
 
 
+@pytest.mark.parametrize("hint", HINTS)
+@pytest.mark.parametrize("D,new", [(64, 3), (64, 50), (128, 9), (128, 25), (128, 130)])
+def test_steps_of_any_size(D, new, hint):
+    """Groups whose steps lie at both ends of the scale grid, and between them."""
+    bt = Batch([new, 2], [150, 33], 4, 2, D, 32, seed=8).fill(0.3)
+    rng = np.random.default_rng(new)
+    for i, pos in enumerate(rng.permutation(150)[:60]):
+        size = [2.0 ** -24, 1e-6, 2.0 ** -17, 300.0, 7600.0, 7700.0, 28000.0][i % 7]
+        for h in range(2):
+            page = bt.table[0, pos // 32]
+            rec = [np.array(x) for x in oa.unpack_record(bt.pool[page, h], 32, D)]
+            for part in (0, 2):
+                codes, metas = oa.kv4_quantize(rng.uniform(-1, 1, (1, D)) * size)
+                rec[part][pos % 32], rec[part + 1][pos % 32] = codes[0], metas[0]
+            bt.pool[page, h] = oa.record(*rec)
+    q = rng.standard_normal((bt.tokens, 4, D)) * 1e-3
+    for dtype in ("f32", "bf16"):
+        check_tree(bt, dtype, masks(bt, rng, "any"), q=q, max_new=new, max_len=hint)
+
+
 @pytest.mark.parametrize("new", [3, 9, 25, 150])
 @pytest.mark.parametrize("part", [0, 2])
 @pytest.mark.parametrize("hint", HINTS)
