@@ -28,6 +28,15 @@ __device__ __forceinline__ float weight(float above, float down) {
   return __builtin_amdgcn_exp2f(fmaf(above, down, Hold<PARTS>::shift));
 }
 constexpr float kRange = 32768.0f;   // 2^(shift + slack): weights below it fit fp16
+// Whether one of a lane's eight weights passes the range or is a NaN, or any is
+// relative to no reference.  bf16 calls hold a weight at the reference as 2^8: eight of
+// them stay far below the range, so their sum tells.  fp32 calls hold it as
+// 2^14, of which two make the range already: the largest tells, and the sum a NaN.
+template <int PARTS>
+__device__ __forceinline__ bool out_of_range(float sum, float most) {
+  if constexpr (PARTS == 1) return !(sum < kRange);
+  return !(sum < 8 * kRange) || most >= kRange;
+}
 
 // Sums over a wave's lanes up to each.
 template <int CTRL, int ROWS>
@@ -159,8 +168,9 @@ template <int R> using TilePlan = Plan<16 * R, kStepTokens, kAhead>;
 // values are expanded once for all tiles.  The queries lie in LDS, in operand
 // order.  The products of a score start from minus the row's reference, which the
 // matrix cores add for nothing; whether a weight passes fp16's range shows in
-// their sum, so that most blocks need no maximum over lanes: some 30
-// instructions a tile and block, beside 330 of the expansion.
+// a lane's own sum (fp32 calls: largest, see out_of_range), so that blocks need no
+// maximum over lanes until a row's scores rise past its reference: some 30
+// instructions a tile and block (four more in fp32), beside 330 of the expansion.
 // Two tiles, 32 trees of 8 tokens over up to 4095: 31 to 33 us, of which vector
 // instructions take half, matrix instructions 14%; the rest is what a workgroup needs to begin and end
 // (prefix sums, table, queries, first block, join of its waves: some 12000 clocks beside
@@ -323,12 +333,15 @@ __global__ __launch_bounds__(kThreads, R == 1 && sizeof(T) == 2 ? 3 : 2) void kv
           }
       };
       half8 p[R][PARTS];
-      float sum[R];
+      float sum[R], most[R];   // of a lane's weights; most: fp32 calls alone
       auto weigh = [&](int x, const floatx4 (&s)[2]) {
-        sum[x] = 0.0f;
+        sum[x] = most[x] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; i += 2)
-          add_pair<PARTS>(weight<PARTS>(s[i / 4][i % 4], down[x]), weight<PARTS>(s[i / 4][i % 4 + 1], down[x]), i, p[x], sum[x]);
+        for (int i = 0; i < 8; i += 2) {
+          const float w0 = weight<PARTS>(s[i / 4][i % 4], down[x]), w1 = weight<PARTS>(s[i / 4][i % 4 + 1], down[x]);
+          if constexpr (PARTS == 2) most[x] = fmaxf(most[x], fmaxf(w0, w1));
+          add_pair<PARTS>(w0, w1, i, p[x], sum[x]);
+        }
       };
       // Blocks that all rows see: weights relative to the reference as it is, unless
       // a sum says that one passes the range (or that there is no reference, or
@@ -341,7 +354,7 @@ __global__ __launch_bounds__(kThreads, R == 1 && sizeof(T) == 2 ? 3 : 2) void kv
         for (int x = 0; x < R; ++x) {
           if (x + 1 < R) scores(x + 1, under[x + 1], s[(x + 1) % 2]);   // on the matrix cores while these are weighed
           weigh(x, s[x % 2]);
-          passed |= !(sum[x] < kRange);
+          passed |= out_of_range<PARTS>(sum[x], most[x]);
         }
       }
       // Others, and those: with the reference no less than the block's largest.
@@ -920,11 +933,13 @@ void launch(const KvAttnArgs &a, int tiles, hipStream_t s) {
 //     2 of 1000 over 1000                      4000    16    121    159     112       79   74
 //     1 of 24 over 131071                        48  1025    112    180     118       97  103
 //     8 of up to 64 over up to 16383           1024   129    145    247     157      111   99
-//   fp32: 16 of 12 over 8191                    384    65     69     63      71
-//     10 of 49 over 1393                       1040    12     50     46      50
-//     4 of 48 over 16000                        384   126    180    134     122
-//     16 heads to 16, 32 of 32 over 2047       1024    17     56     62      67
-//     the same over 6000                       1024    48    132    122     126
+//   fp32, scores with a spread of 2 / of 0.2 about their mean, whose blocks need the
+//   reference moved less often:
+//     16 of 12 over 8191                        384    65    70/67  65/52   75/53
+//     10 of 49 over 1393                       1040    12    50/47  47/40   51/38
+//     4 of 48 over 16000                        384   126   178/167 134/116 124/86
+//     16 heads to 16, 32 of 32 over 2047       1024    17    56/53  63/52   68/49
+//     the same over 6000                       1024    48   130/127 123/101 124/89
 // The plan and the join cost more than they save where units have few steps, and where there
 // is little to share out.
 KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len, int64_t table_tokens, int head_dim, bool f32) {

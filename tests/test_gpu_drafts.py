@@ -349,6 +349,52 @@ def test_strided_queries_given_outputs_and_workspaces():
         assert torch.equal(wide[:, 2:10], want)
 
 
+@pytest.mark.parametrize("size", [0.0, 1e-3, 0.05])
+@pytest.mark.parametrize("D,heads,new", [(64, 4, [20, 1, 33]), (128, 8, [9, 4, 2]), (128, 4, [40, 70])])
+def test_flat_scores(D, heads, new, size):
+    """Rows whose weights are all alike: eight weights at the reference add up to
+    more than one of them may be in fp32 calls."""
+    bt = Batch(new, [700, 90, 1500][:len(new)], heads, 2, D, 32, seed=29).fill(0.3)
+    q = np.random.default_rng(4).standard_normal((bt.tokens, heads, D)) * size
+    for dtype in ("f32", "bf16"):
+        for hint in HINTS:
+            check_tree(bt, dtype, masks(bt, np.random.default_rng(6), "tree"), q=q, max_new=max(new), max_len=hint)
+
+
+def test_flat_scores_take_no_longer():
+    """fp32 over 4 x 16048 tokens: all scores equal, beside one token of every 32
+    that holds nearly all weight.  No reference moves in either, so that the same
+    instructions run; were a row's reference looked for again in every block of the
+    flat ones, they would take 1.6 times as long (226 us beside 143)."""
+    seqs, new, length, kv, heads, D, P = 4, 48, 16048, 8, 32, 128, 64
+    cols = -(-length // P)
+    table = torch.arange(seqs * cols, dtype=torch.int32, device="cuda").view(seqs, cols)
+    keys = torch.zeros((length, kv, D), device="cuda")
+    keys[::32, :, 0] = 15.0
+    none = torch.zeros((length, 0), device="cuda")
+    pools = []
+    for k in (torch.zeros_like(keys), keys):
+        pool = at().kv4_pool(seqs * cols, kv, P, D)
+        for b in range(seqs):
+            at().kv4_append(k, k, torch.zeros_like(k), none, none, pool, table[b:b + 1], ints([0, length]), ints([length]))
+        pools.append(pool)
+    start, lengths = ints([new * b for b in range(seqs + 1)]), ints([length] * seqs)
+    _, seen = dr().draft_tree(ints(([-1] + list(range(new - 1))) * seqs), start, lengths, new)
+    q = torch.zeros((seqs * new, heads, D), device="cuda")
+    q[:, :, 0] = 1.0
+    out, best = torch.empty_like(q), [float("inf")] * 2
+    for _ in range(9):
+        for i, pool in enumerate(pools):
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            begin.record()
+            for _ in range(10):
+                at().kv4_tree_attention(q, pool, table, start, lengths, seen, 1.0, max_new=new, max_len=length, out=out)
+            end.record()
+            end.synchronize()
+            best[i] = min(best[i], begin.elapsed_time(end))
+    assert best[0] < 1.25 * best[1], best
+
+
 def test_more_sequences_than_a_plan_holds():
     bt = Batch([2, 1] * 150, [5, 17] * 150, 2, 1, 64, 16, seed=3).fill(0.3)
     check_tree(bt, "bf16", masks(bt, np.random.default_rng(7), "tree"), max_len=1 << 20)
