@@ -564,7 +564,9 @@ int moe_kv4_tree_attention(const moe_kv4_batch *b, const void *q, int64_t q_stri
  * [seqs]: the next token.  A sequence without new tokens has count 0 and next -1;
  * next is also -1 where the weights' sum is 0, infinite or NaN.  An id outside
  * 0 .. vocab - 1 is refused with weight 0.  Of a sequence's tokens the first 1024
- * take part; vocab is in [1, 2^24].  The workspace (16-byte aligned; NULL if it is 0
+ * take part; vocab is in [1, 2^24].  With q every refused child costs a pass over
+ * its parent's row; from 65536 ids and up to 128 sequences on, workgroups share the
+ * first 128 passes of a sequence (at 131072 ids some 5 us each, 20 those behind them).  The workspace (16-byte aligned; NULL if it is 0
  * bytes) must hold moe_verify_drafts_workspace_bytes (0 for invalid arguments as
  * well); what it holds before does not matter. */
 size_t moe_verify_drafts_workspace_bytes(int seqs, int vocab);

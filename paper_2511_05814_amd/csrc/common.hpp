@@ -358,7 +358,7 @@ struct VerifyArgs {
   int seqs, tokens, vocab, clusters;
 };
 constexpr int kMaxClusters = 64;    // workgroups of a sequence
-constexpr int kVerifyPasses = 16;   // over its rows, that they share
+constexpr int kVerifyPasses = 128;  // over its rows, that they share
 int verify_clusters(int seqs, int vocab);
 hipError_t launch_verify_drafts(const VerifyArgs &a, bool f32, hipStream_t s);
 

@@ -527,6 +527,62 @@ def test_verify_of_more_passes_than_are_shared(vocab, drawn):
     check_verify(lists, p, q_, ids, u, "f32")
 
 
+def refusals(count, vocab):
+    """A first token whose children are all refused: the draft was sure of ids that
+    the target hardly has."""
+    p, q = np.full((2, count + 1, vocab), 1 / vocab, dtype=np.float32)
+    q[:, :count] = 0.5 / count
+    q[:, count:] = 0.5 / (vocab - count)
+    return [[-1] + [0] * count], p, q, np.arange(-1, count, dtype=np.int32), np.full(count + 1, 0.75, dtype=np.float32)
+
+
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("count", [16, 17, 127, 128, 129, 250])
+def test_verify_of_passes_around_the_last_shared_one(count, drawn):
+    """In powers of two: T is always the same sum and S a multiple of it, exact."""
+    vocab = 66000
+    p, q = np.full((count + 1, vocab), 2.0 ** -17, dtype=np.float32), np.zeros((count + 1, vocab), dtype=np.float32)
+    q[:, :256] = 2.0 ** -8
+    u = np.full(count + 1, 0.75, dtype=np.float32)
+    _, kept, after = check_verify([[-1] + [0] * count], p, q if drawn else None, np.arange(-1, count, dtype=np.int32), u, "f32")
+    assert kept[0] == 1 and after[0] >= (256 if drawn else count)
+
+
+@pytest.mark.parametrize("count", [127, 128, 129, 140])
+def test_verify_where_refusals_leave_less_than_a_rounding(count):
+    """Ids from `count` on, all alike, keep p - S q > 0 in exact numbers, and every
+    refusal halves it: S comes within rounding (2^-52 of itself) of p / q long before
+    the last one.  Then |p - S q| <= 2^-51 p whatever was rounded where, and the
+    sign that its rounding has says whether these ids are drawn from, as in exact
+    numbers, or, nothing being left, p itself.  Both draws are of equal weights: the
+    least id at which their share passes 3/4, or, where it is 3/4 of them but for
+    the sums' rounding, the one in front of it."""
+    vocab = 66000
+    lists, p, q, ids, u = refusals(count, vocab)
+    path, kept, after = dr().verify_drafts(*(torch.from_numpy(p).cuda(), ints(ids), ints(lists[0]), torch.from_numpy(u).cuda(), ints([0, count + 1])),
+                                           q=torch.from_numpy(q).cuda())
+    assert kept.tolist() == [1] and path.tolist() == [0] + [-1] * count
+    left, whole = count + 3 * (vocab - count) // 4, 3 * vocab // 4
+    assert after.item() in (left, left - 1, whole, whole - 1)
+
+
+@pytest.mark.parametrize("count", [1, 16, 17, 60, 128])
+def test_verify_shares_its_passes(count):
+    """As many sums in the workspace as there were passes and workgroups: one that is
+    not told to the others is worked out by each of them."""
+    from paper_2511_05814_amd import binding as b
+    vocab = 66000
+    (parent,), p, q, ids, u = refusals(count, vocab)
+    p, q, u = (torch.from_numpy(x).cuda() for x in (p, q, u))
+    ids, parent, start, path, one, after = (ints(x) for x in (ids, parent, [0, count + 1], ids, [0], [0]))
+    ws = torch.zeros(b.moe_verify_drafts_workspace_bytes(1, vocab), dtype=torch.uint8, device="cuda")
+    b.moe_verify_drafts(*(x for t in (p, q) for x in (t.data_ptr(), vocab)), ids.data_ptr(), parent.data_ptr(), u.data_ptr(), start.data_ptr(),
+                        1, count + 1, vocab, b.MOE_DTYPE_F32, path.data_ptr(), one.data_ptr(), after.data_ptr(), ws.data_ptr(), ws.numel(),
+                        torch.cuda.current_stream().cuda_stream)
+    told = int((ws.view(torch.int64) != -1).sum())
+    assert one.item() == 1 and told == count * (vocab // 16384)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("vocab", [60, 5000, 70001])
 def test_verify_reads_no_q_of_tokens_without_children(vocab, dtype):
