@@ -214,6 +214,7 @@ class Speculation:
         self.embedding = torch.from_numpy(rng.standard_normal((vocab, d), dtype=np.float32)).to("cuda")
         self.head = torch.from_numpy(wl.quantize_q4g64(rng.standard_normal((vocab, d), dtype=np.float32) * np.float32(3 * d ** -0.5))).to("cuda")
         self.gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.hidden: Optional[torch.Tensor] = None   # of the last step's tokens, behind all layers
 
     def probabilities(self, h: torch.Tensor) -> torch.Tensor:
         """Of the token behind each row of hidden states, fp32 [rows, vocab]."""
@@ -245,7 +246,7 @@ class Speculation:
         parents, tokens, q = self.draft(pending[active])
         batch = seqs.extend([self.nodes if b in active else 0 for b in range(len(pending))],
                             [parents if b in active else [] for b in range(len(pending))])
-        H = self.embedding[tokens.flatten()]
+        H = self.hidden = self.embedding[tokens.flatten()]
         stack.step(H, batch)
         torch.cuda.current_stream().wait_stream(moe.compute)
         u = torch.rand(H.shape[0], generator=self.gen, device="cuda")
@@ -291,14 +292,15 @@ def main(argv=None) -> None:
         return H
 
     t0 = time.perf_counter()
-    take(0, a.prompt)
+    H = take(0, a.prompt)
     t1 = time.perf_counter()
     if a.drafts:
         spec = Speculation(stack, a.vocab, a.drafts, a.width)
-        pending, steps, H = torch.arange(a.sequences, device="cuda") % a.vocab, 0, states
+        pending, steps = torch.arange(a.sequences, device="cuda") % a.vocab, 0
         while min(seqs.length) < total:
             active = [b for b, n in enumerate(seqs.length) if n < total]
             pending, taken = spec.step(seqs, pending, active)
+            H = spec.hidden
             steps += len(active)
         moe.sync()
         made = sum(seqs.length) - a.sequences * a.prompt

@@ -85,6 +85,18 @@ def test_speculation_takes_what_it_keeps():
         pending = after
 
 
+@pytest.mark.parametrize("tokens,drafts", [("6", "0"), ("6", "5"), ("0", "0"), ("0", "5")])
+def test_the_command_shows_what_came_out(tokens, drafts, capsys, monkeypatch):
+    """The rms that it prints is that of the last step's hidden states behind all layers."""
+    from paper_2511_05814_amd import decoder
+    step, states = decoder.DecoderStack.step, []
+    monkeypatch.setattr(decoder.DecoderStack, "step", lambda self, H, *a, **k: (states.append((H, H.clone())), step(self, H, *a, **k)))
+    decoder.main(["--config", "tiny-stack", "--sequences", "2", "--prompt", "5", "--tokens", tokens, "--drafts", drafts, "--vocab", "200"])
+    said = capsys.readouterr().out.split("last rms ")[1].split()[0]
+    behind, entering = (f"{x.square().mean().sqrt().item():.4f}" for x in states[-1])
+    assert said == behind != entering and np.isfinite(float(said))
+
+
 @pytest.mark.parametrize("drafts", ["0", "5"])
 def test_the_command(drafts, capsys):
     from paper_2511_05814_amd import decoder
