@@ -291,11 +291,11 @@ def main(argv=None) -> None:
         moe.sync()
         return H
 
+    spec = Speculation(stack, a.vocab, a.drafts, a.width) if a.drafts else None
     t0 = time.perf_counter()
     H = take(0, a.prompt)
     t1 = time.perf_counter()
     if a.drafts:
-        spec = Speculation(stack, a.vocab, a.drafts, a.width)
         pending, steps = torch.arange(a.sequences, device="cuda") % a.vocab, 0
         while min(seqs.length) < total:
             active = [b for b, n in enumerate(seqs.length) if n < total]

@@ -97,6 +97,18 @@ def test_the_command_shows_what_came_out(tokens, drafts, capsys, monkeypatch):
     assert said == behind != entering and np.isfinite(float(said))
 
 
+def test_the_command_times_steps_alone(monkeypatch):
+    """An embedding and a head are made before the clock starts: tokens/s are those of
+    the steps."""
+    import time
+    from paper_2511_05814_amd import decoder
+    clock, make, said = time.perf_counter, decoder.Speculation.__init__, []
+    monkeypatch.setattr(time, "perf_counter", lambda: (said.append("clock"), clock())[1])
+    monkeypatch.setattr(decoder.Speculation, "__init__", lambda self, *a, **k: (said.append("make"), make(self, *a, **k))[1])
+    decoder.main(["--config", "tiny-stack", "--sequences", "1", "--prompt", "3", "--tokens", "2", "--drafts", "3", "--vocab", "200"])
+    assert said.index("make") < said.index("clock") and said.count("make") == 1
+
+
 @pytest.mark.parametrize("drafts", ["0", "5"])
 def test_the_command(drafts, capsys):
     from paper_2511_05814_amd import decoder
