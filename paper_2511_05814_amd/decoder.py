@@ -135,6 +135,9 @@ class DecoderStack:
             raise ValueError(f"H must be float32 [tokens, {self.moe.cfg.d_model}], not {H.dtype} {list(H.shape)}")
         if batch.get("tokens", H.shape[0]) != H.shape[0]:
             raise ValueError(f"{H.shape[0]} rows of H for a plan of {batch['tokens']} tokens")
+        self._check_plan(batch)
+
+    def _check_plan(self, batch: dict) -> None:
         if batch.get("longest", 0) > self.max_pos:
             raise ValueError(f"a sequence of {batch['longest']} tokens, but positions end at {self.max_pos}")
         if batch.get("page_size", self.page_size) != self.page_size or batch.get("pages", 0) > self.pages:
@@ -194,6 +197,9 @@ class DecoderStack:
         all layers' caches; enqueued on moe.compute, in line with the steps.
         `Sequences.keep` takes the counts, once the host has them."""
         moe = self.moe
+        self._check_plan(batch)
+        if batch.get("tokens", path.numel()) != path.numel():
+            raise ValueError(f"a path of {path.numel()} tokens for a plan of {batch['tokens']}")
         for t in (batch["page_table"], batch["q_start"], batch["kv_len"], path, count):
             t.record_stream(moe.compute)
         moe.compute.wait_stream(torch.cuda.current_stream())

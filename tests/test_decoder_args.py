@@ -122,6 +122,15 @@ def test_more_kept_than_there_was(count, monkeypatch):
     assert s.length == [2, 0]
 
 
+@pytest.mark.parametrize("wrong,says", [(dict(page_size=32), "pages of 32"), (dict(pages=4), "4 pages"), (dict(longest=41), "positions end at 40"),
+                                        (dict(tokens=3), "plan of 3"), (dict(tokens=1), "plan of 1")])
+def test_keeping_by_a_plan_for_another_stack(wrong, says):
+    """Entries would move between places that are not these tokens'."""
+    path, count = (torch.zeros(n, dtype=torch.int32) for n in (2, 1))
+    with pytest.raises(ValueError, match=says):
+        stack().keep(plan(**wrong), path, count)
+
+
 @pytest.mark.parametrize("vocab,nodes,width", [(0, 4, 2), (9, 0, 2), (9, -1, 2), (9, 1025, 2), (9, 4, 0)])
 def test_trees_that_cannot_be_drafted(vocab, nodes, width):
     with pytest.raises(ValueError, match="cannot be drafted"):
