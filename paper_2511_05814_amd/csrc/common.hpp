@@ -305,8 +305,10 @@ struct KvAttnArgs {
   const void *q;
   void *o;
   int64_t q_stride, o_stride;
-  float *part;                 // [splits][tokens * heads][D]
-  float *ml;                   // [splits][tokens * heads][2]
+  // Parts of rows to be joined: a row each of every split, or, of the tree kernels,
+  // two places of each workgroup (`splits` of them) with the rows of a unit each.
+  float *part;                 // [splits][tokens * heads][D], or [splits][2][16 * tiles][D]
+  float *ml;                   // as many rows of 2: largest score and sum of weights
   float scale;
   int heads, splits, row_blocks, prompt;
   const uint32_t *seen;        // [tokens][words], which new tokens a token sees; NULL: those before it

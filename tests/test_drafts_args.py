@@ -64,6 +64,21 @@ def test_tree_attention_overlaps():
     b.moe_kv4_tree_attention(*tree_attend(batch(tokens=0)))
 
 
+@pytest.mark.parametrize("dtype,max_new,most,groups,rows", [(F32, 1, 251, 512, 16), (BF16, 64, 4031, 256, 256)])
+def test_tree_attention_of_more_work_than_an_int_counts(dtype, max_new, most, groups, rows):
+    """Kernels that share all steps out number them: (4 tokens / rows + 1) blocks of each
+    of 2048 pairs (sequence, kv head), whatever q_start holds, of 2^20 / 64 + 6 steps
+    at most, 2^31 / 2048 / 16390 = 63.98.  One block more and the call is cut as
+    moe_kv4_attention's is."""
+    bt = batch(head_dim=128, kv_heads=8, seqs=256, page_size=1024, table_cols=1024, table_stride=1024, tokens=most)
+    need = b.moe_kv4_tree_attention_workspace_bytes(bt, 32, dtype, max_new, 4096)
+    assert need == groups * 2 * rows * (128 + 2) * 4 + 257 * 4
+    bt.tokens = most + 1
+    assert b.moe_kv4_tree_attention_workspace_bytes(bt, 32, dtype, max_new, 4096) == b.moe_kv4_attention_workspace_bytes(bt, 32, max_new, 4096) != need
+    bt.table_cols = 1023
+    assert b.moe_kv4_tree_attention_workspace_bytes(bt, 32, dtype, max_new, 4096) == need
+
+
 @pytest.mark.parametrize("bad", [dict(parent=None), dict(parent=A + 1), dict(q_start=None), dict(kv_len=None), dict(pos=None), dict(seen=None),
                                  dict(pos=C + 2), dict(seqs=0), dict(seqs=(1 << 20) + 1), dict(tokens=-1), dict(tokens=(1 << 24) + 1),
                                  dict(words=0), dict(words=33)])

@@ -349,6 +349,37 @@ def test_strided_queries_given_outputs_and_workspaces():
         assert torch.equal(wide[:, 2:10], want)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads", [4, 16])
+@pytest.mark.parametrize("hint", HINTS)
+def test_starts_that_go_back_or_past_the_tokens(hint, heads, dtype):
+    """Bounds are cut to the tokens that there are, and to no fewer than none; rows
+    of one sequence alone are right whatever the others claim."""
+    starts_, tokens, D = [0, 12, 5, 30, 2 ** 31 - 1, 40, 60, -7, 3], 60, 128
+    ends = [min(max(e, 0), tokens) for e in starts_]
+    spans = [(s, max(s, e)) for s, e in zip(ends, ends[1:])]   # 12, 0, 25, 30, 0, 20, 0 and 3 tokens
+    bt = Batch([e - s for s, e in spans], [300, 20, 700, 64, 5, 130, 10, 33], heads, 2, D, 16, seed=31).fill(0.3)
+    rng = np.random.default_rng(4)
+    q = rng.standard_normal((tokens, heads, D)) * 2
+    q = bf16(q) if dtype == "bf16" else q.astype(np.float32)
+    seen = rng.random((tokens, 64)) < 0.5
+    mine = [seen[s:e, :e - s] for s, e in spans]
+    pool, table, _, length = bt.args()
+    bits = ints(od.words_of(seen, 2))
+    o = host(at().kv4_tree_attention(device(q, dtype), pool, table, ints(starts_), length, bits, D ** -0.5, max_len=hint))
+    want, reach, top = attend(bt, np.concatenate([q[s:e] for s, e in spans]).astype(np.float64), D ** -0.5, mine)
+    checked = 0
+    for b, (s, e) in enumerate(spans):
+        got, row = o[s:e], slice(bt.q_start[b], bt.q_start[b + 1])
+        prob = 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22   # as in check_tree
+        tol = top[row] * (2 * reach[row] * (2.0 ** -22 + 2 * D * U) + 2 * prob + 64 * U)
+        tol = tol[..., None] + (BF * np.abs(want[row]) if dtype == "bf16" else 0)
+        alone = [i for i in range(e - s) if sum(x <= s + i < y for x, y in spans) == 1]
+        assert (np.abs(got - want[row]) <= tol)[alone].all(), b
+        checked += len(alone)
+    assert checked == 2 + 18 + 10
+
+
 @pytest.mark.parametrize("size", [0.0, 1e-3, 0.05])
 @pytest.mark.parametrize("D,heads,new", [(64, 4, [20, 1, 33]), (128, 8, [9, 4, 2]), (128, 4, [40, 70])])
 def test_flat_scores(D, heads, new, size):
