@@ -508,9 +508,9 @@ int moe_kv4_attention(const moe_kv4_batch *b, const void *q, int64_t q_stride, v
  * Steps with drafted tokens.  A sequence's new tokens are a tree: the first is
  * its pending token, each other follows another one of them (its parent), as
  * one of several guesses.  Token i keeps place kv_len[b] - n + i of the cache,
- * but its position, for which it is rotated, is that of its depth.  Because the
- * experts that a layer copies serve all tokens of a call (Sec. 2.2), a few
- * guesses cost little more than the pending token alone.  The calls in order:
+ * but its position, for which it is rotated, is that of its depth.  An expert that
+ * a layer copies serves all tokens of a call that chose it (Sec. 2.2), so a tree
+ * costs the copies of its tokens' distinct experts, not of every token's.  The calls in order:
  * moe_draft_tree once a step; moe_kv4_append_at and moe_kv4_tree_attention in
  * every layer; moe_verify_drafts; moe_kv4_keep once for all layers. */
 

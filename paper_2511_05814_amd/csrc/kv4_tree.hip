@@ -933,13 +933,21 @@ void launch(const KvAttnArgs &a, int tiles, hipStream_t s) {
 //     2 of 1000 over 1000                      4000    16    121    159     112       79   74
 //     1 of 24 over 131071                        48  1025    112    180     118       97  103
 //     8 of up to 64 over up to 16383           1024   129    145    247     157      111   99
-//   fp32, scores with a spread of 2 / of 0.2 about their mean, whose blocks need the
+//   fp32, scores of a row with a standard deviation of 2.4 / of 0.24, which needs the
 //   reference moved less often:
 //     16 of 12 over 8191                        384    65    70/67  65/52   75/53
 //     10 of 49 over 1393                       1040    12    50/47  47/40   51/38
 //     4 of 48 over 16000                        384   126   178/167 134/116 124/86
 //     16 heads to 16, 32 of 32 over 2047       1024    17    56/53  63/52   68/49
 //     the same over 6000                       1024    48   130/127 123/101 124/89
+//   heads of 64: 64 of 8 over 700              1024     6     20     24      23       31
+//     64 of 8 over 1800                        1024    15     37     38      34       46
+//     32 of 8 over up to 4095                   512    33     36     31      28       37
+//     1 of 8 over 4096                           16    33     15     13      14       16
+//     4 of 16 over 8191                         128    65     30     22      23       28
+//     16 of 24 over 8191                        768    65     68     79      56       51
+//     1 of 24 over 131071                        48  1025     88    131      84       70
+//     8 of up to 64 over up to 16383           1024   129    112    179     113       77
 // The plan and the join cost more than they save where units have few steps, and where there
 // is little to share out.
 KvAttnShape kv4_tree_shape(int seqs, int kv_heads, int heads, int tokens, int max_new, int max_len, int64_t table_tokens, int head_dim, bool f32) {

@@ -1,7 +1,8 @@
 """Steps that take several drafted tokens of a sequence at once.
 
-A layer's expert copies serve every token of a call, so a sequence's pending
-token and a tree of guesses behind it cost little more than the token alone.
+An expert that a layer copies serves every token of a call that chose it, so a
+sequence's pending token and a tree of guesses behind it cost the copies of their
+distinct experts: fewer than the tokens one after another, more than one alone.
 The tree's tokens are a sequence's new tokens, the pending one first; each other
 names its parent.  A step is
 
